@@ -60,8 +60,16 @@ typedef enum {
     ROI_ERR_ALIAS = 6,     /* an output overlaps an input or another output              */
     ROI_ERR_CUDA = 7,      /* launch failed (cudaGetLastError after the launch)          */
     ROI_ERR_TIMEOUT = 8,   /* a kernel gave up waiting on its own copies (see below)     */
-    ROI_ERR_OPT = 9        /* bad optimizer settings (roi_mask_bwd_adamw)                */
+    ROI_ERR_OPT = 9,       /* bad optimizer settings (roi_mask_bwd_adamw)                */
+    ROI_ERR_TYPE = 10      /* unknown element type or norm kind, or eps not finite >= 0  */
 } roi_status;
+
+/* Element types of the calls that take more than one. */
+typedef enum {
+    ROI_BF16 = 0,
+    ROI_FP16 = 1,
+    ROI_FP32 = 2
+} roi_dtype;
 
 /* Noise state of one call (Sec. 4.2.3 sampling temperature included).
  *  seed, step, tensor_id: Philox key and counter words (see above); tensor_id
@@ -310,6 +318,86 @@ roi_status roi_masked_linear_fwd_noalloc(const roi_bf16* X, const float* logits,
 roi_status roi_hard_mask_export(const float* logits, int N, int M, int64_t rows, int64_t cols,
                                 uint32_t* out_bits, const roi_bf16* W, roi_bf16* out_Wpruned,
                                 void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Around the masked linear layers in training.  Every masked layer needs its
+ * input X again in the backward pass, where dWm = dY^T X is what roi_mask_bwd
+ * starts from.  These calls keep such activations in 8 bits, form dWm from them,
+ * and are the norms that make and use them.
+ *
+ * Matrices of these calls (x, y, dy, dx, dY) are row-major with a row stride ld in
+ * elements, ld >= cols, and need only the alignment of their elements, except dY;
+ * base pointers and strides that are multiples of 16 bytes take the fast paths.
+ * Outputs may lie between the rows of inputs, but not on them.
+ *
+ * A checkpoint is a pair of arrays.  Blocks of 32 consecutive columns of a row share
+ * a power of two:
+ *   codes  [rows, roi_checkpoint_pitch(cols)] int8: cols rounded up to 32
+ *   scales [rows, roi_checkpoint_scale_pitch(cols)] uint8: 4 for every 128 columns begun
+ * With a the block's largest magnitude, its scale byte is
+ *   s = clamp((bits(a) + 0xffff) >> 23, 7, 254), bits(a) the float32 pattern of a,
+ * so that s - 133 is the least exponent e with a <= 127.5 * 2^e; a code is
+ *   q = clamp(round_half_even(x * 2^(133 - s)), -127, 127)
+ * and stands for q * 2^(s - 133), at most half of 2^(s - 133) from x (a block whose
+ * largest magnitude is under 127.5 * 2^-126 is held to multiples of 2^-126, one over
+ * 127.5 * 2^121 to magnitudes up to 127 * 2^121).  bf16 and float32 hold these values exactly.  A block with an
+ * infinity or a NaN has s = 255 and codes 0 and stands for NaN throughout.  The sign
+ * of zero is not kept.  Padding codes are 0, padding scale bytes 7.  Both arrays are
+ * contiguous, codes 16-byte and scales 4-byte aligned, as every row of theirs is: rows
+ * may be saved, loaded and used in slices.
+ */
+int64_t roi_checkpoint_pitch(int64_t cols);
+int64_t roi_checkpoint_scale_pitch(int64_t cols);
+
+/* Saves x [rows, cols] of type dtype (roi_dtype). */
+roi_status roi_checkpoint_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx,
+                               int8_t* out_codes, uint8_t* out_scales, void* stream);
+
+/* Restores the values a checkpoint stands for, rounded to dtype (fp16: magnitudes past
+ * 65504 become 65504).  Scale bytes below 7, which no call writes, stand for zero. */
+roi_status roi_checkpoint_load(const int8_t* codes, const uint8_t* scales, int dtype, int64_t rows, int64_t cols,
+                               void* out_x, int64_t ldx, void* stream);
+
+typedef enum {
+    ROI_LAYER_NORM = 0, /* y = (x - mean) * rstd * gamma + beta                      */
+    ROI_RMS_NORM = 1    /* y = x * rstd * gamma; no mean, no beta                    */
+} roi_norm_kind;
+
+/* Norm of each row: rstd = 1 / sqrt(mean((x - mean)^2) + eps), mean 0 for
+ * ROI_RMS_NORM; in fp32, y rounded once.
+ *  x, out_y  [rows, cols] of type dtype
+ *  gamma     [cols] of type param_dtype, which is dtype or ROI_FP32; nullable (1)
+ *  beta      [cols] of type param_dtype; nullable (0); NULL for ROI_RMS_NORM
+ *  eps       finite, >= 0
+ *  out_mean, out_rstd  [rows] float32, nullable; out_mean NULL for ROI_RMS_NORM
+ *  out_xcodes, out_xscales  nullable together: the checkpoint of x
+ *  out_ycodes, out_yscales  nullable together: the checkpoint of out_y as it was
+ *    rounded, the input of the masked layers that follow                          */
+roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int kind,
+                        const void* gamma, const void* beta, int param_dtype, float eps,
+                        void* out_y, int64_t ldy, float* out_mean, float* out_rstd,
+                        int8_t* out_xcodes, uint8_t* out_xscales, int8_t* out_ycodes, uint8_t* out_yscales,
+                        void* stream);
+
+/* Backward of the norm.  With xh = (x - mean) * rstd and a = dy * gamma:
+ *   dx = rstd * (a - mean(a) [ROI_LAYER_NORM] - xh * mean(a * xh))
+ *   dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
+ *  dy, out_dx [rows, cols] of type dtype
+ *  x          [rows, cols] of type dtype, or NULL with codes and scales, the
+ *             checkpoint of x, in its place (exactly one of the two)
+ *  mean       [rows] float32 of the forward; NULL for ROI_RMS_NORM
+ *  rstd       [rows] float32 of the forward
+ *  out_dgamma, out_dbeta  [cols] float32, nullable; OVERWRITTEN (0 where rows == 0);
+ *             out_dbeta NULL for ROI_RMS_NORM.  The sums are taken in a fixed order:
+ *             the same inputs give the same bits.
+ *  workspace  roi_norm_bwd_workspace_size bytes where out_dgamma or out_dbeta is
+ *             given (ROI_ERR_NULL without, ROI_ERR_SHAPE where smaller)            */
+size_t roi_norm_bwd_workspace_size(int64_t rows, int64_t cols);
+roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, int64_t lddy,
+                        const void* x, int64_t ldx, const int8_t* codes, const uint8_t* scales, int kind,
+                        const void* gamma, int param_dtype, const float* mean, const float* rstd,
+                        void* out_dx, int64_t lddx, float* out_dgamma, float* out_dbeta,
+                        void* workspace, size_t workspace_bytes, void* stream);
 
 /* The noise of a call, materialised (for inspecting or reproducing a sample; the
  * mask calls never store it).  st->lambda is ignored; st->row_offset applies.

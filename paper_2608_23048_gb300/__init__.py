@@ -18,6 +18,8 @@ __all__ = [
     "library_path", "hard_words", "roi_noise_words", "roi_gumbel_noise",
     "roi_mask_fwd_st", "roi_mask_bwd_st", "roi_export_compressed_2of4", "AdamW", "roi_mask_bwd_adamw",
     "roi_anneal", "roi_set_ring_wait_limit_ns",
+    "roi_checkpoint_pitch", "roi_checkpoint_scale_pitch", "roi_checkpoint_save", "roi_checkpoint_load",
+    "new_checkpoint", "roi_norm_fwd", "roi_norm_bwd", "roi_norm_bwd_workspace_size",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -25,7 +27,8 @@ library_path = os.path.join(_PKG, "libroi.so")
 
 ROI_OK = 0
 STATUS_NAMES = {0: "ROI_OK", 1: "ROI_ERR_NULL", 2: "ROI_ERR_SHAPE", 3: "ROI_ERR_NM", 4: "ROI_ERR_TAU",
-                5: "ROI_ERR_ALIGN", 6: "ROI_ERR_ALIAS", 7: "ROI_ERR_CUDA", 8: "ROI_ERR_TIMEOUT", 9: "ROI_ERR_OPT"}
+                5: "ROI_ERR_ALIGN", 6: "ROI_ERR_ALIAS", 7: "ROI_ERR_CUDA", 8: "ROI_ERR_TIMEOUT", 9: "ROI_ERR_OPT",
+                10: "ROI_ERR_TYPE"}
 
 
 class RoiError(RuntimeError):
@@ -111,6 +114,17 @@ def lib() -> ctypes.CDLL:
     L.roi_anneal.argtypes = [f32, f32, u32, u32]
     L.roi_anneal.restype = f32
     L.roi_hard_mask_export.argtypes = [_P, i32, i32, i64, i64, _P, _P, _P, _P]
+    L.roi_checkpoint_pitch.argtypes = [i64]
+    L.roi_checkpoint_pitch.restype = i64
+    L.roi_checkpoint_scale_pitch.argtypes = [i64]
+    L.roi_checkpoint_scale_pitch.restype = i64
+    L.roi_checkpoint_save.argtypes = [_P, i32, i64, i64, i64, _P, _P, _P]
+    L.roi_checkpoint_load.argtypes = [_P, _P, i32, i64, i64, _P, i64, _P]
+    L.roi_norm_fwd.argtypes = [_P, i32, i64, i64, i64, i32, _P, _P, i32, f32, _P, i64, _P, _P, _P, _P, _P, _P, _P]
+    L.roi_norm_bwd.argtypes = [_P, i32, i64, i64, i64, _P, i64, _P, _P, i32, _P, i32, _P, _P, _P, i64, _P, _P, _P,
+                               ctypes.c_size_t, _P]
+    L.roi_norm_bwd_workspace_size.argtypes = [i64, i64]
+    L.roi_norm_bwd_workspace_size.restype = ctypes.c_size_t
     L.roi_device_status.argtypes = [_P]
     L.roi_set_ring_wait_limit_ns.argtypes = [u64]
     L.roi_noise_words.argtypes = [ctypes.POINTER(NoiseState), i64, i64, _P, _P]
@@ -124,7 +138,8 @@ def lib() -> ctypes.CDLL:
                  "roi_export_compressed_2of4", "roi_mask_bwd_adamw", "roi_masked_linear_fwd",
                  "roi_masked_linear_fwd_noalloc", "roi_mask_fwd_batch", "roi_mask_bwd_batch",
                  "roi_mask_bwd_adamw_batch", "roi_mask_fwd_st_batch", "roi_mask_bwd_st_batch",
-                 "roi_set_ring_wait_limit_ns"):
+                 "roi_set_ring_wait_limit_ns", "roi_checkpoint_save", "roi_checkpoint_load", "roi_norm_fwd",
+                 "roi_norm_bwd"):
         getattr(L, name).restype = i32
     _LIB = L
     return L
@@ -453,6 +468,155 @@ def roi_hard_mask_export(logits, N, M, out_bits, W=None, out_Wpruned=None, strea
     s = lib().roi_hard_mask_export(_ptr(logits), int(N), int(M), rows, cols, _ptr(out_bits), _ptr(W),
                                    _ptr(out_Wpruned), _stream(stream))
     _raise(s, "roi_hard_mask_export")
+
+
+# ---------------------------------------------------------------------------
+# around the masked linear layers: 8-bit checkpoints, norms, weight gradients
+# ---------------------------------------------------------------------------
+NORM_KINDS = {"layer": 0, "rms": 1}
+
+
+def _dtype(t, name):
+    import torch
+    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"{name}: expected bfloat16, float16 or float32, got {t.dtype}")
+    return code
+
+
+def _matrix(t, name, dtype=None, shape=None):
+    """Checks a matrix whose rows may be apart; returns its row stride in elements."""
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor")
+    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: expected {'a matrix' if shape is None else f'shape {tuple(shape)}'}, got {tuple(t.shape)}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    # the stride of a single row says nothing
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def roi_checkpoint_pitch(cols) -> int:
+    """Codes in a row of a checkpoint of `cols` columns."""
+    return int(lib().roi_checkpoint_pitch(int(cols)))
+
+
+def roi_checkpoint_scale_pitch(cols) -> int:
+    """Scale bytes in a row of a checkpoint of `cols` columns."""
+    return int(lib().roi_checkpoint_scale_pitch(int(cols)))
+
+
+def new_checkpoint(rows, cols, device="cuda"):
+    """Uninitialised (codes, scales) for a matrix [rows, cols]."""
+    import torch
+    return (torch.empty(rows, roi_checkpoint_pitch(cols), dtype=torch.int8, device=device),
+            torch.empty(rows, roi_checkpoint_scale_pitch(cols), dtype=torch.uint8, device=device))
+
+
+def _checkpoint(codes, scales, name, rows, cols):
+    import torch
+    if (codes is None) != (scales is None):
+        raise ValueError(f"{name}: codes and scales go together")
+    _check_tensor(codes, f"{name} codes", torch.int8, (rows, roi_checkpoint_pitch(cols)))
+    _check_tensor(scales, f"{name} scales", torch.uint8, (rows, roi_checkpoint_scale_pitch(cols)))
+
+
+def roi_checkpoint_save(x, out_codes, out_scales, stream=None):
+    """Saves x [rows, cols] (bfloat16, float16 or float32; rows may be apart) in 8 bits."""
+    rows, cols = x.shape
+    ld = _matrix(x, "x")
+    _checkpoint(out_codes, out_scales, "out", rows, cols)
+    s = lib().roi_checkpoint_save(_ptr(x), _dtype(x, "x"), rows, cols, ld, _ptr(out_codes), _ptr(out_scales),
+                                  _stream(stream))
+    _raise(s, "roi_checkpoint_save")
+
+
+def roi_checkpoint_load(codes, scales, out_x, stream=None):
+    """The values a checkpoint stands for, in the type of out_x [rows, cols]."""
+    rows, cols = out_x.shape
+    ld = _matrix(out_x, "out_x")
+    _checkpoint(codes, scales, "checkpoint", rows, cols)
+    s = lib().roi_checkpoint_load(_ptr(codes), _ptr(scales), _dtype(out_x, "out_x"), rows, cols, _ptr(out_x), ld,
+                                  _stream(stream))
+    _raise(s, "roi_checkpoint_load")
+
+
+def _norm_kind(kind):
+    if kind not in NORM_KINDS:
+        raise ValueError(f"kind: expected one of {sorted(NORM_KINDS)}, got {kind!r}")
+    return NORM_KINDS[kind]
+
+
+def _param_dtype(x, *params):
+    """The type code of gamma and beta (that of x, or float32; one for both)."""
+    import torch
+    given = [(name, p) for name, p in params if p is not None]
+    for name, p in given:
+        if p.dtype not in (x.dtype, torch.float32) or p.dtype != given[0][1].dtype:
+            raise TypeError(f"{name}: expected {x.dtype} or torch.float32, one type for all, got {p.dtype}")
+        _check_tensor(p, name, p.dtype, (x.shape[1],))
+    return _dtype(given[0][1], given[0][0]) if given else _dtype(x, "x")
+
+
+def roi_norm_fwd(x, kind, gamma, beta, eps, out_y, out_mean=None, out_rstd=None, x_checkpoint=None, y_checkpoint=None,
+                 stream=None):
+    """Layer norm ("layer") or RMS norm ("rms") of the rows of x; the checkpoints of x and of
+    out_y ((codes, scales) pairs) are written in the same pass where given."""
+    import torch
+    rows, cols = x.shape
+    ldx, ldy = _matrix(x, "x"), _matrix(out_y, "out_y", x.dtype, x.shape)
+    p = _param_dtype(x, ("gamma", gamma), ("beta", beta))
+    _check_tensor(out_mean, "out_mean", torch.float32, (rows,))
+    _check_tensor(out_rstd, "out_rstd", torch.float32, (rows,))
+    xq, xs = x_checkpoint if x_checkpoint is not None else (None, None)
+    yq, ys = y_checkpoint if y_checkpoint is not None else (None, None)
+    _checkpoint(xq, xs, "x_checkpoint", rows, cols)
+    _checkpoint(yq, ys, "y_checkpoint", rows, cols)
+    s = lib().roi_norm_fwd(_ptr(x), _dtype(x, "x"), rows, cols, ldx, _norm_kind(kind), _ptr(gamma), _ptr(beta), p,
+                           float(eps), _ptr(out_y), ldy, _ptr(out_mean), _ptr(out_rstd), _ptr(xq), _ptr(xs), _ptr(yq),
+                           _ptr(ys), _stream(stream))
+    _raise(s, "roi_norm_fwd")
+
+
+def roi_norm_bwd_workspace_size(rows, cols) -> int:
+    """Bytes of workspace roi_norm_bwd needs for the gradients of weight and bias on the current device."""
+    return int(lib().roi_norm_bwd_workspace_size(int(rows), int(cols)))
+
+
+def _workspace(workspace):
+    """(pointer, bytes) of a workspace tensor of any type."""
+    if workspace is None:
+        return None, 0
+    _check_tensor(workspace, "workspace", workspace.dtype)
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def roi_norm_bwd(dy, x, kind, gamma, mean, rstd, out_dx, out_dgamma=None, out_dbeta=None, workspace=None, stream=None):
+    """Backward of roi_norm_fwd.  x: the forward's input, or its checkpoint, a (codes, scales) pair.
+    out_dgamma, out_dbeta: float32 [cols], overwritten."""
+    import torch
+    rows, cols = dy.shape
+    lddy, lddx = _matrix(dy, "dy"), _matrix(out_dx, "out_dx", dy.dtype, dy.shape)
+    codes = scales = None
+    ldx = cols
+    if isinstance(x, (tuple, list)):
+        codes, scales = x
+        x = None
+        _checkpoint(codes, scales, "x", rows, cols)
+    else:
+        ldx = _matrix(x, "x", dy.dtype, dy.shape)
+    p = _param_dtype(dy, ("gamma", gamma))
+    _check_tensor(mean, "mean", torch.float32, (rows,))
+    _check_tensor(rstd, "rstd", torch.float32, (rows,))
+    _check_tensor(out_dgamma, "out_dgamma", torch.float32, (cols,))
+    _check_tensor(out_dbeta, "out_dbeta", torch.float32, (cols,))
+    ws, ws_bytes = _workspace(workspace)
+    s = lib().roi_norm_bwd(_ptr(dy), _dtype(dy, "dy"), rows, cols, lddy, _ptr(x), ldx, _ptr(codes), _ptr(scales),
+                           _norm_kind(kind), _ptr(gamma), p, _ptr(mean), _ptr(rstd), _ptr(out_dx), lddx,
+                           _ptr(out_dgamma), _ptr(out_dbeta), ws, ws_bytes, _stream(stream))
+    _raise(s, "roi_norm_bwd")
 
 
 def roi_noise_words(state: NoiseState, rows, cols, out_words, stream=None):

@@ -96,6 +96,44 @@ NoiseParams make_noise(const roi_noise_state& st, int64_t cols) {
   return np;
 }
 
+// A row-major matrix with a row stride, as a place in memory: `pitch` and `width` in bytes.
+struct Strided {
+  const void* p;
+  uint64_t rows, pitch, width;
+};
+bool overlaps(const Strided& a, const Strided& b) {
+  if (a.p == nullptr || b.p == nullptr || a.rows == 0 || b.rows == 0) return false;
+  const Range ra = {a.p, (a.rows - 1) * a.pitch + a.width}, rb = {b.p, (b.rows - 1) * b.pitch + b.width};
+  if (!overlaps(ra, rb)) return false;
+  if (a.pitch != b.pitch) return true;
+  // the same stride: apart where neither's columns reach the other's
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a.p), pb = reinterpret_cast<uintptr_t>(b.p);
+  const uint64_t d = pb >= pa ? (pb - pa) % a.pitch : (a.pitch - (pa - pb) % a.pitch) % a.pitch;
+  return !(a.width <= d && d + b.width <= a.pitch);
+}
+Strided flat(const void* p, uint64_t bytes) { return {p, bytes == 0 ? 0u : 1u, bytes, bytes}; }
+template <int NI, int NO>
+bool any_alias(const Strided (&in)[NI], const Strided (&out)[NO]) {
+  for (int o = 0; o < NO; ++o) {
+    for (int i = 0; i < NI; ++i)
+      if (overlaps(out[o], in[i])) return true;
+    for (int p = o + 1; p < NO; ++p)
+      if (overlaps(out[o], out[p])) return true;
+  }
+  return false;
+}
+
+bool known_type(int dtype) { return dtype == ROI_BF16 || dtype == ROI_FP16 || dtype == ROI_FP32; }
+int type_bytes(int dtype) { return dtype == ROI_FP32 ? 4 : 2; }
+// A matrix of `rows` rows with stride ld: sizes that fit.
+bool good_shape(int64_t rows, int64_t cols, int64_t ld) {
+  return rows >= 0 && cols > 0 && cols <= INT64_MAX / 1024 && (rows == 0 || (ld >= cols && ld <= INT64_MAX / 64 / rows));
+}
+bool aligned_to(const void* p, int bytes) { return reinterpret_cast<uintptr_t>(p) % unsigned(bytes) == 0; }
+Strided matrix(const void* p, int64_t rows, int64_t cols, int64_t ld, int bytes) {
+  return {p, uint64_t(rows), uint64_t(ld) * uint64_t(bytes), uint64_t(cols) * uint64_t(bytes)};
+}
+
 roi_status finish(int launched) {
   if (launched < 0) return ROI_ERR_CUDA;
   g_launches.fetch_add(static_cast<uint64_t>(launched), std::memory_order_relaxed);
@@ -661,6 +699,160 @@ roi_status roi_masked_linear_fwd_noalloc(const roi_bf16* X, const float* logits,
   return roi_masked_linear_fwd(X, logits, W, N, M, tau, st, T, rows, cols, out_Y, ws, need, stream);
 }
 
+int64_t roi_checkpoint_pitch(int64_t cols) { return cols <= 0 || cols > INT64_MAX / 1024 ? 0 : block8_pitch(cols); }
+int64_t roi_checkpoint_scale_pitch(int64_t cols) {
+  return cols <= 0 || cols > INT64_MAX / 1024 ? 0 : block8_scale_pitch(cols);
+}
+
+static roi_status checkpoint_call(const void* x_in, void* x_out, int8_t* codes, uint8_t* scales, int dtype, int64_t rows,
+                                  int64_t cols, int64_t ld, void* stream) {
+  if (!known_type(dtype)) return ROI_ERR_TYPE;
+  if (!good_shape(rows, cols, ld)) return ROI_ERR_SHAPE;
+  if (rows == 0) return ROI_OK;
+  const void* x = x_in != nullptr ? x_in : x_out;
+  if (x == nullptr || codes == nullptr || scales == nullptr) return ROI_ERR_NULL;
+  const int b = type_bytes(dtype);
+  if (!aligned_to(x, b) || !aligned16(codes) || !aligned_to(scales, 4)) return ROI_ERR_ALIGN;
+  const Strided m = matrix(x, rows, cols, ld, b), q = flat(codes, uint64_t(rows) * uint64_t(block8_pitch(cols))),
+                s = flat(scales, uint64_t(rows) * uint64_t(block8_scale_pitch(cols)));
+  if (overlaps(m, q) || overlaps(m, s) || (x_in != nullptr && overlaps(q, s))) return ROI_ERR_ALIAS;
+  CheckpointCall c;
+  c.x_in = x_in;
+  c.x_out = x_out;
+  c.codes = codes;
+  c.scales = scales;
+  c.dtype = static_cast<Elem>(dtype);
+  c.rows = rows;
+  c.cols = cols;
+  c.ld = ld;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(x_in != nullptr ? launch_checkpoint_save(c) : launch_checkpoint_load(c));
+}
+
+roi_status roi_checkpoint_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int8_t* out_codes,
+                               uint8_t* out_scales, void* stream) {
+  return checkpoint_call(x, nullptr, out_codes, out_scales, dtype, rows, cols, ldx, stream);
+}
+
+roi_status roi_checkpoint_load(const int8_t* codes, const uint8_t* scales, int dtype, int64_t rows, int64_t cols,
+                               void* out_x, int64_t ldx, void* stream) {
+  // (the codes and scales of a load are only read)
+  return checkpoint_call(nullptr, out_x, const_cast<int8_t*>(codes), const_cast<uint8_t*>(scales), dtype, rows, cols, ldx,
+                         stream);
+}
+
+roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int kind, const void* gamma,
+                        const void* beta, int param_dtype, float eps, void* out_y, int64_t ldy, float* out_mean,
+                        float* out_rstd, int8_t* out_xcodes, uint8_t* out_xscales, int8_t* out_ycodes,
+                        uint8_t* out_yscales, void* stream) {
+  const bool layer = kind == ROI_LAYER_NORM;
+  if (!known_type(dtype) || (param_dtype != dtype && param_dtype != ROI_FP32) || (!layer && kind != ROI_RMS_NORM) ||
+      !std::isfinite(eps) || eps < 0.0f || (!layer && (beta != nullptr || out_mean != nullptr)))
+    return ROI_ERR_TYPE;
+  if (!good_shape(rows, cols, ldx) || !good_shape(rows, cols, ldy)) return ROI_ERR_SHAPE;
+  if (rows == 0) return ROI_OK;
+  if (x == nullptr || out_y == nullptr || (out_xcodes == nullptr) != (out_xscales == nullptr) ||
+      (out_ycodes == nullptr) != (out_yscales == nullptr))
+    return ROI_ERR_NULL;
+  const int b = type_bytes(dtype), pb = type_bytes(param_dtype);
+  if (!aligned_to(x, b) || !aligned_to(out_y, b) || !aligned16(gamma) || !aligned16(beta) || !aligned_to(out_mean, 4) ||
+      !aligned_to(out_rstd, 4) || !aligned16(out_xcodes) || !aligned16(out_ycodes) || !aligned_to(out_xscales, 4) ||
+      !aligned_to(out_yscales, 4))
+    return ROI_ERR_ALIGN;
+  const uint64_t q = uint64_t(rows) * uint64_t(block8_pitch(cols)), s = uint64_t(rows) * uint64_t(block8_scale_pitch(cols));
+  const Strided in[3] = {matrix(x, rows, cols, ldx, b), flat(gamma, uint64_t(cols) * pb), flat(beta, uint64_t(cols) * pb)};
+  const Strided out[7] = {matrix(out_y, rows, cols, ldy, b), flat(out_mean, uint64_t(rows) * 4), flat(out_rstd, uint64_t(rows) * 4),
+                          flat(out_xcodes, q), flat(out_xscales, s), flat(out_ycodes, q), flat(out_yscales, s)};
+  if (any_alias(in, out)) return ROI_ERR_ALIAS;
+  NormFwdCall c;
+  c.x = x;
+  c.y = out_y;
+  c.gamma = gamma;
+  c.beta = beta;
+  c.mean = out_mean;
+  c.rstd = out_rstd;
+  c.xcodes = out_xcodes;
+  c.xscales = out_xscales;
+  c.ycodes = out_ycodes;
+  c.yscales = out_yscales;
+  c.dtype = static_cast<Elem>(dtype);
+  c.layer = layer;
+  c.params32 = param_dtype == ROI_FP32;
+  c.eps = eps;
+  c.rows = rows;
+  c.cols = cols;
+  c.ldx = ldx;
+  c.ldy = ldy;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(launch_norm_fwd(c));
+}
+
+size_t roi_norm_bwd_workspace_size(int64_t rows, int64_t cols) {
+  return good_shape(rows, cols, cols) && rows > 0 ? norm_bwd_workspace_bytes(rows, cols) : 0;
+}
+
+roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, int64_t lddy, const void* x, int64_t ldx,
+                        const int8_t* codes, const uint8_t* scales, int kind, const void* gamma, int param_dtype,
+                        const float* mean, const float* rstd, void* out_dx, int64_t lddx, float* out_dgamma,
+                        float* out_dbeta, void* workspace, size_t workspace_bytes, void* stream) {
+  const bool layer = kind == ROI_LAYER_NORM;
+  if (!known_type(dtype) || (param_dtype != dtype && param_dtype != ROI_FP32) || (!layer && kind != ROI_RMS_NORM) ||
+      (!layer && (mean != nullptr || out_dbeta != nullptr)))
+    return ROI_ERR_TYPE;
+  if (!good_shape(rows, cols, lddy) || !good_shape(rows, cols, lddx) || (x != nullptr && !good_shape(rows, cols, ldx)))
+    return ROI_ERR_SHAPE;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (!aligned_to(out_dgamma, 4) || !aligned_to(out_dbeta, 4)) return ROI_ERR_ALIGN;
+  if (rows == 0) {  // empty sums
+    if ((out_dgamma != nullptr && cudaMemsetAsync(out_dgamma, 0, size_t(cols) * 4, st) != cudaSuccess) ||
+        (out_dbeta != nullptr && cudaMemsetAsync(out_dbeta, 0, size_t(cols) * 4, st) != cudaSuccess))
+      return ROI_ERR_CUDA;
+    return ROI_OK;
+  }
+  const bool sums = out_dgamma != nullptr || out_dbeta != nullptr;
+  if (dy == nullptr || out_dx == nullptr || rstd == nullptr || (layer && mean == nullptr) ||
+      (codes == nullptr) != (scales == nullptr) || (x == nullptr) == (codes == nullptr) || (sums && workspace == nullptr))
+    return ROI_ERR_NULL;
+  const size_t need = sums ? norm_bwd_workspace_bytes(rows, cols) : 0;
+  if (workspace_bytes < need) return ROI_ERR_SHAPE;
+  const int b = type_bytes(dtype), pb = type_bytes(param_dtype);
+  if (!aligned_to(dy, b) || !aligned_to(x, b) || !aligned_to(out_dx, b) || !aligned16(codes) || !aligned_to(scales, 4) ||
+      !aligned16(gamma) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !aligned16(workspace))
+    return ROI_ERR_ALIGN;
+  const Strided in[7] = {matrix(dy, rows, cols, lddy, b),
+                         matrix(x, rows, cols, ldx, b),
+                         flat(codes, uint64_t(rows) * uint64_t(block8_pitch(cols))),
+                         flat(scales, uint64_t(rows) * uint64_t(block8_scale_pitch(cols))),
+                         flat(gamma, uint64_t(cols) * pb),
+                         flat(mean, uint64_t(rows) * 4),
+                         flat(rstd, uint64_t(rows) * 4)};
+  const Strided out[4] = {matrix(out_dx, rows, cols, lddx, b), flat(out_dgamma, uint64_t(cols) * 4),
+                          flat(out_dbeta, uint64_t(cols) * 4), flat(sums ? workspace : nullptr, need)};
+  if (any_alias(in, out)) return ROI_ERR_ALIAS;
+  NormBwdCall c;
+  c.dy = dy;
+  c.x = x;
+  c.codes = codes;
+  c.scales = scales;
+  c.gamma = gamma;
+  c.mean = mean;
+  c.rstd = rstd;
+  c.dx = out_dx;
+  c.dgamma = out_dgamma;
+  c.dbeta = out_dbeta;
+  c.workspace = workspace;
+  c.dtype = static_cast<Elem>(dtype);
+  c.layer = layer;
+  c.params32 = param_dtype == ROI_FP32;
+  c.rows = rows;
+  c.cols = cols;
+  c.lddy = lddy;
+  c.ldx = ldx;
+  c.lddx = lddx;
+  c.stream = st;
+  return finish(launch_norm_bwd(c));
+}
+
 static roi_status noise_call(const roi_noise_state* st, int64_t rows, int64_t cols, uint32_t* words, float* g,
                              void* stream) {
   if (st == nullptr) return ROI_ERR_NULL;
@@ -713,6 +905,8 @@ const char* roi_status_string(roi_status s) {
     case ROI_ERR_CUDA: return "CUDA error while launching";
     case ROI_ERR_TIMEOUT: return "a kernel gave up waiting on its own copies";
     case ROI_ERR_OPT: return "bad optimizer settings: need lr, weight_decay >= 0 finite, 0 <= beta < 1, eps > 0, t >= 1";
+    case ROI_ERR_TYPE:
+      return "unknown element type or norm kind, eps not finite and >= 0, or a mean or bias with a norm that has none";
   }
   return "unknown status";
 }

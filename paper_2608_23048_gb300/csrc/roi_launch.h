@@ -5,6 +5,7 @@
 #include <cstdint>
 #include <cuda_runtime.h>
 
+#include "roi_block8.cuh"
 #include "roi_common.cuh"
 
 namespace roi {
@@ -122,7 +123,60 @@ struct LinearCall {
   cudaStream_t stream;
 };
 
+// One side of a checkpoint call: x_in -> codes, scales (save) or codes, scales -> x_out (load).
+struct CheckpointCall {
+  const void* x_in;
+  void* x_out;
+  int8_t* codes;
+  uint8_t* scales;
+  Elem dtype;
+  int64_t rows, cols, ld;
+  cudaStream_t stream;
+};
+
+struct NormFwdCall {
+  const void* x;
+  void* y;
+  const void* gamma;  // nullable: 1
+  const void* beta;   // nullable: 0
+  float* mean;        // nullable
+  float* rstd;        // nullable
+  int8_t* xcodes;     // nullable with xscales
+  uint8_t* xscales;
+  int8_t* ycodes;     // nullable with yscales
+  uint8_t* yscales;
+  Elem dtype;
+  bool layer;         // layer norm, else RMS norm
+  bool params32;      // gamma and beta in fp32, else in dtype
+  float eps;
+  int64_t rows, cols, ldx, ldy;
+  cudaStream_t stream;
+};
+
+struct NormBwdCall {
+  const void* dy;
+  const void* x;  // or, where nullptr, the checkpoint
+  const int8_t* codes;
+  const uint8_t* scales;
+  const void* gamma;
+  const float* mean;  // layer norm
+  const float* rstd;
+  void* dx;
+  float* dgamma;      // nullable
+  float* dbeta;       // nullable
+  void* workspace;    // norm_bwd_workspace_bytes where dgamma or dbeta is wanted
+  Elem dtype;
+  bool layer, params32;
+  int64_t rows, cols, lddy, ldx, lddx;
+  cudaStream_t stream;
+};
+
 // Each returns the number of kernels launched (>= 0) or -1 after a CUDA error.
+int launch_checkpoint_save(const CheckpointCall& c);
+int launch_checkpoint_load(const CheckpointCall& c);
+int launch_norm_fwd(const NormFwdCall& c);
+int launch_norm_bwd(const NormBwdCall& c);
+size_t norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);
 // Many independent tensors on one stream: one launch per tensor, or per run of
