@@ -399,6 +399,28 @@ roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, i
                         void* out_dx, int64_t lddx, float* out_dgamma, float* out_dbeta,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* Weight gradient of a masked linear layer Y = X Wm^T from the checkpoint of X:
+ *   dWm[r, c] = sum_t float(dY[t, r]) * x[t, c]  (+ acc[r, c])
+ * x the values that the checkpoint stands for; products exact, sums in fp32, on the
+ * tensor cores.  The result is what roi_mask_bwd takes as dWm.
+ *  dY        [T, rows] bf16, row stride lddy; 16-byte aligned
+ *  codes, scales  the checkpoint of X [T, cols]
+ *  out_dWm   [rows, cols] bf16, nullable: the sum, rounded
+ *  acc       [rows, cols] float32, nullable, updated in place: the sum over the
+ *            micro-batches of a step (one of the two outputs is required)
+ *  workspace nullable, 16-byte aligned.  With roi_masked_linear_wgrad_workspace_size
+ *            bytes the tokens of the last tiles are divided among the SMs; with less
+ *            they are not.  Where lddy is no multiple of 8 (and T > 1) dY is laid out
+ *            again in it: ROI_ERR_NULL or ROI_ERR_SHAPE where the T rows, each rounded
+ *            up to a multiple of 8 elements, do not fit.
+ * The order of the sums depends on the sizes, the GPU and the workspace's size, not
+ * on timing.  T == 0: an empty sum (out_dWm = acc, or 0).  roi_device_status reports
+ * a kernel that gave up waiting on its copies.                                       */
+size_t roi_masked_linear_wgrad_workspace_size(int64_t T, int64_t rows, int64_t cols, int64_t lddy);
+roi_status roi_masked_linear_wgrad(const roi_bf16* dY, int64_t lddy, const int8_t* codes, const uint8_t* scales,
+                                   int64_t T, int64_t rows, int64_t cols, roi_bf16* out_dWm, float* acc,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
 /* The noise of a call, materialised (for inspecting or reproducing a sample; the
  * mask calls never store it).  st->lambda is ignored; st->row_offset applies.
  *  roi_noise_words: out_words[rows*cols] uint32, the Philox word x_e of element e.

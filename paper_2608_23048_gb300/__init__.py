@@ -20,6 +20,7 @@ __all__ = [
     "roi_anneal", "roi_set_ring_wait_limit_ns",
     "roi_checkpoint_pitch", "roi_checkpoint_scale_pitch", "roi_checkpoint_save", "roi_checkpoint_load",
     "new_checkpoint", "roi_norm_fwd", "roi_norm_bwd", "roi_norm_bwd_workspace_size",
+    "roi_masked_linear_wgrad", "roi_masked_linear_wgrad_workspace_size",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -125,6 +126,9 @@ def lib() -> ctypes.CDLL:
                                ctypes.c_size_t, _P]
     L.roi_norm_bwd_workspace_size.argtypes = [i64, i64]
     L.roi_norm_bwd_workspace_size.restype = ctypes.c_size_t
+    L.roi_masked_linear_wgrad.argtypes = [_P, i64, _P, _P, i64, i64, i64, _P, _P, _P, ctypes.c_size_t, _P]
+    L.roi_masked_linear_wgrad_workspace_size.argtypes = [i64, i64, i64, i64]
+    L.roi_masked_linear_wgrad_workspace_size.restype = ctypes.c_size_t
     L.roi_device_status.argtypes = [_P]
     L.roi_set_ring_wait_limit_ns.argtypes = [u64]
     L.roi_noise_words.argtypes = [ctypes.POINTER(NoiseState), i64, i64, _P, _P]
@@ -139,7 +143,7 @@ def lib() -> ctypes.CDLL:
                  "roi_masked_linear_fwd_noalloc", "roi_mask_fwd_batch", "roi_mask_bwd_batch",
                  "roi_mask_bwd_adamw_batch", "roi_mask_fwd_st_batch", "roi_mask_bwd_st_batch",
                  "roi_set_ring_wait_limit_ns", "roi_checkpoint_save", "roi_checkpoint_load", "roi_norm_fwd",
-                 "roi_norm_bwd"):
+                 "roi_norm_bwd", "roi_masked_linear_wgrad"):
         getattr(L, name).restype = i32
     _LIB = L
     return L
@@ -617,6 +621,33 @@ def roi_norm_bwd(dy, x, kind, gamma, mean, rstd, out_dx, out_dgamma=None, out_db
                            _norm_kind(kind), _ptr(gamma), p, _ptr(mean), _ptr(rstd), _ptr(out_dx), lddx,
                            _ptr(out_dgamma), _ptr(out_dbeta), ws, ws_bytes, _stream(stream))
     _raise(s, "roi_norm_bwd")
+
+
+def roi_masked_linear_wgrad_workspace_size(T, rows, cols, lddy=None) -> int:
+    """Bytes of workspace roi_masked_linear_wgrad can use on the current device (lddy: row stride
+    of dY in elements, `rows` unless given)."""
+    return int(lib().roi_masked_linear_wgrad_workspace_size(int(T), int(rows), int(cols),
+                                                            int(rows if lddy is None else lddy)))
+
+
+def roi_masked_linear_wgrad(dY, x_checkpoint, out_dWm=None, acc=None, workspace=None, stream=None):
+    """out_dWm[rows, cols] = bf16(dY[T, rows]^T x[T, cols] + acc), x the values of the (codes, scales)
+    pair x_checkpoint; acc (float32), where given, is updated in place."""
+    import torch
+    T, rows = dY.shape
+    shape = next((t.shape for t in (out_dWm, acc) if t is not None), None)
+    if shape is None or len(shape) != 2:
+        raise ValueError("out_dWm or acc: a matrix is required")
+    cols = shape[1]
+    lddy = _matrix(dY, "dY", torch.bfloat16)
+    codes, scales = x_checkpoint
+    _checkpoint(codes, scales, "x_checkpoint", T, cols)
+    _check_tensor(out_dWm, "out_dWm", torch.bfloat16, (rows, cols))
+    _check_tensor(acc, "acc", torch.float32, (rows, cols))
+    ws, ws_bytes = _workspace(workspace)
+    s = lib().roi_masked_linear_wgrad(_ptr(dY), lddy, _ptr(codes), _ptr(scales), T, rows, cols, _ptr(out_dWm), _ptr(acc),
+                                      ws, ws_bytes, _stream(stream))
+    _raise(s, "roi_masked_linear_wgrad")
 
 
 def roi_noise_words(state: NoiseState, rows, cols, out_words, stream=None):

@@ -853,6 +853,55 @@ roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, i
   return finish(launch_norm_bwd(c));
 }
 
+// Tensor-map coordinates and tile numbers are 32-bit.
+static bool wgrad_shape(int64_t T, int64_t rows, int64_t cols, int64_t lddy) {
+  constexpr int64_t kMost = int64_t(1) << 30;
+  return good_shape(T, rows, lddy) && good_shape(rows, cols, cols) && rows > 0 && T <= kMost && rows <= kMost && cols <= kMost &&
+         (rows / 128 + 1) * (cols / 128 + 1) <= kMost;
+}
+
+size_t roi_masked_linear_wgrad_workspace_size(int64_t T, int64_t rows, int64_t cols, int64_t lddy) {
+  return T > 0 && wgrad_shape(T, rows, cols, lddy) ? wgrad_workspace_bytes(T, rows, cols, lddy) : 0;
+}
+
+roi_status roi_masked_linear_wgrad(const roi_bf16* dY, int64_t lddy, const int8_t* codes, const uint8_t* scales, int64_t T,
+                                   int64_t rows, int64_t cols, roi_bf16* out_dWm, float* acc, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+  if (rows == 0 && T >= 0 && cols > 0) return ROI_OK;
+  if (!wgrad_shape(T, rows, cols, lddy)) return ROI_ERR_SHAPE;
+  const size_t copy = wgrad_copy_bytes(T, rows, lddy);
+  if ((out_dWm == nullptr && acc == nullptr) || (T > 0 && (dY == nullptr || codes == nullptr || scales == nullptr)) ||
+      (copy > 0 && workspace == nullptr))
+    return ROI_ERR_NULL;
+  if (copy > 0 && workspace_bytes < copy) return ROI_ERR_SHAPE;
+  if (!aligned16(dY) || !aligned16(codes) || !aligned_to(scales, 4) || !aligned16(out_dWm) || !aligned16(acc) ||
+      !aligned16(workspace))
+    return ROI_ERR_ALIGN;
+  const uint64_t E = uint64_t(rows) * uint64_t(cols);
+  const size_t need = T > 0 ? wgrad_workspace_bytes(T, rows, cols, lddy) : 0;
+  const uint64_t used = workspace == nullptr ? 0 : need < workspace_bytes ? need : workspace_bytes;
+  const Strided in[3] = {matrix(dY, T, rows, lddy, 2), flat(codes, uint64_t(T) * uint64_t(block8_pitch(cols))),
+                         flat(scales, uint64_t(T) * uint64_t(block8_scale_pitch(cols)))};
+  const Strided out[3] = {flat(out_dWm, E * 2), flat(acc, E * 4), flat(workspace, used)};
+  if (any_alias(in, out)) return ROI_ERR_ALIAS;
+  WgradCall c;
+  c.dY = dY;
+  c.codes = codes;
+  c.scales = scales;
+  c.dWm = out_dWm;
+  c.acc = acc;
+  c.workspace = workspace;
+  c.workspace_bytes = workspace == nullptr ? 0 : workspace_bytes;
+  c.T = T;
+  c.rows = rows;
+  c.cols = cols;
+  c.lddy = lddy;
+  c.status = status_word();
+  if (c.status == nullptr) return ROI_ERR_CUDA;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(launch_wgrad(c));
+}
+
 static roi_status noise_call(const roi_noise_state* st, int64_t rows, int64_t cols, uint32_t* words, float* g,
                              void* stream) {
   if (st == nullptr) return ROI_ERR_NULL;

@@ -171,12 +171,30 @@ struct NormBwdCall {
   cudaStream_t stream;
 };
 
+struct WgradCall {
+  const uint16_t* dY;   // [T, rows] bf16, stride lddy
+  const int8_t* codes;  // the checkpoint of X [T, cols]
+  const uint8_t* scales;
+  uint16_t* dWm;        // nullable
+  float* acc;           // nullable
+  void* workspace;      // nullable
+  size_t workspace_bytes;
+  int64_t T, rows, cols, lddy;
+  unsigned int* status;
+  cudaStream_t stream;
+};
+
 // Each returns the number of kernels launched (>= 0) or -1 after a CUDA error.
 int launch_checkpoint_save(const CheckpointCall& c);
 int launch_checkpoint_load(const CheckpointCall& c);
 int launch_norm_fwd(const NormFwdCall& c);
 int launch_norm_bwd(const NormBwdCall& c);
 size_t norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
+// Weight gradient of a masked linear layer on the tensor cores (roi_wgrad.cu).  All that it
+// can use, and what it cannot do without (dY laid out again).
+size_t wgrad_workspace_bytes(int64_t T, int64_t rows, int64_t cols, int64_t lddy);
+size_t wgrad_copy_bytes(int64_t T, int64_t rows, int64_t lddy);
+int launch_wgrad(const WgradCall& c);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);
 // Many independent tensors on one stream: one launch per tensor, or per run of

@@ -21,11 +21,9 @@
 // the first (programmatic dependent launch: it is scheduled while the GEMM drains
 // and reads once the GEMM has completed), adds them in split order across the
 // whole GPU, so Y does not depend on timing.
-#include <cuda.h>
-#include <cudaTypedefs.h>
-
 #include "roi_launch.h"
 #include "roi_tc.cuh"
+#include "roi_tmap.h"
 
 namespace roi {
 namespace {
@@ -423,34 +421,12 @@ __global__ void __launch_bounds__(256) roi_linear_reduce_kernel(const float* par
   }
 }
 
-// cuTensorMapEncodeTiled through the runtime's driver entry point (no link
-// dependency on the driver library).
-PFN_cuTensorMapEncodeTiled_v12000 encode_tiled() {
-  static PFN_cuTensorMapEncodeTiled_v12000 fn = nullptr;
-  if (fn == nullptr) {
-    void* p = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) ==
-            cudaSuccess &&
-        q == cudaDriverEntryPointSuccess)
-      fn = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(p);
-  }
-  return fn;
-}
-
 // A 2-D row-major tensor of dim1 rows x dim0 elements, box of box1 rows x box0
 // elements, no swizzle, out-of-range elements read as zero.
 bool make_map(CUtensorMap* m, CUtensorMapDataType dt, uint32_t esize, const void* base, uint64_t dim0,
               uint64_t dim1, uint32_t box0, uint32_t box1) {
-  auto fn = encode_tiled();
-  if (fn == nullptr) return false;
-  const cuuint64_t dims[2] = {dim0, dim1};
-  const cuuint64_t strides[1] = {dim0 * esize};
-  const cuuint32_t box[2] = {box0, box1};
-  const cuuint32_t estr[2] = {1, 1};
-  return fn(m, dt, 2, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
-         CUDA_SUCCESS;
+  return make_tensor_map(m, dt, base, dim0, dim1, dim0 * esize, box0, box1, CU_TENSOR_MAP_SWIZZLE_NONE,
+                         CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
 }
 
 template <int N, int M>

@@ -95,4 +95,124 @@ __device__ __forceinline__ void tma_load_2d(void* dst_smem, const void* tmap, in
       : "memory");
 }
 
+// ---------------------------------------------------------------------------
+// MN-major operands with 128-byte swizzle, and pairs of CTAs (cta_group::2)
+// ---------------------------------------------------------------------------
+// A tile of K rows of 64 bf16 (128 bytes along M or N), as a TMA box of that shape with
+// 128-byte swizzle leaves it: atoms of 8 rows (1024 bytes) follow one another along K; the
+// next 64 elements along M or N are `next64` bytes on.  The 16 bytes c of row k lie at
+// chunk c ^ (k & 7).  1024-byte aligned.
+__device__ __forceinline__ uint64_t tc_smem_desc_mn128(uint32_t saddr, uint32_t next64) {
+  uint64_t d = uint64_t((saddr >> 4) & 0x3FFFu);
+  d |= uint64_t((next64 >> 4) & 0x3FFFu) << 16;
+  d |= uint64_t(1024 >> 4) << 32;
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(2) << 61;  // 128-byte swizzle
+  return d;
+}
+// As tc_idesc_bf16_f32, both operands MN-major (bits 15 and 16).
+__host__ __device__ constexpr uint32_t tc_idesc_bf16_f32_mn(int m, int n) {
+  return tc_idesc_bf16_f32(m, n) | (1u << 15) | (1u << 16);
+}
+
+template <int CG>
+__device__ __forceinline__ void tc_alloc_group(uint32_t* dst_smem, uint32_t ncols) {
+  if constexpr (CG == 1) {
+    tc_alloc(dst_smem, ncols);
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst_smem)),
+                 "r"(ncols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+}
+template <int CG>
+__device__ __forceinline__ void tc_dealloc_group(uint32_t taddr, uint32_t ncols) {
+  if constexpr (CG == 1) {
+    tc_dealloc(taddr, ncols);
+  } else {
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+  }
+}
+// One M x N x 16 step; with a pair, issued by one thread of the even CTA for both (M and N
+// over the pair: each CTA holds half of A's rows, half of B's, and half of D's rows).
+template <int CG>
+__device__ __forceinline__ void tc_mma_bf16_group(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                  bool accumulate) {
+  if constexpr (CG == 1) {
+    tc_mma_bf16(d_tmem, a_desc, b_desc, idesc, accumulate);
+  } else {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(uint32_t(accumulate))
+        : "memory");
+  }
+}
+// The mbarrier (of both CTAs of a pair) receives one arrival when every MMA this thread issued
+// so far is done.
+template <int CG>
+__device__ __forceinline__ void tc_commit_group(uint64_t* bar) {
+  if constexpr (CG == 1) {
+    tc_commit(bar);
+  } else {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+            smem_addr(bar)),
+        "h"(uint16_t(3))
+        : "memory");
+  }
+}
+// 32 consecutive fp32 columns of this warp's 32 TMEM lanes.
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+      "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]),
+        "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]),
+        "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]),
+        "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+// Every thread of both CTAs of a pair (arrive has release, wait acquire semantics).
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+}
+// One arrival on the mbarrier at `bar`'s place in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ void mbar_arrive_cluster(uint64_t* bar, uint32_t rank) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [ra];\n\t}" ::"r"(smem_addr(bar)),
+      "r"(rank)
+      : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint64_t* bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(smem_addr(bar)), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// mbar_wait_ring for a barrier on which other CTAs of the cluster arrive.
+__device__ __forceinline__ bool mbar_wait_ring_cluster(uint64_t* bar, uint32_t parity, uint64_t lim) {
+  if (lim == 0) return false;
+  if (mbar_try_wait_cluster(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (true) {
+    if (mbar_try_wait_cluster(bar, parity)) return true;
+    if (global_timer_ns() - t0 > lim) return false;
+  }
+}
+
 }  // namespace roi

@@ -1,0 +1,487 @@
+// Weight gradient of a masked linear layer from the 8-bit checkpoint of its input:
+//   dWm[o, i] = sum_t dY[t, o] x^[t, i]  (+ acc[o, i])
+// on the fifth-generation tensor cores, the sums in fp32.  x^ is formed from codes and scales
+// on the way into shared memory; its values have 7 bits and a sign, so bf16 holds them exactly
+// and the product is that of dY with the checkpoint's own values.
+//
+// One or two CTAs (CG; a pair shares its MMAs, cta_group::2) own a tile of 128 CG outputs x
+// 128 CG inputs; each CTA holds 128 outputs of dY, 128 inputs of x^ and, in TMEM, 128 rows of
+// the sums, 128 CG columns wide.  Both operands are MN-major (a token's row is contiguous
+// along outputs or inputs), in tiles of 64 tokens with 128-byte swizzle.
+//
+// Roles of the 14 warps of a CTA, each a loop over the same list of tiles and chunks of tokens:
+//   warp 0        stages dY and the codes of a chunk by TMA (rows past the last token, and
+//                 columns past the last, as zeros), `full`
+//   warps 2 - 9   turn the codes into bf16 in the layout of the MMA, `ready`
+//   warp 1        issues four MMAs of 16 tokens a chunk (in a pair, the even CTA's for both),
+//                 commits them to `empty` and after the last chunk to `sum`
+//   warps 10 - 13 read the sums from TMEM and write them out, `free`, while the next tile's
+//                 MMAs go to the other half of TMEM
+// Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
+//
+// Tiles go to the groups (CTAs or pairs) in rounds.  In the last, partial round the tokens of
+// its tiles are cut into even ranges, one a group, where that ends sooner: ranges that do not
+// cover a whole tile leave fp32 partial sums in the workspace, which a second launch adds in
+// the order of the tokens, so that results do not depend on timing.
+#include <atomic>
+
+#include "roi_launch.h"
+#include "roi_tc.cuh"
+#include "roi_tmap.h"
+
+namespace roi {
+namespace {
+
+constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
+constexpr int kChunk = 64;                 // tokens a stage
+constexpr int kStages = 5;
+constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
+constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
+constexpr uint32_t kCodes = kChunk * kEdge;
+constexpr uint32_t kStage = 2 * kOperand + kCodes;
+constexpr uint32_t kLanded = kOperand + kCodes;  // bytes of a stage that TMA brings
+constexpr int kConvertWarps = 8, kConvert = 32 * kConvertWarps;
+constexpr int kThreads = 64 + kConvert + 128;
+constexpr uint32_t kTmemCols = 512;
+constexpr uint32_t kSmem = kStages * kStage + 256;
+// The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
+// partial sums is written and read again.
+constexpr int kMinRange = 8, kSplitCost = 8;
+
+struct WgradArgs {
+  const uint8_t* scales;
+  uint16_t* dWm;  // nullable
+  float* acc;     // nullable
+  float* part;    // [2 * ranges][128 CG][128 CG] (split)
+  int64_t T, rows, cols, spitch;
+  int tiles_m, tiles_n;
+  bool n_first;   // consecutive tiles run along the inputs
+  int chunks;     // of a whole tile
+  int groups;     // CTAs or pairs
+  int rounds;     // whole rounds of tiles
+  int rest;       // tiles of the last round
+  int ranges;     // ranges of its tokens, 0 where they are not cut
+  unsigned int* status;
+  bool wait;
+};
+
+struct Work {
+  int tile, c0, c1;  // tile and its chunks
+  int slot;          // place of its partial sums, -1 where it is whole
+};
+
+__host__ __device__ inline int64_t range_start(const WgradArgs& a, int64_t r) {
+  return r * (int64_t(a.rest) * a.chunks) / a.ranges;
+}
+
+// The i-th piece of work of group g; false after the last.
+__device__ __forceinline__ bool work_of(const WgradArgs& a, int g, int i, Work& w) {
+  w.slot = -1;
+  w.c0 = 0;
+  w.c1 = a.chunks;
+  if (i < a.rounds) {
+    w.tile = i * a.groups + g;
+    return true;
+  }
+  const int j = i - a.rounds;
+  if (a.ranges == 0) {
+    w.tile = a.rounds * a.groups + g;
+    return j == 0 && g < a.rest;
+  }
+  if (g >= a.ranges || j > 1) return false;
+  // a range is no longer than a tile: it touches two tiles at most
+  const int64_t begin = range_start(a, g), end = range_start(a, g + 1);
+  const int first = int(begin / a.chunks);
+  const int64_t t0 = int64_t(first + j) * a.chunks;  // the tile's first chunk among all
+  const int64_t from = begin > t0 ? begin : t0, to = end < t0 + a.chunks ? end : t0 + a.chunks;
+  if (from >= to) return false;
+  w.tile = a.rounds * a.groups + first + j;
+  w.c0 = int(from - t0);
+  w.c1 = int(to - t0);
+  if (w.c0 != 0 || w.c1 != a.chunks) w.slot = 2 * g + j;
+  return true;
+}
+
+__device__ __forceinline__ void tile_origin(const WgradArgs& a, int tile, int edge, int64_t& m0, int64_t& n0) {
+  const int m = a.n_first ? tile / a.tiles_n : tile % a.tiles_m;
+  const int n = a.n_first ? tile % a.tiles_n : tile / a.tiles_m;
+  m0 = int64_t(m) * edge;
+  n0 = int64_t(n) * edge;
+}
+
+// Four codes to four bf16 (two words), times the block's power of two.  A code byte b is
+// (128 + (b & 127)) - (128 + (b & 128)): both terms are bf16 numbers whose mantissa holds the
+// byte's bits, and the difference is exact.
+__device__ __forceinline__ uint32_t codes2_bf16(uint32_t spread, __nv_bfloat162 step) {
+  const uint32_t m = (spread & 0x007f007fu) | 0x43004300u, n = (spread & 0x00800080u) | 0x43004300u;
+  const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&n)), step);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint4 codes8_bf16(uint32_t a, uint32_t b, __nv_bfloat162 step) {
+  return make_uint4(codes2_bf16(__byte_perm(a, 0, 0x4140), step), codes2_bf16(__byte_perm(a, 0, 0x4342), step),
+                    codes2_bf16(__byte_perm(b, 0, 0x4140), step), codes2_bf16(__byte_perm(b, 0, 0x4342), step));
+}
+__device__ __forceinline__ __nv_bfloat162 step_bf16x2(uint32_t s) {
+  const uint32_t h = __float_as_uint(block8_step(s)) >> 16;
+  const uint32_t w = h | (h << 16);
+  return *reinterpret_cast<const __nv_bfloat162*>(&w);
+}
+
+// 32 columns of a row of the sums, from column n on: added to acc, and written out.
+__device__ __forceinline__ void store_sums(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
+  const int64_t at = m * a.cols + n;
+  if (a.cols % 8 == 0) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (n + 8 * q >= a.cols) break;
+      float* s = v + 8 * q;
+      if (a.acc != nullptr) {
+        float4* p = reinterpret_cast<float4*>(a.acc + at + 8 * q);
+        const float4 x = p[0], y = p[1];
+        s[0] += x.x, s[1] += x.y, s[2] += x.z, s[3] += x.w;
+        s[4] += y.x, s[5] += y.y, s[6] += y.z, s[7] += y.w;
+        p[0] = make_float4(s[0], s[1], s[2], s[3]);
+        p[1] = make_float4(s[4], s[5], s[6], s[7]);
+      }
+      if (a.dWm != nullptr) {
+        *reinterpret_cast<uint4*>(a.dWm + at + 8 * q) =
+            make_uint4(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]), pack_bf16x2(s[4], s[5]), pack_bf16x2(s[6], s[7]));
+      }
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+      if (n + k < a.cols) {
+        if (a.acc != nullptr) a.acc[at + k] = v[k] += a.acc[at + k];
+        if (a.dWm != nullptr) a.dWm[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(v[k]));
+      }
+    }
+  }
+}
+
+template <int CG>
+__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
+    roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
+  uint64_t *full = bars, *ready = full + kStages, *empty = ready + kStages, *sum = empty + kStages, *free = sum + 2;
+  uint32_t* misc = reinterpret_cast<uint32_t*>(free + 2);  // [0] TMEM base, [1] ok
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = CG == 1 ? 0u : cluster_rank();
+  const int g = blockIdx.x / CG;
+
+  if (tid == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(ready + s, kConvertWarps * CG);
+      mbar_init(empty + s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(sum + b, 1);
+      mbar_init(free + b, 4 * CG);
+    }
+    misc[1] = 1u;
+    fence_mbar_init();
+  }
+  if (warp == 0) tc_alloc_group<CG>(misc, kTmemCols);
+  tc_fence_before();
+  __syncthreads();
+  if constexpr (CG > 1) cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = misc[0];
+  pdl_begin(a.wait);
+
+  const uint64_t lim = ring_wait_limit(a.status);
+  bool ok = true;
+  int issued = 0, committed = 0;  // chunks whose copies, and whose MMAs, this thread has sent off
+  Work w;
+  int64_t m0, n0;
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+        tile_origin(a, w.tile, kEdge * CG, m0, n0);
+        const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
+        for (int c = w.c0; c < w.c1; ++c, ++issued) {
+          const int s = issued % kStages;
+          ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
+          if (!ok) break;
+          uint8_t* st = smem + s * kStage;
+          mbar_arrive_expect_tx(full + s, kLanded);
+          tma_load_2d(st, &tm_dy, m, c * kChunk, full + s);
+          tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, full + s);
+          tma_load_2d(st + 2 * kOperand, &tm_codes, n, c * kChunk, full + s);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      const uint32_t idesc = tc_idesc_bf16_f32_mn(kEdge * CG, kEdge * CG);
+      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+        const int b = i & 1;
+        ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
+        const uint32_t d = tmem + uint32_t(b) * (kEdge * CG);
+        for (int c = w.c0; ok && c < w.c1; ++c, ++committed) {
+          const int s = committed % kStages;
+          ok = mbar_wait_ring_cluster(ready + s, uint32_t(committed / kStages) & 1u, lim);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t st = smem_addr(smem + s * kStage);
+#pragma unroll
+          for (int k = 0; k < kChunk / 16; ++k)
+            tc_mma_bf16_group<CG>(d, tc_smem_desc_mn128(st + k * 2048, kHalf), tc_smem_desc_mn128(st + kOperand + k * 2048, kHalf),
+                                  idesc, c > w.c0 || k > 0);
+          tc_commit_group<CG>(empty + s);
+        }
+        if (ok) tc_commit_group<CG>(sum + b);
+      }
+    }
+  } else if (warp < 2 + kConvertWarps) {
+    // this thread's codes of a chunk: 16 inputs from 16 j on, of tokens k and k + 32
+    const int t = tid - 64, k = t >> 3, j = t & 7;
+    const uint32_t half = uint32_t(j >> 2) * kHalf, swizzle = uint32_t(k & 7);
+    const uint32_t first = (uint32_t(2 * (j & 3)) ^ swizzle) * 16, second = (uint32_t(2 * (j & 3) + 1) ^ swizzle) * 16;
+    int n = 0;  // chunks done
+    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      const int64_t block = (n0 + int64_t(rank) * kEdge) / 32 + (j >> 1);
+      const uint8_t* sp = a.scales + block;
+      const bool in = block < a.spitch;
+      // the scales of a chunk are loaded while the one before is waited for
+      uint32_t scale[2], next[2];
+      auto load = [&](int c) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t row = int64_t(c) * kChunk + k + 32 * h;
+          next[h] = in && c < w.c1 && row < a.T ? uint32_t(__ldg(sp + row * a.spitch)) : 0u;
+        }
+      };
+      load(w.c0);
+      for (int c = w.c0; c < w.c1; ++c, ++n) {
+        const int s = n % kStages;
+        scale[0] = next[0], scale[1] = next[1];
+        load(c + 1);
+        ok = mbar_wait_ring(full + s, uint32_t(n / kStages) & 1u, lim);
+        if (!ok) break;
+        uint8_t* st = smem + s * kStage;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint4 q = *reinterpret_cast<const uint4*>(st + 2 * kOperand + (k + 32 * h) * kEdge + 16 * j);
+          const __nv_bfloat162 step = step_bf16x2(scale[h]);
+          const uint4 lo = codes8_bf16(q.x, q.y, step), hi = codes8_bf16(q.z, q.w, step);
+          uint8_t* row = st + kOperand + half + (k + 32 * h) * 128;
+          // four of the eight lanes of a row start with their upper half: no two on one bank
+          const bool up = j >= 4;
+          *reinterpret_cast<uint4*>(row + (up ? second : first)) = up ? hi : lo;
+          *reinterpret_cast<uint4*>(row + (up ? first : second)) = up ? lo : hi;
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(ready + s, 0);
+      }
+    }
+  } else {
+    const int quarter = warp & 3;
+    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+      const int b = i & 1;
+      ok = mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim);
+      if (!ok) break;
+      tc_fence_after();
+      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      const int r = int(rank) * kEdge + quarter * 32 + lane;  // row of the tile
+      const int64_t m = m0 + r;
+      float* part = a.part + (int64_t(w.slot) * (kEdge * CG) + r) * (kEdge * CG);
+      for (int q = 0; q < kEdge * CG / 32; ++q) {
+        uint32_t u[32];
+        tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * (kEdge * CG) + 32 * q), u);
+        float v[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
+        if (w.slot >= 0) {
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + 32 * q + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        } else if (m < a.rows && n0 + 32 * q < a.cols) {
+          store_sums(a, m, n0 + 32 * q, v);
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(free + b, 0);
+    }
+  }
+  if (!ok) misc[1] = 0u;
+  __syncthreads();
+  if (misc[1] == 0u) {
+    // a wait gave up: the copies this CTA sent off land, and its MMAs end, before it leaves
+    if (warp == 0 && lane == 0) {
+      for (int c = issued > kStages ? issued - kStages : 0; c < issued; ++c)
+        mbar_wait_bounded(full + c % kStages, uint32_t(c / kStages) & 1u);
+    }
+    if (warp == 1 && committed > 0)
+      mbar_wait_bounded(empty + (committed - 1) % kStages, uint32_t((committed - 1) / kStages) & 1u);
+    if (tid == 0) atomicOr(a.status, kStatusTimeout);
+    __syncthreads();
+  }
+  tc_fence_after();
+  if constexpr (CG > 1) cluster_sync();
+  if (warp == 0) tc_dealloc_group<CG>(tmem, kTmemCols);
+}
+
+// The tiles of the last round whose tokens were cut: their partial sums in the order of the
+// ranges, four columns a thread.
+template <int CG>
+__global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
+  constexpr int kSide = kEdge * CG, kQuads = kSide / 4;
+  pdl_begin(true);  // the partial sums of the launch before
+  const int64_t per_tile = int64_t(kSide) * kQuads;
+  const int64_t total = a.rest * per_tile;
+  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += int64_t(gridDim.x) * blockDim.x) {
+    const int tile = int(i / per_tile);
+    const int e = int(i - tile * per_tile), r = e / kQuads, c = e % kQuads * 4;
+    int64_t m0, n0;
+    tile_origin(a, a.rounds * a.groups + tile, kSide, m0, n0);
+    const int64_t m = m0 + r, n = n0 + c;
+    if (m >= a.rows || n >= a.cols) continue;
+    // the ranges that hold the tile's first and last chunk
+    const int64_t t0 = int64_t(tile) * a.chunks, t1 = t0 + a.chunks - 1;
+    int p0 = int(t0 * a.ranges / (int64_t(a.rest) * a.chunks)), p1 = int(t1 * a.ranges / (int64_t(a.rest) * a.chunks));
+    while (range_start(a, p0 + 1) <= t0) ++p0;
+    while (range_start(a, p1 + 1) <= t1) ++p1;
+    if (p0 == p1) continue;  // whole, and written already
+    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int p = p0; p <= p1; ++p) {
+      const int j = tile - int(range_start(a, p) / a.chunks);
+      const float4 v = __ldcs(reinterpret_cast<const float4*>(a.part + (int64_t(2 * p + j) * kSide + r) * kSide + c));
+      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+    }
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    const int64_t at = m * a.cols + n;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (n + k >= a.cols) break;
+      float x = v[k];
+      if (a.acc != nullptr) a.acc[at + k] = x += a.acc[at + k];
+      if (a.dWm != nullptr) a.dWm[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+    }
+  }
+}
+
+// dY with rows that are not multiples of 16 bytes apart, laid out again with rows that are.
+__global__ void __launch_bounds__(256) roi_wgrad_align_kernel(const uint16_t* src, int64_t ld, uint16_t* dst, int64_t pitch, int64_t T,
+                                                              int64_t cols, bool wait) {
+  pdl_begin(wait);
+  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
+#pragma unroll 8
+    for (int64_t c = threadIdx.x; c < cols; c += 256) dst[t * pitch + c] = src[t * ld + c];
+  }
+}
+
+// No tokens: an empty sum.
+__global__ void __launch_bounds__(256) roi_wgrad_empty_kernel(uint16_t* dWm, const float* acc, int64_t n, bool wait) {
+  pdl_begin(wait);
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < n; i += int64_t(gridDim.x) * 256)
+    dWm[i] = __bfloat16_as_ushort(__float2bfloat16_rn(acc == nullptr ? 0.0f : acc[i]));
+}
+
+constexpr int kGroup = 1;
+
+// The division of the work among the groups, and the bytes of partial sums it needs.
+size_t plan(int64_t T, int64_t rows, int64_t cols, WgradArgs& a) {
+  constexpr int64_t side = kEdge * kGroup;
+  a.T = T;
+  a.rows = rows;
+  a.cols = cols;
+  a.tiles_m = int((rows + side - 1) / side);
+  a.tiles_n = int((cols + side - 1) / side);
+  a.n_first = 2 * rows >= cols;  // the larger operand (dY in 2 bytes, codes in one) is read through once
+  a.chunks = int((T + kChunk - 1) / kChunk);
+  a.groups = sm_count() / kGroup;
+  if (a.groups < 1) a.groups = 1;
+  const int64_t tiles = int64_t(a.tiles_m) * a.tiles_n;
+  a.rounds = int(tiles / a.groups);
+  a.rest = int(tiles - int64_t(a.rounds) * a.groups);
+  a.ranges = 0;
+  const int64_t units = int64_t(a.rest) * a.chunks;
+  const int64_t most = units / kMinRange < a.groups ? units / kMinRange : a.groups;
+  if (most > a.rest && (units + most - 1) / most + kSplitCost < a.chunks) a.ranges = int(most);
+  return a.ranges == 0 ? 0 : size_t(a.ranges) * 2 * side * side * 4;
+}
+
+int64_t aligned_pitch(int64_t rows) { return (rows + 7) / 8 * 8; }
+bool needs_copy(int64_t T, int64_t ld) { return T > 1 && ld % 8 != 0; }
+
+}  // namespace
+
+size_t wgrad_workspace_bytes(int64_t T, int64_t rows, int64_t cols, int64_t lddy) {
+  WgradArgs a;
+  return plan(T, rows, cols, a) + (needs_copy(T, lddy) ? size_t(T) * size_t(aligned_pitch(rows)) * 2 : 0);
+}
+size_t wgrad_copy_bytes(int64_t T, int64_t rows, int64_t lddy) {
+  return needs_copy(T, lddy) ? size_t(T) * size_t(aligned_pitch(rows)) * 2 : 0;
+}
+
+int launch_wgrad(const WgradCall& c) {
+  bool wait = lone_pdl(c.stream);
+  if (c.T == 0) {
+    if (c.dWm == nullptr) return 0;
+    const int64_t n = c.rows * c.cols, blocks = (n + 255) / 256, cap = int64_t(sm_count()) * 8;
+    return launch_maybe_pdl(roi_wgrad_empty_kernel, int(blocks < cap ? blocks : cap), 256, 0, c.stream, wait, c.dWm,
+                            static_cast<const float*>(c.acc), n, wait);
+  }
+  int launched = 0;
+  const uint16_t* dY = c.dY;
+  int64_t ld = c.T > 1 ? c.lddy : aligned_pitch(c.rows);
+  uint8_t* ws = static_cast<uint8_t*>(c.workspace);
+  size_t room = c.workspace_bytes;
+  if (needs_copy(c.T, c.lddy)) {
+    // the copy lies at the workspace's start, the partial sums behind it
+    ld = aligned_pitch(c.rows);
+    const int64_t cap = int64_t(sm_count()) * 8;
+    launched = launch_maybe_pdl(roi_wgrad_align_kernel, int(c.T < cap ? c.T : cap), 256, 0, c.stream, wait, c.dY, c.lddy,
+                                reinterpret_cast<uint16_t*>(ws), ld, c.T, c.rows, wait);
+    if (launched < 0) return -1;
+    dY = reinterpret_cast<const uint16_t*>(ws);
+    const size_t used = wgrad_copy_bytes(c.T, c.rows, c.lddy);
+    ws += used;
+    room -= used;
+    wait = true;
+  }
+  WgradArgs a;
+  const size_t need = plan(c.T, c.rows, c.cols, a);
+  if (need > (ws == nullptr ? 0 : room)) a.ranges = 0;  // no room for partial sums: tiles stay whole
+  a.scales = c.scales;
+  a.dWm = c.dWm;
+  a.acc = c.acc;
+  a.part = reinterpret_cast<float*>(ws);
+  a.spitch = block8_scale_pitch(c.cols);
+  a.status = c.status;
+  a.wait = wait;
+  CUtensorMap tm_dy, tm_codes;
+  const int64_t pitch = block8_pitch(c.cols);
+  if (!make_tensor_map(&tm_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, dY, uint64_t(c.rows), uint64_t(c.T), uint64_t(ld) * 2, 64, kChunk,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
+      !make_tensor_map(&tm_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.codes, uint64_t(pitch), uint64_t(c.T), uint64_t(pitch), kEdge,
+                       kChunk, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
+    return -1;
+  auto kern = roi_wgrad_kernel<kGroup>;
+  constexpr size_t smem = kSmem + 1024;
+  static std::atomic<bool> set[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
+  if (!set[dev].load(std::memory_order_acquire)) {
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return -1;
+    set[dev].store(true, std::memory_order_release);
+  }
+  const int64_t busy = a.rounds > 0 ? a.groups : a.ranges > 0 ? a.ranges : a.rest;
+  if (launch_maybe_pdl(kern, int(busy) * kGroup, kThreads, smem, c.stream, wait, tm_dy, tm_codes, a) < 0) return -1;
+  ++launched;
+  if (a.ranges > 0) {
+    const int64_t quads = int64_t(a.rest) * kEdge * kGroup * kEdge * kGroup / 4, cap = int64_t(sm_count()) * 8;
+    const int64_t blocks = (quads + 255) / 256;
+    if (launch_maybe_pdl(roi_wgrad_join_kernel<kGroup>, int(blocks < cap ? blocks : cap), 256, 0, c.stream, true, a) < 0) return -1;
+    ++launched;
+  }
+  return launched;
+}
+
+}  // namespace roi
