@@ -38,12 +38,13 @@ constexpr int kStages = 5;
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
+constexpr uint32_t kScales = kChunk * 4;   // a word of four blocks a token
 constexpr uint32_t kStage = 2 * kOperand + kCodes;
 constexpr uint32_t kLanded = kOperand + kCodes;  // bytes of a stage that TMA brings
 constexpr int kConvertWarps = 8, kConvert = 32 * kConvertWarps;
 constexpr int kThreads = 64 + kConvert + 128;
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kSmem = kStages * kStage + 256;
+constexpr uint32_t kSmem = kStages * (kStage + kScales) + 256;
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
 // partial sums is written and read again.
 constexpr int kMinRange = 8, kSplitCost = 8;
@@ -164,7 +165,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kStages * kStage);
+  uint8_t* smem_scales = smem + kStages * kStage;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_scales + kStages * kScales);
   uint64_t *full = bars, *ready = full + kStages, *empty = ready + kStages, *sum = empty + kStages, *free = sum + 2;
   uint32_t* misc = reinterpret_cast<uint32_t*>(free + 2);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -173,7 +175,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(full + s, 1);
+      mbar_init(full + s, 1 + 32);  // the TMA copies', and each lane's copies of scales
       mbar_init(ready + s, kConvertWarps * CG);
       mbar_init(empty + s, 1);
     }
@@ -198,20 +200,29 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   Work w;
   int64_t m0, n0;
   if (warp == 0) {
-    if (lane == 0) {
-      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-        tile_origin(a, w.tile, kEdge * CG, m0, n0);
-        const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
-        for (int c = w.c0; c < w.c1; ++c, ++issued) {
-          const int s = issued % kStages;
-          ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
-          if (!ok) break;
+    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
+      const bool in = n / 32 < a.spitch;  // (a row's scales end with whole words)
+      for (int c = w.c0; c < w.c1; ++c, ++issued) {
+        const int s = issued % kStages;
+        ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
+        if (!ok) break;
+        if (lane == 0) {
           uint8_t* st = smem + s * kStage;
           mbar_arrive_expect_tx(full + s, kLanded);
           tma_load_2d(st, &tm_dy, m, c * kChunk, full + s);
           tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, full + s);
           tma_load_2d(st + 2 * kOperand, &tm_codes, n, c * kChunk, full + s);
         }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = lane + 32 * h;
+          const int64_t row = int64_t(c) * kChunk + k;
+          const bool there = in && row < a.T;
+          cp_async4_zfill(smem_scales + s * kScales + 4 * k, there ? a.scales + row * a.spitch + n / 32 : a.scales, there ? 4u : 0u);
+        }
+        cp_async_arrive(full + s);
       }
     }
   } else if (warp == 1) {
@@ -243,31 +254,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     const uint32_t first = (uint32_t(2 * (j & 3)) ^ swizzle) * 16, second = (uint32_t(2 * (j & 3) + 1) ^ swizzle) * 16;
     int n = 0;  // chunks done
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      tile_origin(a, w.tile, kEdge * CG, m0, n0);
-      const int64_t block = (n0 + int64_t(rank) * kEdge) / 32 + (j >> 1);
-      const uint8_t* sp = a.scales + block;
-      const bool in = block < a.spitch;
-      // the scales of a chunk are loaded while the one before is waited for
-      uint32_t scale[2], next[2];
-      auto load = [&](int c) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int64_t row = int64_t(c) * kChunk + k + 32 * h;
-          next[h] = in && c < w.c1 && row < a.T ? uint32_t(__ldg(sp + row * a.spitch)) : 0u;
-        }
-      };
-      load(w.c0);
       for (int c = w.c0; c < w.c1; ++c, ++n) {
         const int s = n % kStages;
-        scale[0] = next[0], scale[1] = next[1];
-        load(c + 1);
         ok = mbar_wait_ring(full + s, uint32_t(n / kStages) & 1u, lim);
         if (!ok) break;
         uint8_t* st = smem + s * kStage;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint4 q = *reinterpret_cast<const uint4*>(st + 2 * kOperand + (k + 32 * h) * kEdge + 16 * j);
-          const __nv_bfloat162 step = step_bf16x2(scale[h]);
+          const __nv_bfloat162 step = step_bf16x2(smem_scales[s * kScales + 4 * (k + 32 * h) + (j >> 1)]);
           const uint4 lo = codes8_bf16(q.x, q.y, step), hi = codes8_bf16(q.z, q.w, step);
           uint8_t* row = st + kOperand + half + (k + 32 * h) * 128;
           // four of the eight lanes of a row start with their upper half: no two on one bank
@@ -383,7 +378,10 @@ __global__ void __launch_bounds__(256) roi_wgrad_empty_kernel(uint16_t* dWm, con
     dWm[i] = __bfloat16_as_ushort(__float2bfloat16_rn(acc == nullptr ? 0.0f : acc[i]));
 }
 
-constexpr int kGroup = 1;
+#ifndef ROI_WGRAD_GROUP
+#define ROI_WGRAD_GROUP 2
+#endif
+constexpr int kGroup = ROI_WGRAD_GROUP;
 
 // The division of the work among the groups, and the bytes of partial sums it needs.
 size_t plan(int64_t T, int64_t rows, int64_t cols, WgradArgs& a) {
