@@ -41,8 +41,13 @@ constexpr uint32_t kCodes = kChunk * kEdge;
 constexpr uint32_t kScales = kChunk * 4;   // a word of four blocks a token
 constexpr uint32_t kStage = 2 * kOperand + kCodes;
 constexpr uint32_t kLanded = kOperand + kCodes;  // bytes of a stage that TMA brings
-constexpr int kConvertWarps = 8, kConvert = 32 * kConvertWarps;
-constexpr int kThreads = 64 + kConvert + 128;
+#ifndef ROI_WGRAD_SETS
+#define ROI_WGRAD_SETS 2
+#endif
+constexpr int kSets = ROI_WGRAD_SETS;      // sets of warps that turn codes into bf16, each every kSets-th chunk
+constexpr int kConvertWarps = 8;           // of a set
+constexpr int kWarpScales = 2 + kConvertWarps * kSets;  // warps 2 on: the sets; this one; four that write
+constexpr int kThreads = 32 * (kWarpScales + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSmem = kStages * (kStage + kScales) + 256;
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
@@ -200,29 +205,41 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   Work w;
   int64_t m0, n0;
   if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+        tile_origin(a, w.tile, kEdge * CG, m0, n0);
+        const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
+        for (int c = w.c0; c < w.c1; ++c, ++issued) {
+          const int s = issued % kStages;
+          ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
+          if (!ok) break;
+          uint8_t* st = smem + s * kStage;
+          mbar_arrive_expect_tx(full + s, kLanded);
+          tma_load_2d(st + 2 * kOperand, &tm_codes, n, c * kChunk, full + s);
+          tma_load_2d(st, &tm_dy, m, c * kChunk, full + s);
+          tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, full + s);
+        }
+      }
+    }
+  } else if (warp == kWarpScales) {
+    // the scales of a chunk: two tokens a lane, a word of four blocks each
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       tile_origin(a, w.tile, kEdge * CG, m0, n0);
-      const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
+      const int64_t n = n0 + int64_t(rank) * kEdge;
       const bool in = n / 32 < a.spitch;  // (a row's scales end with whole words)
+      int64_t row = int64_t(w.c0) * kChunk + lane;
+      const uint8_t* from = a.scales + row * a.spitch + n / 32;
       for (int c = w.c0; c < w.c1; ++c, ++issued) {
         const int s = issued % kStages;
         ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
         if (!ok) break;
-        if (lane == 0) {
-          uint8_t* st = smem + s * kStage;
-          mbar_arrive_expect_tx(full + s, kLanded);
-          tma_load_2d(st, &tm_dy, m, c * kChunk, full + s);
-          tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, full + s);
-          tma_load_2d(st + 2 * kOperand, &tm_codes, n, c * kChunk, full + s);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int k = lane + 32 * h;
-          const int64_t row = int64_t(c) * kChunk + k;
-          const bool there = in && row < a.T;
-          cp_async4_zfill(smem_scales + s * kScales + 4 * k, there ? a.scales + row * a.spitch + n / 32 : a.scales, there ? 4u : 0u);
-        }
+        uint8_t* to = smem_scales + s * kScales + 4 * lane;
+        const bool there = in && row < a.T, next = in && row + 32 < a.T;
+        cp_async4_zfill(to, there ? from : a.scales, there ? 4u : 0u);
+        cp_async4_zfill(to + 128, next ? from + 32 * a.spitch : a.scales, next ? 4u : 0u);
         cp_async_arrive(full + s);
+        row += kChunk;
+        from += kChunk * a.spitch;
       }
     }
   } else if (warp == 1) {
@@ -247,14 +264,15 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         if (ok) tc_commit_group<CG>(sum + b);
       }
     }
-  } else if (warp < 2 + kConvertWarps) {
+  } else if (warp < 2 + kConvertWarps * kSets) {
     // this thread's codes of a chunk: 16 inputs from 16 j on, of tokens k and k + 32
-    const int t = tid - 64, k = t >> 3, j = t & 7;
+    const int t = (tid - 64) % (32 * kConvertWarps), set = (warp - 2) / kConvertWarps, k = t >> 3, j = t & 7;
     const uint32_t half = uint32_t(j >> 2) * kHalf, swizzle = uint32_t(k & 7);
     const uint32_t first = (uint32_t(2 * (j & 3)) ^ swizzle) * 16, second = (uint32_t(2 * (j & 3) + 1) ^ swizzle) * 16;
     int n = 0;  // chunks done
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       for (int c = w.c0; c < w.c1; ++c, ++n) {
+        if (n % kSets != set) continue;
         const int s = n % kStages;
         ok = mbar_wait_ring(full + s, uint32_t(n / kStages) & 1u, lim);
         if (!ok) break;
@@ -308,7 +326,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   __syncthreads();
   if (misc[1] == 0u) {
     // a wait gave up: the copies this CTA sent off land, and its MMAs end, before it leaves
-    if (warp == 0 && lane == 0) {
+    if (warp == 0 || warp == kWarpScales) {
       for (int c = issued > kStages ? issued - kStages : 0; c < issued; ++c)
         mbar_wait_bounded(full + c % kStages, uint32_t(c / kStages) & 1u);
     }
