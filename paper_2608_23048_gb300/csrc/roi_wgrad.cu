@@ -34,22 +34,28 @@ namespace {
 
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
 constexpr int kChunk = 64;                 // tokens a stage
-constexpr int kStages = 5;
+#ifndef ROI_WGRAD_STAGES
+#define ROI_WGRAD_STAGES 7
+#define ROI_WGRAD_SLOTS 3
+#endif
+constexpr int kStages = ROI_WGRAD_STAGES;  // of dY, codes and scales
+constexpr int kSlots = ROI_WGRAD_SLOTS;    // of converted x^: fewer, as nothing waits for memory in between
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
 constexpr uint32_t kScales = kChunk * 4;   // a word of four blocks a token
-constexpr uint32_t kStage = 2 * kOperand + kCodes;
-constexpr uint32_t kLanded = kOperand + kCodes;  // bytes of a stage that TMA brings
+constexpr uint32_t kStage = kOperand + kCodes;
+constexpr uint32_t kOffSlots = kStages * kStage, kOffScales = kOffSlots + kSlots * kOperand;
+constexpr uint32_t kOffBars = kOffScales + kStages * kScales;
 #ifndef ROI_WGRAD_SETS
 #define ROI_WGRAD_SETS 2
 #endif
 constexpr int kSets = ROI_WGRAD_SETS;      // sets of warps that turn codes into bf16, each every kSets-th chunk
-constexpr int kConvertWarps = 8;           // of a set
+constexpr int kConvertWarps = 4;           // of a set
 constexpr int kWarpScales = 2 + kConvertWarps * kSets;  // warps 2 on: the sets; this one; four that write
 constexpr int kThreads = 32 * (kWarpScales + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kSmem = kStages * (kStage + kScales) + 256;
+constexpr uint32_t kSmem = kOffBars + 256;
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
 // partial sums is written and read again.
 constexpr int kMinRange = 8, kSplitCost = 8;
@@ -115,23 +121,43 @@ __device__ __forceinline__ void tile_origin(const WgradArgs& a, int tile, int ed
   n0 = int64_t(n) * edge;
 }
 
-// Four codes to four bf16 (two words), times the block's power of two.  A code byte b is
-// (128 + (b & 127)) - (128 + (b & 128)): both terms are bf16 numbers whose mantissa holds the
-// byte's bits, and the difference is exact.
-__device__ __forceinline__ uint32_t codes2_bf16(uint32_t spread, __nv_bfloat162 step) {
-  const uint32_t m = (spread & 0x007f007fu) | 0x43004300u, n = (spread & 0x00800080u) | 0x43004300u;
+// Two codes to two bf16, times the block's power of two: the codes in the low bytes of the
+// halves of `w` (the high bytes are ignored).  A code byte b is (128 + (b & 127)) -
+// (128 + (b & 128)): both terms are bf16 numbers whose mantissa holds the byte's bits, and
+// difference and product are exact.
+__device__ __forceinline__ uint32_t codes2_bf16(uint32_t w, __nv_bfloat162 step) {
+  const uint32_t m = (w & 0x007f007fu) | 0x43004300u, n = (w & 0x00800080u) | 0x43004300u;
   const __nv_bfloat162 v = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&m), *reinterpret_cast<const __nv_bfloat162*>(&n)), step);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+// Eight codes (two words) to eight bf16.  The even bytes of a word are taken where they are and
+// the odd ones after one shift, which leaves each four in the order 0, 2, 1, 3: the order of the
+// tile's columns in the sums, which the epilogue undoes (input_order) at no cost.
 __device__ __forceinline__ uint4 codes8_bf16(uint32_t a, uint32_t b, __nv_bfloat162 step) {
-  return make_uint4(codes2_bf16(__byte_perm(a, 0, 0x4140), step), codes2_bf16(__byte_perm(a, 0, 0x4342), step),
-                    codes2_bf16(__byte_perm(b, 0, 0x4140), step), codes2_bf16(__byte_perm(b, 0, 0x4342), step));
+  return make_uint4(codes2_bf16(a, step), codes2_bf16(a >> 8, step), codes2_bf16(b, step), codes2_bf16(b >> 8, step));
+}
+__device__ __forceinline__ void input_order(const uint32_t (&u)[32], float (&v)[32]) {
+#pragma unroll
+  for (int e = 0; e < 32; e += 4) {
+    v[e] = __uint_as_float(u[e]), v[e + 1] = __uint_as_float(u[e + 2]);
+    v[e + 2] = __uint_as_float(u[e + 1]), v[e + 3] = __uint_as_float(u[e + 3]);
+  }
 }
 __device__ __forceinline__ __nv_bfloat162 step_bf16x2(uint32_t s) {
   const uint32_t h = __float_as_uint(block8_step(s)) >> 16;
   const uint32_t w = h | (h << 16);
   return *reinterpret_cast<const __nv_bfloat162*>(&w);
 }
+
+// A place in a ring of N, and the parity of the pass over it.
+template <int N>
+struct Ring {
+  int at = 0;
+  uint32_t pass = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) at = 0, pass ^= 1u;
+  }
+};
 
 // 32 columns of a row of the sums, from column n on: added to acc, and written out.
 __device__ __forceinline__ void store_sums(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
@@ -170,9 +196,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* smem_scales = smem + kStages * kStage;
-  uint64_t* bars = reinterpret_cast<uint64_t*>(smem_scales + kStages * kScales);
-  uint64_t *full = bars, *ready = full + kStages, *empty = ready + kStages, *sum = empty + kStages, *free = sum + 2;
+  uint8_t* smem_scales = smem + kOffScales;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
+  uint64_t *full = bars, *empty = full + kStages, *ready = empty + kStages, *sum = ready + kSlots, *free = sum + 2;
   uint32_t* misc = reinterpret_cast<uint32_t*>(free + 2);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_rank();
@@ -181,9 +207,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + s, 1 + 32);  // the TMA copies', and each lane's copies of scales
-      mbar_init(ready + s, kConvertWarps * CG);
       mbar_init(empty + s, 1);
     }
+    for (int s = 0; s < kSlots; ++s) mbar_init(ready + s, kConvertWarps * CG);
     for (int b = 0; b < 2; ++b) {
       mbar_init(sum + b, 1);
       mbar_init(free + b, 4 * CG);
@@ -204,20 +230,21 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   int issued = 0, committed = 0;  // chunks whose copies, and whose MMAs, this thread has sent off
   Work w;
   int64_t m0, n0;
+  Ring<kStages> ring;
   if (warp == 0) {
     if (lane == 0) {
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         tile_origin(a, w.tile, kEdge * CG, m0, n0);
         const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
-        for (int c = w.c0; c < w.c1; ++c, ++issued) {
-          const int s = issued % kStages;
-          ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
+        for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
+          ok = mbar_wait_ring_cluster(empty + ring.at, ring.pass ^ 1u, lim);
           if (!ok) break;
-          uint8_t* st = smem + s * kStage;
-          mbar_arrive_expect_tx(full + s, kLanded);
-          tma_load_2d(st + 2 * kOperand, &tm_codes, n, c * kChunk, full + s);
-          tma_load_2d(st, &tm_dy, m, c * kChunk, full + s);
-          tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, full + s);
+          uint8_t* st = smem + ring.at * kStage;
+          uint64_t* bar = full + ring.at;
+          mbar_arrive_expect_tx(bar, kStage);
+          tma_load_2d(st + kOperand, &tm_codes, n, c * kChunk, bar);
+          tma_load_2d(st, &tm_dy, m, c * kChunk, bar);
+          tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, bar);
         }
       }
     }
@@ -229,15 +256,14 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       const bool in = n / 32 < a.spitch;  // (a row's scales end with whole words)
       int64_t row = int64_t(w.c0) * kChunk + lane;
       const uint8_t* from = a.scales + row * a.spitch + n / 32;
-      for (int c = w.c0; c < w.c1; ++c, ++issued) {
-        const int s = issued % kStages;
-        ok = mbar_wait_ring_cluster(empty + s, (uint32_t(issued / kStages) & 1u) ^ 1u, lim);
+      for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
+        ok = mbar_wait_ring_cluster(empty + ring.at, ring.pass ^ 1u, lim);
         if (!ok) break;
-        uint8_t* to = smem_scales + s * kScales + 4 * lane;
+        uint8_t* to = smem_scales + ring.at * kScales + 4 * lane;
         const bool there = in && row < a.T, next = in && row + 32 < a.T;
         cp_async4_zfill(to, there ? from : a.scales, there ? 4u : 0u);
         cp_async4_zfill(to + 128, next ? from + 32 * a.spitch : a.scales, next ? 4u : 0u);
-        cp_async_arrive(full + s);
+        cp_async_arrive(full + ring.at);
         row += kChunk;
         from += kChunk * a.spitch;
       }
@@ -245,52 +271,72 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {
       const uint32_t idesc = tc_idesc_bf16_f32_mn(kEdge * CG, kEdge * CG);
+      // descriptors of the first stage and slot; addresses count in units of 16 bytes
+      const uint64_t dy0 = tc_smem_desc_mn128(smem_addr(smem), kHalf), x0 = tc_smem_desc_mn128(smem_addr(smem + kOffSlots), kHalf);
+      Ring<kSlots> slot;
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         const int b = i & 1;
         ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
         const uint32_t d = tmem + uint32_t(b) * (kEdge * CG);
-        for (int c = w.c0; ok && c < w.c1; ++c, ++committed) {
-          const int s = committed % kStages;
-          ok = mbar_wait_ring_cluster(ready + s, uint32_t(committed / kStages) & 1u, lim);
+        bool add = false;
+        for (int c = w.c0; ok && c < w.c1; ++c, ++committed, ring.next(), slot.next()) {
+          ok = mbar_wait_ring_cluster(ready + slot.at, slot.pass, lim);
           if (!ok) break;
           tc_fence_after();
-          const uint32_t st = smem_addr(smem + s * kStage);
+          const uint64_t dy = dy0 + uint32_t(ring.at) * (kStage / 16), x = x0 + uint32_t(slot.at) * (kOperand / 16);
 #pragma unroll
-          for (int k = 0; k < kChunk / 16; ++k)
-            tc_mma_bf16_group<CG>(d, tc_smem_desc_mn128(st + k * 2048, kHalf), tc_smem_desc_mn128(st + kOperand + k * 2048, kHalf),
-                                  idesc, c > w.c0 || k > 0);
-          tc_commit_group<CG>(empty + s);
+          for (int k = 0; k < kChunk / 16; ++k) {
+            tc_mma_bf16_group<CG>(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, add);
+            add = true;
+          }
+          tc_commit_group<CG>(empty + ring.at);
         }
         if (ok) tc_commit_group<CG>(sum + b);
       }
     }
   } else if (warp < 2 + kConvertWarps * kSets) {
-    // this thread's codes of a chunk: 16 inputs from 16 j on, of tokens k and k + 32
-    const int t = (tid - 64) % (32 * kConvertWarps), set = (warp - 2) / kConvertWarps, k = t >> 3, j = t & 7;
-    const uint32_t half = uint32_t(j >> 2) * kHalf, swizzle = uint32_t(k & 7);
-    const uint32_t first = (uint32_t(2 * (j & 3)) ^ swizzle) * 16, second = (uint32_t(2 * (j & 3) + 1) ^ swizzle) * 16;
-    int n = 0;  // chunks done
-    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      for (int c = w.c0; c < w.c1; ++c, ++n) {
-        if (n % kSets != set) continue;
-        const int s = n % kStages;
-        ok = mbar_wait_ring(full + s, uint32_t(n / kStages) & 1u, lim);
+    // This thread's codes of a chunk: block b (of four) of tokens k and k + 32.  The block's four
+    // 16-byte pieces of bf16 come in the order of its two 16-byte pieces of codes, and which of
+    // those is first changes with the token and the half, so that neither the loads nor the
+    // stores of eight neighbouring lanes meet on a bank.
+    const int t = (tid - 64) % (32 * kConvertWarps), set = (warp - 2) / kConvertWarps, k = t >> 2, b = t & 3;
+    const uint32_t second = uint32_t((b >> 1) ^ (k & 1));  // whether the second piece of codes goes first
+    const uint32_t codes_at = kOperand + k * kEdge + 32 * b + 16 * second, scale_at = 4 * k + b;
+    const uint32_t row = uint32_t(b >> 1) * kHalf + uint32_t(k) * 128;
+    uint32_t piece[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) piece[e] = row + (((uint32_t(b & 1) * 4 + (uint32_t(e) ^ (2 * second))) ^ uint32_t(k & 7)) * 16);
+    uint32_t n = 0;  // chunks of the tiles before
+    for (int i = 0; ok && work_of(a, g, i, w); n += uint32_t(w.c1 - w.c0), ++i) {
+      for (uint32_t q = n + (uint32_t(set) + kSets - n % kSets) % kSets; q < n + uint32_t(w.c1 - w.c0); q += kSets) {
+        const uint32_t stage = q % kStages, slot = q % kSlots;
+        ok = mbar_wait_ring(full + stage, (q / kStages) & 1u, lim);
         if (!ok) break;
-        uint8_t* st = smem + s * kStage;
+        const uint8_t* codes = smem + stage * kStage + codes_at;
+        uint4 o[2][4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint4 q = *reinterpret_cast<const uint4*>(st + 2 * kOperand + (k + 32 * h) * kEdge + 16 * j);
-          const __nv_bfloat162 step = step_bf16x2(smem_scales[s * kScales + 4 * (k + 32 * h) + (j >> 1)]);
-          const uint4 lo = codes8_bf16(q.x, q.y, step), hi = codes8_bf16(q.z, q.w, step);
-          uint8_t* row = st + kOperand + half + (k + 32 * h) * 128;
-          // four of the eight lanes of a row start with their upper half: no two on one bank
-          const bool up = j >= 4;
-          *reinterpret_cast<uint4*>(row + (up ? second : first)) = up ? hi : lo;
-          *reinterpret_cast<uint4*>(row + (up ? first : second)) = up ? lo : hi;
+          const uint4 c0 = *reinterpret_cast<const uint4*>(codes + 32 * kEdge * h);
+          const uint4 c1 = *reinterpret_cast<const uint4*>(smem + ((stage * kStage + codes_at) ^ 16u) + 32 * kEdge * h);
+          const __nv_bfloat162 step = step_bf16x2(smem_scales[stage * kScales + scale_at + 128 * h]);
+          o[h][0] = codes8_bf16(c0.x, c0.y, step), o[h][1] = codes8_bf16(c0.z, c0.w, step);
+          o[h][2] = codes8_bf16(c1.x, c1.y, step), o[h][3] = codes8_bf16(c1.z, c1.w, step);
+        }
+        // the slot is free once the MMAs of the chunk that had it are done: what `empty` of that
+        // chunk's stage says (whose next phase cannot end before this chunk is converted)
+        if (q >= kSlots) {
+          ok = mbar_wait_ring_cluster(empty + (q - kSlots) % kStages, ((q - kSlots) / kStages) & 1u, lim);
+          if (!ok) break;
+        }
+        uint8_t* to = smem + kOffSlots + slot * kOperand;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(to + piece[e] + 32 * 128 * h) = o[h][e];
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(ready + s, 0);
+        if (lane == 0) mbar_arrive_cluster(ready + slot, 0);
       }
     }
   } else {
@@ -308,8 +354,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         uint32_t u[32];
         tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * (kEdge * CG) + 32 * q), u);
         float v[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
+        input_order(u, v);
         if (w.slot >= 0) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + 32 * q + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
