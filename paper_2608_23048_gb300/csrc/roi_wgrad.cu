@@ -35,11 +35,12 @@ namespace {
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
 constexpr int kChunk = 64;                 // tokens a stage
 #ifndef ROI_WGRAD_STAGES
-#define ROI_WGRAD_STAGES 7
-#define ROI_WGRAD_SLOTS 3
+#define ROI_WGRAD_STAGES 6
+#define ROI_WGRAD_SLOTS 4
 #endif
 constexpr int kStages = ROI_WGRAD_STAGES;  // of dY, codes and scales
 constexpr int kSlots = ROI_WGRAD_SLOTS;    // of converted x^: fewer, as nothing waits for memory in between
+static_assert(kSlots <= kStages, "a slot is taken again once its chunk's stage is");
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
@@ -48,7 +49,7 @@ constexpr uint32_t kStage = kOperand + kCodes;
 constexpr uint32_t kOffSlots = kStages * kStage, kOffScales = kOffSlots + kSlots * kOperand;
 constexpr uint32_t kOffBars = kOffScales + kStages * kScales;
 #ifndef ROI_WGRAD_SETS
-#define ROI_WGRAD_SETS 2
+#define ROI_WGRAD_SETS 4
 #endif
 constexpr int kSets = ROI_WGRAD_SETS;      // sets of warps that turn codes into bf16, each every kSets-th chunk
 constexpr int kConvertWarps = 4;           // of a set
