@@ -34,27 +34,32 @@ namespace {
 
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
 constexpr int kChunk = 64;                 // tokens a stage
-#ifndef ROI_WGRAD_STAGES
-#define ROI_WGRAD_STAGES 6
+#ifndef ROI_WGRAD_CODES
+#define ROI_WGRAD_CODES 7
+#define ROI_WGRAD_DY 6
 #define ROI_WGRAD_SLOTS 4
 #endif
-constexpr int kStages = ROI_WGRAD_STAGES;  // of dY, codes and scales
-constexpr int kSlots = ROI_WGRAD_SLOTS;    // of converted x^: fewer, as nothing waits for memory in between
-static_assert(kSlots <= kStages, "a slot is taken again once its chunk's stage is");
+#ifndef ROI_WGRAD_SETS
+#define ROI_WGRAD_SETS 4
+#endif
+#ifndef ROI_WGRAD_WARPS
+#define ROI_WGRAD_WARPS 4
+#endif
+// Rings: codes and scales, dY, and converted x^ (where nothing waits for memory in between).
+constexpr int kCodeStages = ROI_WGRAD_CODES, kDyStages = ROI_WGRAD_DY, kSlots = ROI_WGRAD_SLOTS;
+static_assert(kSlots <= kDyStages, "a slot is taken again once the dY of its chunk is done with");
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
 constexpr uint32_t kScales = kChunk * 4;   // a word of four blocks a token
-constexpr uint32_t kStage = kOperand + kCodes;
-constexpr uint32_t kOffSlots = kStages * kStage, kOffScales = kOffSlots + kSlots * kOperand;
-constexpr uint32_t kOffBars = kOffScales + kStages * kScales;
-#ifndef ROI_WGRAD_SETS
-#define ROI_WGRAD_SETS 4
-#endif
-constexpr int kSets = ROI_WGRAD_SETS;      // sets of warps that turn codes into bf16, each every kSets-th chunk
-constexpr int kConvertWarps = 4;           // of a set
-constexpr int kWarpScales = 2 + kConvertWarps * kSets;  // warps 2 on: the sets; this one; four that write
-constexpr int kThreads = 32 * (kWarpScales + 1 + 4);
+constexpr uint32_t kOffSlots = kDyStages * kOperand, kOffCodes = kOffSlots + kSlots * kOperand;
+constexpr uint32_t kOffScales = kOffCodes + kCodeStages * kCodes, kOffBars = kOffScales + kCodeStages * kScales;
+constexpr int kSets = ROI_WGRAD_SETS;            // sets of warps that turn codes into bf16, each every kSets-th chunk
+constexpr int kConvertWarps = ROI_WGRAD_WARPS;   // of a set
+constexpr int kUnits = 8 / kConvertWarps;        // blocks of 32 codes a thread takes of a chunk
+// warp 0: dY; 1: MMA; 2 on: the sets; then codes and scales; the landed dY's notice; four that write
+constexpr int kWarpCodes = 2 + kConvertWarps * kSets, kWarpNotice = kWarpCodes + 1;
+constexpr int kThreads = 32 * (kWarpNotice + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
 constexpr uint32_t kSmem = kOffBars + 256;
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
@@ -197,20 +202,24 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* smem_scales = smem + kOffScales;
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
-  uint64_t *full = bars, *empty = full + kStages, *ready = empty + kStages, *sum = ready + kSlots, *free = sum + 2;
+  uint64_t *code_full = bars, *code_empty = code_full + kCodeStages, *dy_full = code_empty + kCodeStages, *dy_empty = dy_full + kDyStages;
+  uint64_t *ready = dy_empty + kDyStages, *sum = ready + kSlots, *free = sum + 2;
   uint32_t* misc = reinterpret_cast<uint32_t*>(free + 2);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_rank();
   const int g = blockIdx.x / CG;
 
   if (tid == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(full + s, 1 + 32);  // the TMA copies', and each lane's copies of scales
-      mbar_init(empty + s, 1);
+    for (int s = 0; s < kCodeStages; ++s) {
+      mbar_init(code_full + s, 1 + 32);  // the TMA copy, and each lane's copies of scales
+      mbar_init(code_empty + s, kConvertWarps);
     }
-    for (int s = 0; s < kSlots; ++s) mbar_init(ready + s, kConvertWarps * CG);
+    for (int s = 0; s < kDyStages; ++s) {
+      mbar_init(dy_full + s, 1);
+      mbar_init(dy_empty + s, 1);
+    }
+    for (int s = 0; s < kSlots; ++s) mbar_init(ready + s, (kConvertWarps + 1) * CG);
     for (int b = 0; b < 2; ++b) {
       mbar_init(sum + b, 1);
       mbar_init(free + b, 4 * CG);
@@ -231,42 +240,65 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   int issued = 0, committed = 0;  // chunks whose copies, and whose MMAs, this thread has sent off
   Work w;
   int64_t m0, n0;
-  Ring<kStages> ring;
+  Ring<kDyStages> ring;
+  Ring<kCodeStages> code_ring;
+  Ring<kSlots> slot;
+  // A slot, and its `ready`, are free again once the MMAs of the chunk that had it are done: what
+  // dy_empty of that chunk's stage says (whose next phase cannot end before this chunk is ready).
+  auto slot_free = [&](uint32_t q) {
+    return q < kSlots || mbar_wait_ring_cluster(dy_empty + (q - kSlots) % kDyStages, ((q - kSlots) / kDyStages) & 1u, lim);
+  };
   if (warp == 0) {
     if (lane == 0) {
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         tile_origin(a, w.tile, kEdge * CG, m0, n0);
-        const int m = int(m0) + int(rank) * kEdge, n = int(n0) + int(rank) * kEdge;
+        const int m = int(m0) + int(rank) * kEdge;
         for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
-          ok = mbar_wait_ring_cluster(empty + ring.at, ring.pass ^ 1u, lim);
+          ok = mbar_wait_ring_cluster(dy_empty + ring.at, ring.pass ^ 1u, lim);
           if (!ok) break;
-          uint8_t* st = smem + ring.at * kStage;
-          uint64_t* bar = full + ring.at;
-          mbar_arrive_expect_tx(bar, kStage);
-          tma_load_2d(st + kOperand, &tm_codes, n, c * kChunk, bar);
+          uint8_t* st = smem + ring.at * kOperand;
+          uint64_t* bar = dy_full + ring.at;
+          mbar_arrive_expect_tx(bar, kOperand);
           tma_load_2d(st, &tm_dy, m, c * kChunk, bar);
           tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, bar);
         }
       }
     }
-  } else if (warp == kWarpScales) {
-    // the scales of a chunk: two tokens a lane, a word of four blocks each
+  } else if (warp == kWarpCodes) {
+    // codes, and scales: two tokens a lane, a word of four blocks each
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       tile_origin(a, w.tile, kEdge * CG, m0, n0);
       const int64_t n = n0 + int64_t(rank) * kEdge;
       const bool in = n / 32 < a.spitch;  // (a row's scales end with whole words)
       int64_t row = int64_t(w.c0) * kChunk + lane;
       const uint8_t* from = a.scales + row * a.spitch + n / 32;
-      for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
-        ok = mbar_wait_ring_cluster(empty + ring.at, ring.pass ^ 1u, lim);
+      for (int c = w.c0; c < w.c1; ++c, ++issued, code_ring.next()) {
+        ok = mbar_wait_ring(code_empty + code_ring.at, code_ring.pass ^ 1u, lim);
         if (!ok) break;
-        uint8_t* to = smem_scales + ring.at * kScales + 4 * lane;
+        uint64_t* bar = code_full + code_ring.at;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(bar, kCodes);
+          tma_load_2d(smem + kOffCodes + code_ring.at * kCodes, &tm_codes, int(n), c * kChunk, bar);
+        }
+        uint8_t* to = smem + kOffScales + code_ring.at * kScales + 4 * lane;
         const bool there = in && row < a.T, next = in && row + 32 < a.T;
         cp_async4_zfill(to, there ? from : a.scales, there ? 4u : 0u);
         cp_async4_zfill(to + 128, next ? from + 32 * a.spitch : a.scales, next ? 4u : 0u);
-        cp_async_arrive(full + ring.at);
+        cp_async_arrive(bar);
         row += kChunk;
         from += kChunk * a.spitch;
+      }
+    }
+  } else if (warp == kWarpNotice) {
+    // tells the thread that issues the MMAs, the pair's for both CTAs, that dY has landed
+    if (lane == 0) {
+      uint32_t q = 0;
+      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+        for (int c = w.c0; c < w.c1; ++c, ++q, ring.next(), slot.next()) {
+          ok = mbar_wait_ring(dy_full + ring.at, ring.pass, lim) && slot_free(q);
+          if (!ok) break;
+          mbar_arrive_cluster(ready + slot.at, 0);
+        }
       }
     }
   } else if (warp == 1) {
@@ -274,7 +306,6 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       const uint32_t idesc = tc_idesc_bf16_f32_mn(kEdge * CG, kEdge * CG);
       // descriptors of the first stage and slot; addresses count in units of 16 bytes
       const uint64_t dy0 = tc_smem_desc_mn128(smem_addr(smem), kHalf), x0 = tc_smem_desc_mn128(smem_addr(smem + kOffSlots), kHalf);
-      Ring<kSlots> slot;
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         const int b = i & 1;
         ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
@@ -284,60 +315,59 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
           ok = mbar_wait_ring_cluster(ready + slot.at, slot.pass, lim);
           if (!ok) break;
           tc_fence_after();
-          const uint64_t dy = dy0 + uint32_t(ring.at) * (kStage / 16), x = x0 + uint32_t(slot.at) * (kOperand / 16);
+          const uint64_t dy = dy0 + uint32_t(ring.at) * (kOperand / 16), x = x0 + uint32_t(slot.at) * (kOperand / 16);
 #pragma unroll
           for (int k = 0; k < kChunk / 16; ++k) {
             tc_mma_bf16_group<CG>(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, add);
             add = true;
           }
-          tc_commit_group<CG>(empty + ring.at);
+          tc_commit_group<CG>(dy_empty + ring.at);
         }
         if (ok) tc_commit_group<CG>(sum + b);
       }
     }
   } else if (warp < 2 + kConvertWarps * kSets) {
-    // This thread's codes of a chunk: block b (of four) of tokens k and k + 32.  The block's four
-    // 16-byte pieces of bf16 come in the order of its two 16-byte pieces of codes, and which of
-    // those is first changes with the token and the half, so that neither the loads nor the
-    // stores of eight neighbouring lanes meet on a bank.
+    // This thread's codes of a chunk: block b (of four) of every (64 / kUnits)-th token from k on.
+    // The block's four 16-byte pieces of bf16 come in the order of its two 16-byte pieces of
+    // codes, and which of those is first changes with the token and the half, so that neither the
+    // loads nor the stores of eight neighbouring lanes meet on a bank.
     const int t = (tid - 64) % (32 * kConvertWarps), set = (warp - 2) / kConvertWarps, k = t >> 2, b = t & 3;
+    constexpr int kStep = kChunk / kUnits;  // tokens from one unit to the next
     const uint32_t second = uint32_t((b >> 1) ^ (k & 1));  // whether the second piece of codes goes first
-    const uint32_t codes_at = kOperand + k * kEdge + 32 * b + 16 * second, scale_at = 4 * k + b;
-    const uint32_t row = uint32_t(b >> 1) * kHalf + uint32_t(k) * 128;
+    const uint32_t codes_at = kOffCodes + k * kEdge + 32 * b + 16 * second, scale_at = kOffScales + 4 * k + b;
+    const uint32_t row = kOffSlots + uint32_t(b >> 1) * kHalf + uint32_t(k) * 128;
     uint32_t piece[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) piece[e] = row + (((uint32_t(b & 1) * 4 + (uint32_t(e) ^ (2 * second))) ^ uint32_t(k & 7)) * 16);
     uint32_t n = 0;  // chunks of the tiles before
     for (int i = 0; ok && work_of(a, g, i, w); n += uint32_t(w.c1 - w.c0), ++i) {
       for (uint32_t q = n + (uint32_t(set) + kSets - n % kSets) % kSets; q < n + uint32_t(w.c1 - w.c0); q += kSets) {
-        const uint32_t stage = q % kStages, slot = q % kSlots;
-        ok = mbar_wait_ring(full + stage, (q / kStages) & 1u, lim);
+        const uint32_t stage = q % kCodeStages, slot_at = q % kSlots;
+        ok = mbar_wait_ring(code_full + stage, (q / kCodeStages) & 1u, lim);
         if (!ok) break;
-        const uint8_t* codes = smem + stage * kStage + codes_at;
-        uint4 o[2][4];
+        uint4 o[kUnits][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint4 c0 = *reinterpret_cast<const uint4*>(codes + 32 * kEdge * h);
-          const uint4 c1 = *reinterpret_cast<const uint4*>(smem + ((stage * kStage + codes_at) ^ 16u) + 32 * kEdge * h);
-          const __nv_bfloat162 step = step_bf16x2(smem_scales[stage * kScales + scale_at + 128 * h]);
+        for (int h = 0; h < kUnits; ++h) {
+          const uint32_t at = stage * kCodes + codes_at + kStep * kEdge * h;
+          const uint4 c0 = *reinterpret_cast<const uint4*>(smem + at), c1 = *reinterpret_cast<const uint4*>(smem + (at ^ 16u));
+          const __nv_bfloat162 step = step_bf16x2(smem[stage * kScales + scale_at + 4 * kStep * h]);
           o[h][0] = codes8_bf16(c0.x, c0.y, step), o[h][1] = codes8_bf16(c0.z, c0.w, step);
           o[h][2] = codes8_bf16(c1.x, c1.y, step), o[h][3] = codes8_bf16(c1.z, c1.w, step);
         }
-        // the slot is free once the MMAs of the chunk that had it are done: what `empty` of that
-        // chunk's stage says (whose next phase cannot end before this chunk is converted)
-        if (q >= kSlots) {
-          ok = mbar_wait_ring_cluster(empty + (q - kSlots) % kStages, ((q - kSlots) / kStages) & 1u, lim);
-          if (!ok) break;
-        }
-        uint8_t* to = smem + kOffSlots + slot * kOperand;
+        ok = slot_free(q);
+        if (!ok) break;
+        uint8_t* to = smem + slot_at * kOperand;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < kUnits; ++h) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(to + piece[e] + 32 * 128 * h) = o[h][e];
+          for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(to + piece[e] + kStep * 128 * h) = o[h][e];
         }
         fence_proxy_async_smem();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(ready + slot, 0);
+        if (lane == 0) {
+          mbar_arrive(code_empty + stage);
+          mbar_arrive_cluster(ready + slot_at, 0);
+        }
       }
     }
   } else {
@@ -372,12 +402,16 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   __syncthreads();
   if (misc[1] == 0u) {
     // a wait gave up: the copies this CTA sent off land, and its MMAs end, before it leaves
-    if (warp == 0 || warp == kWarpScales) {
-      for (int c = issued > kStages ? issued - kStages : 0; c < issued; ++c)
-        mbar_wait_bounded(full + c % kStages, uint32_t(c / kStages) & 1u);
+    if (warp == 0 && lane == 0) {
+      for (int c = issued > kDyStages ? issued - kDyStages : 0; c < issued; ++c)
+        mbar_wait_bounded(dy_full + c % kDyStages, uint32_t(c / kDyStages) & 1u);
+    }
+    if (warp == kWarpCodes) {
+      for (int c = issued > kCodeStages ? issued - kCodeStages : 0; c < issued; ++c)
+        mbar_wait_bounded(code_full + c % kCodeStages, uint32_t(c / kCodeStages) & 1u);
     }
     if (warp == 1 && committed > 0)
-      mbar_wait_bounded(empty + (committed - 1) % kStages, uint32_t((committed - 1) / kStages) & 1u);
+      mbar_wait_bounded(dy_empty + (committed - 1) % kDyStages, uint32_t((committed - 1) / kDyStages) & 1u);
     if (tid == 0) atomicOr(a.status, kStatusTimeout);
     __syncthreads();
   }
