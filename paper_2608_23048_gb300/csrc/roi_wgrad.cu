@@ -35,19 +35,14 @@ namespace {
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
 constexpr int kChunk = 64;                 // tokens a stage
 #ifndef ROI_WGRAD_CODES
-#define ROI_WGRAD_CODES 7
-#define ROI_WGRAD_DY 6
-#define ROI_WGRAD_SLOTS 4
-#endif
-#ifndef ROI_WGRAD_SETS
-#define ROI_WGRAD_SETS 4
-#endif
-#ifndef ROI_WGRAD_WARPS
-#define ROI_WGRAD_WARPS 4
+#define ROI_WGRAD_CODES 10
+#define ROI_WGRAD_DY 5
+#define ROI_WGRAD_SLOTS 3
+#define ROI_WGRAD_SETS 5
+#define ROI_WGRAD_WARPS 2
 #endif
 // Rings: codes and scales, dY, and converted x^ (where nothing waits for memory in between).
 constexpr int kCodeStages = ROI_WGRAD_CODES, kDyStages = ROI_WGRAD_DY, kSlots = ROI_WGRAD_SLOTS;
-static_assert(kSlots <= kDyStages, "a slot is taken again once the dY of its chunk is done with");
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
@@ -56,6 +51,10 @@ constexpr uint32_t kOffSlots = kDyStages * kOperand, kOffCodes = kOffSlots + kSl
 constexpr uint32_t kOffScales = kOffCodes + kCodeStages * kCodes, kOffBars = kOffScales + kCodeStages * kScales;
 constexpr int kSets = ROI_WGRAD_SETS;            // sets of warps that turn codes into bf16, each every kSets-th chunk
 constexpr int kConvertWarps = ROI_WGRAD_WARPS;   // of a set
+// A wait for a phase of a barrier takes the one before to be over.  Copies may land out of their
+// order, so a set waits for every phase of its code stages itself; dY's stages end in order, and a
+// set that waits for one has seen a chunk end that is at most kSets before.
+static_assert(kCodeStages % kSets == 0 && kSlots <= kDyStages && kSets <= kDyStages, "phases in turn");
 constexpr int kUnits = 8 / kConvertWarps;        // blocks of 32 codes a thread takes of a chunk
 // warp 0: dY; 1: MMA; 2 on: the sets; then codes and scales; the landed dY's notice; four that write
 constexpr int kWarpCodes = 2 + kConvertWarps * kSets, kWarpNotice = kWarpCodes + 1;
@@ -70,7 +69,7 @@ struct WgradArgs {
   const uint8_t* scales;
   uint16_t* dWm;  // nullable
   float* acc;     // nullable
-  float* part;    // [2 * ranges][128 CG][128 CG] (split)
+  float* part;    // [2 * ranges][32 CG][128 CG][4] (split): four columns of all rows after one another
   int64_t T, rows, cols, spitch;
   int tiles_m, tiles_n;
   bool n_first;   // consecutive tiles run along the inputs
@@ -80,6 +79,7 @@ struct WgradArgs {
   int rest;       // tiles of the last round
   int ranges;     // ranges of its tokens, 0 where they are not cut
   unsigned int* status;
+  bool wide;      // rows of the outputs are whole 32-byte sectors
   bool wait;
 };
 
@@ -165,10 +165,47 @@ struct Ring {
   }
 };
 
-// 32 columns of a row of the sums, from column n on: added to acc, and written out.
+// 32 bytes, one whole sector a lane (32-byte aligned).
+__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
+               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+__device__ __forceinline__ void load32(const void* p, float (&v)[8]) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "l"(p)
+               : "memory");
+}
+
+// 32 columns of a row of the sums, from column n on (a multiple of 32): added to acc, and
+// written out.  A lane has a row of its own, so it stores whole sectors where it can.
 __device__ __forceinline__ void store_sums(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
   const int64_t at = m * a.cols + n;
-  if (a.cols % 8 == 0) {
+  if (a.wide) {  // (columns come in sixteens)
+    if (a.acc != nullptr) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        if (n + 8 * q >= a.cols) break;
+        float x[8];
+        uint32_t w[8];
+        load32(a.acc + at + 8 * q, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += x[e]);
+        store32(a.acc + at + 8 * q, w);
+      }
+    }
+    if (a.dWm != nullptr) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        if (n + 16 * q >= a.cols) break;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
+        store32(a.dWm + at + 16 * q, w);
+      }
+    }
+  } else if (a.cols % 8 == 0) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (n + 8 * q >= a.cols) break;
@@ -249,19 +286,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     return q < kSlots || mbar_wait_ring_cluster(dy_empty + (q - kSlots) % kDyStages, ((q - kSlots) / kDyStages) & 1u, lim);
   };
   if (warp == 0) {
-    if (lane == 0) {
-      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-        tile_origin(a, w.tile, kEdge * CG, m0, n0);
-        const int m = int(m0) + int(rank) * kEdge;
-        for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
-          ok = mbar_wait_ring_cluster(dy_empty + ring.at, ring.pass ^ 1u, lim);
-          if (!ok) break;
-          uint8_t* st = smem + ring.at * kOperand;
-          uint64_t* bar = dy_full + ring.at;
+    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      const int m = int(m0) + int(rank) * kEdge;
+      for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
+        ok = mbar_wait_ring_cluster(dy_empty + ring.at, ring.pass ^ 1u, lim);
+        if (!ok) break;
+        uint8_t* st = smem + ring.at * kOperand;
+        uint64_t* bar = dy_full + ring.at;
+        if (elect_one()) {
           mbar_arrive_expect_tx(bar, kOperand);
           tma_load_2d(st, &tm_dy, m, c * kChunk, bar);
           tma_load_2d(st + kHalf, &tm_dy, m + 64, c * kChunk, bar);
         }
+        __syncwarp();
       }
     }
   } else if (warp == kWarpCodes) {
@@ -276,7 +314,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         ok = mbar_wait_ring(code_empty + code_ring.at, code_ring.pass ^ 1u, lim);
         if (!ok) break;
         uint64_t* bar = code_full + code_ring.at;
-        if (lane == 0) {
+        if (elect_one()) {
           mbar_arrive_expect_tx(bar, kCodes);
           tma_load_2d(smem + kOffCodes + code_ring.at * kCodes, &tm_codes, int(n), c * kChunk, bar);
         }
@@ -291,18 +329,17 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp == kWarpNotice) {
     // tells the thread that issues the MMAs, the pair's for both CTAs, that dY has landed
-    if (lane == 0) {
-      uint32_t q = 0;
-      for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-        for (int c = w.c0; c < w.c1; ++c, ++q, ring.next(), slot.next()) {
-          ok = mbar_wait_ring(dy_full + ring.at, ring.pass, lim) && slot_free(q);
-          if (!ok) break;
-          mbar_arrive_cluster(ready + slot.at, 0);
-        }
+    uint32_t q = 0;
+    for (int i = 0; ok && work_of(a, g, i, w); ++i) {
+      for (int c = w.c0; c < w.c1; ++c, ++q, ring.next(), slot.next()) {
+        ok = mbar_wait_ring(dy_full + ring.at, ring.pass, lim) && slot_free(q);
+        if (!ok) break;
+        if (elect_one()) mbar_arrive_cluster(ready + slot.at, 0);
+        __syncwarp();
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0) {
       const uint32_t idesc = tc_idesc_bf16_f32_mn(kEdge * CG, kEdge * CG);
       // descriptors of the first stage and slot; addresses count in units of 16 bytes
       const uint64_t dy0 = tc_smem_desc_mn128(smem_addr(smem), kHalf), x0 = tc_smem_desc_mn128(smem_addr(smem + kOffSlots), kHalf);
@@ -310,20 +347,20 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         const int b = i & 1;
         ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
         const uint32_t d = tmem + uint32_t(b) * (kEdge * CG);
-        bool add = false;
         for (int c = w.c0; ok && c < w.c1; ++c, ++committed, ring.next(), slot.next()) {
           ok = mbar_wait_ring_cluster(ready + slot.at, slot.pass, lim);
           if (!ok) break;
           tc_fence_after();
           const uint64_t dy = dy0 + uint32_t(ring.at) * (kOperand / 16), x = x0 + uint32_t(slot.at) * (kOperand / 16);
+          if (elect_one()) {
 #pragma unroll
-          for (int k = 0; k < kChunk / 16; ++k) {
-            tc_mma_bf16_group<CG>(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, add);
-            add = true;
+            for (int k = 0; k < kChunk / 16; ++k)
+              tc_mma_bf16_group<CG>(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, k > 0 || c > w.c0);
+            tc_commit_group<CG>(dy_empty + ring.at);
+            if (c == w.c1 - 1) tc_commit_group<CG>(sum + b);
           }
-          tc_commit_group<CG>(dy_empty + ring.at);
+          __syncwarp();
         }
-        if (ok) tc_commit_group<CG>(sum + b);
       }
     }
   } else if (warp < 2 + kConvertWarps * kSets) {
@@ -380,7 +417,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       tile_origin(a, w.tile, kEdge * CG, m0, n0);
       const int r = int(rank) * kEdge + quarter * 32 + lane;  // row of the tile
       const int64_t m = m0 + r;
-      float* part = a.part + (int64_t(w.slot) * (kEdge * CG) + r) * (kEdge * CG);
+      float4* part = reinterpret_cast<float4*>(a.part) + int64_t(w.slot) * (kEdge * CG) * (kEdge * CG / 4) + r;
       for (int q = 0; q < kEdge * CG / 32; ++q) {
         uint32_t u[32];
         tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * (kEdge * CG) + 32 * q), u);
@@ -388,7 +425,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
         input_order(u, v);
         if (w.slot >= 0) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(part + 32 * q + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          for (int e = 0; e < 32; e += 4) part[(8 * q + e / 4) * (kEdge * CG)] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         } else if (m < a.rows && n0 + 32 * q < a.cols) {
           store_sums(a, m, n0 + 32 * q, v);
         }
@@ -402,7 +439,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   __syncthreads();
   if (misc[1] == 0u) {
     // a wait gave up: the copies this CTA sent off land, and its MMAs end, before it leaves
-    if (warp == 0 && lane == 0) {
+    if (warp == 0) {
       for (int c = issued > kDyStages ? issued - kDyStages : 0; c < issued; ++c)
         mbar_wait_bounded(dy_full + c % kDyStages, uint32_t(c / kDyStages) & 1u);
     }
@@ -421,40 +458,63 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // The tiles of the last round whose tokens were cut: their partial sums in the order of the
-// ranges, four columns a thread.
+// ranges.  A CTA takes 32 rows of a tile: a lane reads four columns of its row (a warp 512
+// consecutive bytes), and the rows are written out through shared memory.
+constexpr int kJoinRows = 32;
 template <int CG>
 __global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
-  constexpr int kSide = kEdge * CG, kQuads = kSide / 4;
+  constexpr int kSide = kEdge * CG, kQuads = kSide / 4, kEach = kQuads / 8;
+  __shared__ float rows[kJoinRows][kSide + 4];
   pdl_begin(true);  // the partial sums of the launch before
-  const int64_t per_tile = int64_t(kSide) * kQuads;
-  const int64_t total = a.rest * per_tile;
-  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < total; i += int64_t(gridDim.x) * blockDim.x) {
-    const int tile = int(i / per_tile);
-    const int e = int(i - tile * per_tile), r = e / kQuads, c = e % kQuads * 4;
-    int64_t m0, n0;
-    tile_origin(a, a.rounds * a.groups + tile, kSide, m0, n0);
-    const int64_t m = m0 + r, n = n0 + c;
-    if (m >= a.rows || n >= a.cols) continue;
-    // the ranges that hold the tile's first and last chunk
-    const int64_t t0 = int64_t(tile) * a.chunks, t1 = t0 + a.chunks - 1;
-    int p0 = int(t0 * a.ranges / (int64_t(a.rest) * a.chunks)), p1 = int(t1 * a.ranges / (int64_t(a.rest) * a.chunks));
-    while (range_start(a, p0 + 1) <= t0) ++p0;
-    while (range_start(a, p1 + 1) <= t1) ++p1;
-    if (p0 == p1) continue;  // whole, and written already
-    float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    for (int p = p0; p <= p1; ++p) {
-      const int j = tile - int(range_start(a, p) / a.chunks);
-      const float4 v = __ldcs(reinterpret_cast<const float4*>(a.part + (int64_t(2 * p + j) * kSide + r) * kSide + c));
-      s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
-    }
-    const float v[4] = {s.x, s.y, s.z, s.w};
-    const int64_t at = m * a.cols + n;
+  const int tile = blockIdx.x / (kSide / kJoinRows), r0 = blockIdx.x % (kSide / kJoinRows) * kJoinRows;
+  int64_t m0, n0;
+  tile_origin(a, a.rounds * a.groups + tile, kSide, m0, n0);
+  m0 += r0;
+  if (m0 >= a.rows) return;
+  // the ranges that hold the tile's first and last chunk
+  const int64_t t0 = int64_t(tile) * a.chunks, t1 = t0 + a.chunks - 1;
+  int p0 = int(t0 * a.ranges / (int64_t(a.rest) * a.chunks)), p1 = int(t1 * a.ranges / (int64_t(a.rest) * a.chunks));
+  while (range_start(a, p0 + 1) <= t0) ++p0;
+  while (range_start(a, p1 + 1) <= t1) ++p1;
+  if (p0 == p1) return;  // whole, and written already
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float4 s[kEach];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (n + k >= a.cols) break;
-      float x = v[k];
-      if (a.acc != nullptr) a.acc[at + k] = x += a.acc[at + k];
-      if (a.dWm != nullptr) a.dWm[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+  for (int e = 0; e < kEach; ++e) s[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int p = p0; p <= p1; ++p) {
+    // (only the first range may have begun in the tile before)
+    const int j = p == p0 && range_start(a, p) < t0 ? 1 : 0;
+    const float4* from = reinterpret_cast<const float4*>(a.part) + int64_t(2 * p + j) * kSide * kQuads + r0 + lane;
+    float4 v[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) v[e] = __ldcs(from + (warp + 8 * e) * kSide);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s[e].x += v[e].x, s[e].y += v[e].y, s[e].z += v[e].z, s[e].w += v[e].w;
+  }
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) *reinterpret_cast<float4*>(&rows[lane][4 * (warp + 8 * e)]) = s[e];
+  __syncthreads();
+  const bool fours = a.cols % 4 == 0;
+  for (int i = threadIdx.x; i < kJoinRows * kQuads; i += 256) {
+    const int r = i / kQuads, c = i % kQuads * 4;
+    if (m0 + r >= a.rows || n0 + c >= a.cols) continue;
+    float v[4] = {rows[r][c], rows[r][c + 1], rows[r][c + 2], rows[r][c + 3]};
+    const int64_t at = (m0 + r) * a.cols + n0 + c;
+    if (fours) {
+      if (a.acc != nullptr) {
+        float4* q = reinterpret_cast<float4*>(a.acc + at);
+        const float4 x = *q;
+        v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+        *q = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      if (a.dWm != nullptr) *reinterpret_cast<uint2*>(a.dWm + at) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (n0 + c + k >= a.cols) break;
+        if (a.acc != nullptr) a.acc[at + k] = v[k] += a.acc[at + k];
+        if (a.dWm != nullptr) a.dWm[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(v[k]));
+      }
     }
   }
 }
@@ -551,6 +611,7 @@ int launch_wgrad(const WgradCall& c) {
   a.part = reinterpret_cast<float*>(ws);
   a.spitch = block8_scale_pitch(c.cols);
   a.status = c.status;
+  a.wide = c.cols % 16 == 0 && ((reinterpret_cast<uintptr_t>(c.dWm) | reinterpret_cast<uintptr_t>(c.acc)) & 31u) == 0;
   a.wait = wait;
   CUtensorMap tm_dy, tm_codes;
   const int64_t pitch = block8_pitch(c.cols);
@@ -572,9 +633,7 @@ int launch_wgrad(const WgradCall& c) {
   if (launch_maybe_pdl(kern, int(busy) * kGroup, kThreads, smem, c.stream, wait, tm_dy, tm_codes, a) < 0) return -1;
   ++launched;
   if (a.ranges > 0) {
-    const int64_t quads = int64_t(a.rest) * kEdge * kGroup * kEdge * kGroup / 4, cap = int64_t(sm_count()) * 8;
-    const int64_t blocks = (quads + 255) / 256;
-    if (launch_maybe_pdl(roi_wgrad_join_kernel<kGroup>, int(blocks < cap ? blocks : cap), 256, 0, c.stream, true, a) < 0) return -1;
+    if (launch_maybe_pdl(roi_wgrad_join_kernel<kGroup>, a.rest * (kEdge * kGroup / kJoinRows), 256, 0, c.stream, true, a) < 0) return -1;
     ++launched;
   }
   return launched;
