@@ -480,26 +480,32 @@ def roi_hard_mask_export(logits, N, M, out_bits, W=None, out_Wpruned=None, strea
 NORM_KINDS = {"layer": 0, "rms": 1}
 
 
-def _dtype(t, name):
-    import torch
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(t.dtype)
+_TYPES = {}  # torch type -> roi_dtype, of the types that the calls take
+
+
+def _type(t, name):
+    code = _TYPES.get(t.dtype)
     if code is None:
-        raise TypeError(f"{name}: expected bfloat16, float16 or float32, got {t.dtype}")
+        import torch
+        _TYPES.update({torch.bfloat16: 0, torch.float16: 1, torch.float32: 2})
+        code = _TYPES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"{name}: expected bfloat16, float16 or float32, got {t.dtype}")
     return code
 
 
-def _matrix(t, name, dtype=None, shape=None):
-    """Checks a matrix whose rows may be apart; returns its row stride in elements."""
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+def _stride(t, name, shape=None):
+    """Row stride, in elements, of a CUDA matrix whose rows may be apart."""
     if not t.is_cuda:
         raise ValueError(f"{name}: expected a CUDA tensor")
-    if t.dim() != 2 or (shape is not None and tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{name}: expected {'a matrix' if shape is None else f'shape {tuple(shape)}'}, got {tuple(t.shape)}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    have = t.shape
+    if len(have) != 2 or (shape is not None and have != shape):
+        raise ValueError(f"{name}: expected {'a matrix' if shape is None else f'shape {tuple(shape)}'}, got {tuple(have)}")
+    if t.is_contiguous() or have[0] <= 1 and (have[1] <= 1 or t.stride(1) == 1):
+        return have[1]  # (the stride of a single row says nothing)
+    if have[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    # the stride of a single row says nothing
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    return t.stride(0)
 
 
 def roi_checkpoint_pitch(cols) -> int:
@@ -519,49 +525,51 @@ def new_checkpoint(rows, cols, device="cuda"):
             torch.empty(rows, roi_checkpoint_scale_pitch(cols), dtype=torch.uint8, device=device))
 
 
-def _checkpoint(codes, scales, name, rows, cols):
+def _checkpoint(pair, name, rows, cols):
+    """Addresses of a checkpoint's codes and scales (of a matrix [rows, cols]; None: none)."""
     import torch
-    if (codes is None) != (scales is None):
+    if pair is None:
+        return None, None
+    codes, scales = pair
+    if codes is None or scales is None:
         raise ValueError(f"{name}: codes and scales go together")
-    _check_tensor(codes, f"{name} codes", torch.int8, (rows, roi_checkpoint_pitch(cols)))
-    _check_tensor(scales, f"{name} scales", torch.uint8, (rows, roi_checkpoint_scale_pitch(cols)))
+    _check_tensor(codes, f"{name} codes", torch.int8, (rows, (cols + 31) // 32 * 32))
+    _check_tensor(scales, f"{name} scales", torch.uint8, (rows, (cols + 127) // 128 * 4))
+    return codes.data_ptr(), scales.data_ptr()
 
 
 def roi_checkpoint_save(x, out_codes, out_scales, stream=None):
     """Saves x [rows, cols] (bfloat16, float16 or float32; rows may be apart) in 8 bits."""
+    ld = _stride(x, "x")
     rows, cols = x.shape
-    ld = _matrix(x, "x")
-    _checkpoint(out_codes, out_scales, "out", rows, cols)
-    s = lib().roi_checkpoint_save(_ptr(x), _dtype(x, "x"), rows, cols, ld, _ptr(out_codes), _ptr(out_scales),
-                                  _stream(stream))
+    codes, scales = _checkpoint((out_codes, out_scales), "out", rows, cols)
+    s = lib().roi_checkpoint_save(x.data_ptr(), _type(x, "x"), rows, cols, ld, codes, scales, _stream(stream))
     _raise(s, "roi_checkpoint_save")
 
 
 def roi_checkpoint_load(codes, scales, out_x, stream=None):
     """The values a checkpoint stands for, in the type of out_x [rows, cols]."""
+    ld = _stride(out_x, "out_x")
     rows, cols = out_x.shape
-    ld = _matrix(out_x, "out_x")
-    _checkpoint(codes, scales, "checkpoint", rows, cols)
-    s = lib().roi_checkpoint_load(_ptr(codes), _ptr(scales), _dtype(out_x, "out_x"), rows, cols, _ptr(out_x), ld,
-                                  _stream(stream))
+    codes, scales = _checkpoint((codes, scales), "checkpoint", rows, cols)
+    s = lib().roi_checkpoint_load(codes, scales, _type(out_x, "out_x"), rows, cols, out_x.data_ptr(), ld, _stream(stream))
     _raise(s, "roi_checkpoint_load")
 
 
 def _norm_kind(kind):
-    if kind not in NORM_KINDS:
+    code = NORM_KINDS.get(kind)
+    if code is None:
         raise ValueError(f"kind: expected one of {sorted(NORM_KINDS)}, got {kind!r}")
-    return NORM_KINDS[kind]
+    return code
 
 
-def _param_dtype(x, *params):
-    """The type code of gamma and beta (that of x, or float32; one for both)."""
-    import torch
-    given = [(name, p) for name, p in params if p is not None]
-    for name, p in given:
-        if p.dtype not in (x.dtype, torch.float32) or p.dtype != given[0][1].dtype:
-            raise TypeError(f"{name}: expected {x.dtype} or torch.float32, one type for all, got {p.dtype}")
-        _check_tensor(p, name, p.dtype, (x.shape[1],))
-    return _dtype(given[0][1], given[0][0]) if given else _dtype(x, "x")
+def _param(t, name, like, cols, other=None):
+    """Type code of a norm's weight or bias: the type of `like`, or float32; that of `other`, if given."""
+    code = _type(t, name)
+    if (code != 2 and t.dtype != like.dtype) or (other is not None and t.dtype != other.dtype):
+        raise TypeError(f"{name}: expected {like.dtype} or torch.float32, one type for all, got {t.dtype}")
+    _check_tensor(t, name, t.dtype, (cols,))
+    return code
 
 
 def roi_norm_fwd(x, kind, gamma, beta, eps, out_y, out_mean=None, out_rstd=None, x_checkpoint=None, y_checkpoint=None,
@@ -569,18 +577,25 @@ def roi_norm_fwd(x, kind, gamma, beta, eps, out_y, out_mean=None, out_rstd=None,
     """Layer norm ("layer") or RMS norm ("rms") of the rows of x; the checkpoints of x and of
     out_y ((codes, scales) pairs) are written in the same pass where given."""
     import torch
-    rows, cols = x.shape
-    ldx, ldy = _matrix(x, "x"), _matrix(out_y, "out_y", x.dtype, x.shape)
-    p = _param_dtype(x, ("gamma", gamma), ("beta", beta))
-    _check_tensor(out_mean, "out_mean", torch.float32, (rows,))
-    _check_tensor(out_rstd, "out_rstd", torch.float32, (rows,))
-    xq, xs = x_checkpoint if x_checkpoint is not None else (None, None)
-    yq, ys = y_checkpoint if y_checkpoint is not None else (None, None)
-    _checkpoint(xq, xs, "x_checkpoint", rows, cols)
-    _checkpoint(yq, ys, "y_checkpoint", rows, cols)
-    s = lib().roi_norm_fwd(_ptr(x), _dtype(x, "x"), rows, cols, ldx, _norm_kind(kind), _ptr(gamma), _ptr(beta), p,
-                           float(eps), _ptr(out_y), ldy, _ptr(out_mean), _ptr(out_rstd), _ptr(xq), _ptr(xs), _ptr(yq),
-                           _ptr(ys), _stream(stream))
+    ldx = _stride(x, "x")
+    dtype = param = _type(x, "x")
+    shape = x.shape
+    rows, cols = shape
+    ldy = _stride(out_y, "out_y", shape)
+    if out_y.dtype is not x.dtype:
+        raise TypeError(f"out_y: expected {x.dtype}, got {out_y.dtype}")
+    if gamma is not None:
+        param = _param(gamma, "gamma", x, cols)
+    if beta is not None:
+        param = _param(beta, "beta", x, cols, gamma)
+    if out_mean is not None:
+        _check_tensor(out_mean, "out_mean", torch.float32, (rows,))
+    if out_rstd is not None:
+        _check_tensor(out_rstd, "out_rstd", torch.float32, (rows,))
+    xq, xs = _checkpoint(x_checkpoint, "x_checkpoint", rows, cols)
+    yq, ys = _checkpoint(y_checkpoint, "y_checkpoint", rows, cols)
+    s = lib().roi_norm_fwd(x.data_ptr(), dtype, rows, cols, ldx, _norm_kind(kind), _ptr(gamma), _ptr(beta), param, eps,
+                           out_y.data_ptr(), ldy, _ptr(out_mean), _ptr(out_rstd), xq, xs, yq, ys, _stream(stream))
     _raise(s, "roi_norm_fwd")
 
 
@@ -594,32 +609,43 @@ def _workspace(workspace):
     if workspace is None:
         return None, 0
     _check_tensor(workspace, "workspace", workspace.dtype)
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def roi_norm_bwd(dy, x, kind, gamma, mean, rstd, out_dx, out_dgamma=None, out_dbeta=None, workspace=None, stream=None):
     """Backward of roi_norm_fwd.  x: the forward's input, or its checkpoint, a (codes, scales) pair.
     out_dgamma, out_dbeta: float32 [cols], overwritten."""
     import torch
-    rows, cols = dy.shape
-    lddy, lddx = _matrix(dy, "dy"), _matrix(out_dx, "out_dx", dy.dtype, dy.shape)
-    codes = scales = None
+    lddy = _stride(dy, "dy")
+    dtype = param = _type(dy, "dy")
+    shape = dy.shape
+    rows, cols = shape
+    lddx = _stride(out_dx, "out_dx", shape)
+    x_ptr = codes = scales = None
     ldx = cols
     if isinstance(x, (tuple, list)):
-        codes, scales = x
-        x = None
-        _checkpoint(codes, scales, "x", rows, cols)
+        codes, scales = _checkpoint(x, "x", rows, cols)
     else:
-        ldx = _matrix(x, "x", dy.dtype, dy.shape)
-    p = _param_dtype(dy, ("gamma", gamma))
-    _check_tensor(mean, "mean", torch.float32, (rows,))
-    _check_tensor(rstd, "rstd", torch.float32, (rows,))
-    _check_tensor(out_dgamma, "out_dgamma", torch.float32, (cols,))
-    _check_tensor(out_dbeta, "out_dbeta", torch.float32, (cols,))
+        ldx = _stride(x, "x", shape)
+        if x.dtype is not dy.dtype:
+            raise TypeError(f"x: expected {dy.dtype}, got {x.dtype}")
+        x_ptr = x.data_ptr()
+    if out_dx.dtype is not dy.dtype:
+        raise TypeError(f"out_dx: expected {dy.dtype}, got {out_dx.dtype}")
+    if gamma is not None:
+        param = _param(gamma, "gamma", dy, cols)
+    f32 = torch.float32
+    if mean is not None:
+        _check_tensor(mean, "mean", f32, (rows,))
+    _check_tensor(rstd, "rstd", f32, (rows,))
+    if out_dgamma is not None:
+        _check_tensor(out_dgamma, "out_dgamma", f32, (cols,))
+    if out_dbeta is not None:
+        _check_tensor(out_dbeta, "out_dbeta", f32, (cols,))
     ws, ws_bytes = _workspace(workspace)
-    s = lib().roi_norm_bwd(_ptr(dy), _dtype(dy, "dy"), rows, cols, lddy, _ptr(x), ldx, _ptr(codes), _ptr(scales),
-                           _norm_kind(kind), _ptr(gamma), p, _ptr(mean), _ptr(rstd), _ptr(out_dx), lddx,
-                           _ptr(out_dgamma), _ptr(out_dbeta), ws, ws_bytes, _stream(stream))
+    s = lib().roi_norm_bwd(dy.data_ptr(), dtype, rows, cols, lddy, x_ptr, ldx, codes, scales, _norm_kind(kind),
+                           _ptr(gamma), param, _ptr(mean), _ptr(rstd), out_dx.data_ptr(), lddx, _ptr(out_dgamma),
+                           _ptr(out_dbeta), ws, ws_bytes, _stream(stream))
     _raise(s, "roi_norm_bwd")
 
 
@@ -634,19 +660,22 @@ def roi_masked_linear_wgrad(dY, x_checkpoint, out_dWm=None, acc=None, workspace=
     """out_dWm[rows, cols] = bf16(dY[T, rows]^T x[T, cols] + acc), x the values of the (codes, scales)
     pair x_checkpoint; acc (float32), where given, is updated in place."""
     import torch
+    lddy = _stride(dY, "dY")
     T, rows = dY.shape
-    shape = next((t.shape for t in (out_dWm, acc) if t is not None), None)
-    if shape is None or len(shape) != 2:
+    if dY.dtype is not torch.bfloat16:
+        raise TypeError(f"dY: expected torch.bfloat16, got {dY.dtype}")
+    out = out_dWm if out_dWm is not None else acc
+    if out is None or out.dim() != 2:
         raise ValueError("out_dWm or acc: a matrix is required")
-    cols = shape[1]
-    lddy = _matrix(dY, "dY", torch.bfloat16)
-    codes, scales = x_checkpoint
-    _checkpoint(codes, scales, "x_checkpoint", T, cols)
-    _check_tensor(out_dWm, "out_dWm", torch.bfloat16, (rows, cols))
-    _check_tensor(acc, "acc", torch.float32, (rows, cols))
+    cols = out.shape[1]
+    codes, scales = _checkpoint(x_checkpoint, "x_checkpoint", T, cols)
+    if out_dWm is not None:
+        _check_tensor(out_dWm, "out_dWm", torch.bfloat16, (rows, cols))
+    if acc is not None:
+        _check_tensor(acc, "acc", torch.float32, (rows, cols))
     ws, ws_bytes = _workspace(workspace)
-    s = lib().roi_masked_linear_wgrad(_ptr(dY), lddy, _ptr(codes), _ptr(scales), T, rows, cols, _ptr(out_dWm), _ptr(acc),
-                                      ws, ws_bytes, _stream(stream))
+    s = lib().roi_masked_linear_wgrad(dY.data_ptr(), lddy, codes, scales, T, rows, cols, _ptr(out_dWm), _ptr(acc), ws,
+                                      ws_bytes, _stream(stream))
     _raise(s, "roi_masked_linear_wgrad")
 
 

@@ -60,7 +60,8 @@ constexpr int kUnits = 8 / kConvertWarps;        // blocks of 32 codes a thread 
 constexpr int kWarpCodes = 2 + kConvertWarps * kSets, kWarpNotice = kWarpCodes + 1;
 constexpr int kThreads = 32 * (kWarpNotice + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
-constexpr uint32_t kSmem = kOffBars + 256;
+constexpr int kBars = 2 * kCodeStages + 2 * kDyStages + kSlots + 2 + 2;
+constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 16;  // from a 1024-byte boundary on
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
 // partial sums is written and read again.
 constexpr int kMinRange = 8, kSplitCost = 8;
@@ -242,7 +243,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
   uint64_t *code_full = bars, *code_empty = code_full + kCodeStages, *dy_full = code_empty + kCodeStages, *dy_empty = dy_full + kDyStages;
   uint64_t *ready = dy_empty + kDyStages, *sum = ready + kSlots, *free = sum + 2;
-  uint32_t* misc = reinterpret_cast<uint32_t*>(free + 2);  // [0] TMEM base, [1] ok
+  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 1 ? 0u : cluster_rank();
   const int g = blockIdx.x / CG;
