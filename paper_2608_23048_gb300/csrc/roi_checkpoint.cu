@@ -1,20 +1,20 @@
 // Activation checkpoints in 8 bits (the layout is in roi_block8.cuh): save and load.
 //
-// Bound by memory: a save reads b bytes an element and writes 33/32, a load the reverse.
-// Vector kernels: a thread takes 16 consecutive columns (two or four 16-byte loads, one
-// 16-byte store of codes), so a block is two neighbouring lanes, whose largest magnitudes
-// meet in one shuffle; kUnits such pieces are loaded before the first is used.  Rows whose
-// start or stride is not a multiple of 16 bytes go to the element kernels, where a warp
-// takes a block, a lane a column.
+// Bound by memory: a save reads b bytes an element and writes 33/32, a load the reverse.  A
+// thread takes 16 consecutive columns (one 16-byte access of codes), so a block is two
+// neighbouring lanes, whose largest magnitudes meet in one shuffle; kUnits such pieces are
+// loaded before the first is used.  Where rows are whole 32-byte sectors apart, the pieces of
+// all rows follow one another and every access is whole sectors; elsewhere a warp, or a part of
+// one, has a row of its own and goes by granules (roi_rows.cuh).
 #include "roi_block8.cuh"
 #include "roi_launch.h"
+#include "roi_rows.cuh"
 
 namespace roi {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnits = 2;        // pieces of 16 columns a thread has in flight
-constexpr int kBlocksAWarp = 8;  // element kernels: blocks a warp has in flight
 
 struct SaveArgs {
   const void* x;
@@ -23,6 +23,7 @@ struct SaveArgs {
   int64_t rows, cols, ld;
   int64_t pitch, spitch;
   int64_t pieces;  // of 16 columns in a row, the scales' padding included
+  int width, segments;  // rows anywhere: lanes of a row, and how often they go over it
   bool wait;
 };
 
@@ -33,6 +34,7 @@ struct LoadArgs {
   int64_t rows, cols, ld;
   int64_t pitch, spitch;
   int64_t pieces;  // of 16 columns in a row
+  int width, segments;
   bool wait;
 };
 
@@ -53,90 +55,63 @@ __device__ __forceinline__ void walk(int64_t row0, int64_t rem0, uint32_t i, int
   }
 }
 
+// Codes and scale of the piece whose values are v (all lanes of the warp); `q` is its place in the row.
+__device__ __forceinline__ void save_piece(const SaveArgs& a, const float (&v)[16], int64_t row, int64_t q) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) top = max(top, abs_bits(v[i]));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  const uint32_t s = block8_scale(top);
+  const float inverse = block8_inverse(min(s, kScaleMax));
+  const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
+  if (row < a.rows && q < a.pieces) {
+    if (16 * q < a.pitch)
+      *reinterpret_cast<uint4*>(a.codes + row * a.pitch + 16 * q) =
+          make_uint4(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep), block8_codes4(v + 8, inverse, keep),
+                     block8_codes4(v + 12, inverse, keep));
+    if ((q & 1) == 0) a.scales[row * a.spitch + (q >> 1)] = uint8_t(s);
+  }
+}
+template <Elem E>
+__device__ __forceinline__ void load_piece(const uint4& q, uint32_t s, RowWords<E, 16>& r) {
+  const float step = block8_step(s);
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  float v[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = block8_clip<E>(block8_value(w[i / 4], i % 4, step));
+  r.set(v);
+}
+
 template <Elem E>
 __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_kernel(SaveArgs a) {
   using T = typename ElemType<E>::T;
+  constexpr int kWords = RowWords<E, 16>::kWords;
   pdl_begin(a.wait);
   const T* x = static_cast<const T*>(a.x);
   const int64_t total = a.rows * a.pieces;
   constexpr int kTile = kThreads * kUnits;
   for (int64_t base = int64_t(blockIdx.x) * kTile; base < total; base += int64_t(gridDim.x) * kTile) {
     const int64_t row0 = base / a.pieces, rem0 = base - row0 * a.pieces;
-    Raw8<E> r[kUnits][2];
+    RowWords<E, 16> r[kUnits];
     int64_t row[kUnits], j[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       walk(row0, rem0, uint32_t(u * kThreads) + threadIdx.x, a.pieces, row[u], j[u]);
       const T* p = x + row[u] * a.ld + 16 * j[u];
+      if (row[u] < a.rows && a.cols - 16 * j[u] >= 16) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int64_t left = a.cols - 16 * j[u] - 8 * h;
-        if (row[u] < a.rows && left >= 8) {
-          r[u][h].load(p + 8 * h);
-        } else if (row[u] < a.rows && left > 0) {
-          float v[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) v[i] = i < left ? to_f32<E>(p[8 * h + i]) : 0.0f;
-          r[u][h].set(v);
-        } else {
-          r[u][h].zero();
-        }
+        for (int i = 0; i < kWords / 8; ++i) load32(reinterpret_cast<const uint4*>(p) + 2 * i, r[u].u + 8 * i);
+      } else if (row[u] < a.rows) {
+        r[u].load_elements(x + row[u] * a.ld, 16 * j[u], a.cols);
+      } else {
+        r[u].zero();
       }
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       float v[16];
-      {
-        float lo[8], hi[8];
-        r[u][0].get(lo), r[u][1].get(hi);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = lo[i], v[8 + i] = hi[i];
-      }
-      uint32_t top = 0;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = max(top, abs_bits(v[i]));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      const uint32_t s = block8_scale(top);
-      const float inverse = block8_inverse(min(s, kScaleMax));
-      const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
-      if (row[u] < a.rows) {
-        if (16 * j[u] < a.pitch)
-          *reinterpret_cast<uint4*>(a.codes + row[u] * a.pitch + 16 * j[u]) =
-              make_uint4(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep),
-                         block8_codes4(v + 8, inverse, keep), block8_codes4(v + 12, inverse, keep));
-        if ((j[u] & 1) == 0) a.scales[row[u] * a.spitch + (j[u] >> 1)] = uint8_t(s);
-      }
-    }
-  }
-}
-
-// A warp a block of 32 columns, a lane a column (`pieces`: blocks in a row here).
-template <Elem E>
-__global__ void __launch_bounds__(kThreads) roi_checkpoint_save_elem_kernel(SaveArgs a) {
-  using T = typename ElemType<E>::T;
-  pdl_begin(a.wait);
-  const T* x = static_cast<const T*>(a.x);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t total = a.rows * a.pieces;
-  constexpr int kTile = kThreads / 32 * kBlocksAWarp;
-  for (int64_t base = int64_t(blockIdx.x) * kTile; base < total; base += int64_t(gridDim.x) * kTile) {
-    const int64_t row0 = base / a.pieces, rem0 = base - row0 * a.pieces;
-    float v[kBlocksAWarp];
-    int64_t row[kBlocksAWarp], b[kBlocksAWarp];
-#pragma unroll
-    for (int u = 0; u < kBlocksAWarp; ++u) {
-      walk(row0, rem0, uint32_t(warp * kBlocksAWarp + u), a.pieces, row[u], b[u]);
-      const int64_t c = 32 * b[u] + lane;
-      v[u] = row[u] < a.rows && c < a.cols ? to_f32<E>(x[row[u] * a.ld + c]) : 0.0f;
-    }
-#pragma unroll
-    for (int u = 0; u < kBlocksAWarp; ++u) {
-      const uint32_t s = block8_scale(__reduce_max_sync(0xffffffffu, abs_bits(v[u])));
-      const uint32_t q = block8_code(v[u], block8_inverse(min(s, kScaleMax)));
-      if (row[u] < a.rows) {
-        if (32 * b[u] < a.pitch) a.codes[row[u] * a.pitch + 32 * b[u] + lane] = s == kScaleNaN ? int8_t(0) : int8_t(q);
-        if (lane == 0) a.scales[row[u] * a.spitch + b[u]] = uint8_t(s);
-      }
+      r[u].get(v);
+      save_piece(a, v, row[u], j[u]);
     }
   }
 }
@@ -144,6 +119,7 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_elem_kernel(Save
 template <Elem E>
 __global__ void __launch_bounds__(kThreads) roi_checkpoint_load_kernel(LoadArgs a) {
   using T = typename ElemType<E>::T;
+  constexpr int kWords = RowWords<E, 16>::kWords;
   pdl_begin(a.wait);
   T* x = static_cast<T*>(a.x);
   const int64_t total = a.rows * a.pieces;
@@ -165,56 +141,84 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_load_kernel(LoadArgs 
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       if (row[u] >= a.rows) continue;
-      const float step = block8_step(s[u]);
+      RowWords<E, 16> r;
+      load_piece<E>(q[u], s[u], r);
       T* p = x + row[u] * a.ld + 16 * j[u];
-      const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+      const int64_t left = a.cols - 16 * j[u];
+      if (left >= 16) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float v[8];
+        for (int i = 0; i < kWords / 8; ++i) store32(reinterpret_cast<uint4*>(p) + 2 * i, r.u + 8 * i);
+      } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = block8_clip<E>(block8_value(w[2 * h + i / 4], i % 4, step));
-        const int64_t left = a.cols - 16 * j[u] - 8 * h;
-        if (left >= 8) {
-          Raw8<E> r;
-          r.set(v);
-          r.store(p + 8 * h);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < left) p[8 * h + i] = from_f32<E>(v[i]);
-        }
+        for (int i = 0; i < 16; ++i)
+          if (i < left) p[i] = r.at(i);
       }
     }
   }
 }
 
+// Rows anywhere.  A warp's task: 32 / width rows, or one segment of a row.
+__device__ __forceinline__ void row_task(int64_t task, int width, int segments, int64_t& row, int64_t& piece) {
+  const int lane = threadIdx.x & 31;
+  if (segments > 1) {
+    row = task / segments;
+    piece = (task - row * segments) * 32 + lane;
+  } else {
+    row = task * (32 / width) + lane / width;
+    piece = lane & (width - 1);
+  }
+}
+
 template <Elem E>
-__global__ void __launch_bounds__(kThreads) roi_checkpoint_load_elem_kernel(LoadArgs a) {
+__global__ void __launch_bounds__(kThreads) roi_checkpoint_save_rows_kernel(SaveArgs a) {
   using T = typename ElemType<E>::T;
   pdl_begin(a.wait);
-  T* x = static_cast<T*>(a.x);
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t total = a.rows * a.pieces;
-  constexpr int kTile = kThreads / 32 * kBlocksAWarp;
-  for (int64_t base = int64_t(blockIdx.x) * kTile; base < total; base += int64_t(gridDim.x) * kTile) {
-    const int64_t row0 = base / a.pieces, rem0 = base - row0 * a.pieces;
-    int8_t q[kBlocksAWarp];
-    uint8_t s[kBlocksAWarp];
-    int64_t row[kBlocksAWarp], b[kBlocksAWarp];
+  const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
+  const int64_t stride = int64_t(gridDim.x) * (kThreads / 32) * kUnits;
+  for (int64_t t = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits; t < tasks; t += stride) {
+    Window<E, 16, false> x[kUnits];
+    int64_t row[kUnits], j[kUnits];
 #pragma unroll
-    for (int u = 0; u < kBlocksAWarp; ++u) {
-      walk(row0, rem0, uint32_t(warp * kBlocksAWarp + u), a.pieces, row[u], b[u]);
-      q[u] = 0, s[u] = 0;
-      if (row[u] < a.rows) {
-        q[u] = a.codes[row[u] * a.pitch + 32 * b[u] + lane];
-        s[u] = a.scales[row[u] * a.spitch + b[u]];
+    for (int u = 0; u < kUnits; ++u) {
+      row_task(t + u, a.width, a.segments, row[u], j[u]);
+      x[u].load(static_cast<const T*>(a.x) + row[u] * a.ld, 16 * j[u], row[u] < a.rows ? a.cols : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      RowWords<E, 16> r;
+      float v[16];
+      x[u].get(r);
+      r.get(v);
+      save_piece(a, v, row[u], j[u]);
+    }
+  }
+}
+
+template <Elem E>
+__global__ void __launch_bounds__(kThreads) roi_checkpoint_load_rows_kernel(LoadArgs a) {
+  using T = typename ElemType<E>::T;
+  pdl_begin(a.wait);
+  const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
+  const int64_t stride = int64_t(gridDim.x) * (kThreads / 32) * kUnits;
+  for (int64_t t = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits; t < tasks; t += stride) {
+    uint4 q[kUnits];
+    uint32_t s[kUnits];
+    int64_t row[kUnits], j[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      row_task(t + u, a.width, a.segments, row[u], j[u]);
+      q[u] = make_uint4(0, 0, 0, 0), s[u] = 0;
+      if (row[u] < a.rows && j[u] < a.pieces) {
+        q[u] = __ldg(reinterpret_cast<const uint4*>(a.codes + row[u] * a.pitch + 16 * j[u]));
+        s[u] = __ldg(a.scales + row[u] * a.spitch + (j[u] >> 1));
       }
     }
 #pragma unroll
-    for (int u = 0; u < kBlocksAWarp; ++u) {
-      const int64_t c = 32 * b[u] + lane;
-      if (row[u] < a.rows && c < a.cols)
-        x[row[u] * a.ld + c] = from_f32<E>(block8_clip<E>(float(q[u]) * block8_step(s[u])));
+    for (int u = 0; u < kUnits; ++u) {
+      RowWords<E, 16> r;
+      load_piece<E>(q[u], s[u], r);
+      const int64_t none = -(int64_t(1) << 40);
+      store_row<E, 16, false>(static_cast<T*>(a.x) + row[u] * a.ld, 16 * j[u], row[u] < a.rows ? a.cols : none, r, a.width);
     }
   }
 }
@@ -227,17 +231,28 @@ int launch(void (*kern)(Args), const Args& a, int64_t total, int tile, cudaStrea
   return launch_maybe_pdl(kern, int(grid), kThreads, 0, stream, a.wait, a);
 }
 
-bool rows_aligned(const void* p, int64_t ld, int64_t rows, int bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * bytes % 16 == 0);
+// Rows that are whole 32-byte sectors apart.
+bool in_sectors(const void* p, int64_t ld, int64_t rows, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & 31u) == 0 && (rows <= 1 || ld * bytes % 32 == 0);
+}
+// Rows anywhere: the lanes of a row, a power of two that holds its pieces, or a whole warp that
+// goes over it in segments.  Returns the tiles of the launch.
+template <class Args>
+int64_t by_rows(Args& a) {
+  a.width = 1;
+  while (a.width < 32 && a.width < a.pieces) a.width *= 2;
+  a.segments = int((a.pieces + 31) / 32);
+  const int64_t per = 32 / a.width;
+  return (a.rows + per - 1) / per * a.segments;
 }
 
 template <Elem E>
 int save(const CheckpointCall& c) {
-  SaveArgs a{c.x_in, c.codes, c.scales, c.rows, c.cols, c.ld, block8_pitch(c.cols), block8_scale_pitch(c.cols), 0,
+  SaveArgs a{c.x_in, c.codes, c.scales, c.rows, c.cols, c.ld, block8_pitch(c.cols), block8_scale_pitch(c.cols), 0, 0, 0,
              lone_pdl(c.stream)};
-  if (!rows_aligned(c.x_in, c.ld, c.rows, elem_bytes<E>())) {
-    a.pieces = a.spitch;
-    return launch(roi_checkpoint_save_elem_kernel<E>, a, a.rows * a.pieces, kThreads / 32 * kBlocksAWarp, c.stream);
+  if (!in_sectors(c.x_in, c.ld, c.rows, elem_bytes<E>())) {
+    a.pieces = a.spitch * 2;
+    return launch(roi_checkpoint_save_rows_kernel<E>, a, by_rows(a), kThreads / 32 * kUnits, c.stream);
   }
   if (a.ld == a.cols && a.cols % 128 == 0) {  // the rows follow one another in every array: one long row
     a.cols *= a.rows, a.pitch *= a.rows, a.spitch *= a.rows, a.ld = a.cols, a.rows = 1;
@@ -248,16 +263,15 @@ int save(const CheckpointCall& c) {
 
 template <Elem E>
 int load(const CheckpointCall& c) {
-  LoadArgs a{c.codes, c.scales, c.x_out, c.rows, c.cols, c.ld, block8_pitch(c.cols), block8_scale_pitch(c.cols), 0,
+  LoadArgs a{c.codes, c.scales, c.x_out, c.rows, c.cols, c.ld, block8_pitch(c.cols), block8_scale_pitch(c.cols), 0, 0, 0,
              lone_pdl(c.stream)};
-  if (!rows_aligned(c.x_out, c.ld, c.rows, elem_bytes<E>())) {
-    a.pieces = a.pitch / 32;
-    return launch(roi_checkpoint_load_elem_kernel<E>, a, a.rows * a.pieces, kThreads / 32 * kBlocksAWarp, c.stream);
-  }
+  a.pieces = (a.cols + 15) / 16;
+  if (!in_sectors(c.x_out, c.ld, c.rows, elem_bytes<E>()))
+    return launch(roi_checkpoint_load_rows_kernel<E>, a, by_rows(a), kThreads / 32 * kUnits, c.stream);
   if (a.ld == a.cols && a.cols % 128 == 0) {
     a.cols *= a.rows, a.pitch *= a.rows, a.spitch *= a.rows, a.ld = a.cols, a.rows = 1;
+    a.pieces = a.cols / 16;
   }
-  a.pieces = (a.cols + 15) / 16;
   return launch(roi_checkpoint_load_kernel<E>, a, a.rows * a.pieces, kThreads * kUnits, c.stream);
 }
 
