@@ -741,6 +741,9 @@ roi_status roi_checkpoint_load(const int8_t* codes, const uint8_t* scales, int d
                          stream);
 }
 
+// The norms count the columns of a row in 32 bits.
+static constexpr int64_t kNormCols = int64_t(1) << 30;
+
 roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int kind, const void* gamma,
                         const void* beta, int param_dtype, float eps, void* out_y, int64_t ldy, float* out_mean,
                         float* out_rstd, int8_t* out_xcodes, uint8_t* out_xscales, int8_t* out_ycodes,
@@ -749,7 +752,7 @@ roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, in
   if (!known_type(dtype) || (param_dtype != dtype && param_dtype != ROI_FP32) || (!layer && kind != ROI_RMS_NORM) ||
       !std::isfinite(eps) || eps < 0.0f || (!layer && (beta != nullptr || out_mean != nullptr)))
     return ROI_ERR_TYPE;
-  if (!good_shape(rows, cols, ldx) || !good_shape(rows, cols, ldy)) return ROI_ERR_SHAPE;
+  if (!good_shape(rows, cols, ldx) || !good_shape(rows, cols, ldy) || cols > kNormCols) return ROI_ERR_SHAPE;
   if (rows == 0) return ROI_OK;
   if (x == nullptr || out_y == nullptr || (out_xcodes == nullptr) != (out_xscales == nullptr) ||
       (out_ycodes == nullptr) != (out_yscales == nullptr))
@@ -783,6 +786,8 @@ roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, in
   c.cols = cols;
   c.ldx = ldx;
   c.ldy = ldy;
+  c.status = status_word();
+  if (c.status == nullptr) return ROI_ERR_CUDA;
   c.stream = static_cast<cudaStream_t>(stream);
   return finish(launch_norm_fwd(c));
 }
@@ -799,7 +804,8 @@ roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, i
   if (!known_type(dtype) || (param_dtype != dtype && param_dtype != ROI_FP32) || (!layer && kind != ROI_RMS_NORM) ||
       (!layer && (mean != nullptr || out_dbeta != nullptr)))
     return ROI_ERR_TYPE;
-  if (!good_shape(rows, cols, lddy) || !good_shape(rows, cols, lddx) || (x != nullptr && !good_shape(rows, cols, ldx)))
+  if (!good_shape(rows, cols, lddy) || !good_shape(rows, cols, lddx) || (x != nullptr && !good_shape(rows, cols, ldx)) ||
+      cols > kNormCols)
     return ROI_ERR_SHAPE;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (!aligned_to(out_dgamma, 4) || !aligned_to(out_dbeta, 4)) return ROI_ERR_ALIGN;
@@ -849,6 +855,8 @@ roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, i
   c.lddy = lddy;
   c.ldx = ldx;
   c.lddx = lddx;
+  c.status = status_word();
+  if (c.status == nullptr) return ROI_ERR_CUDA;
   c.stream = st;
   return finish(launch_norm_bwd(c));
 }

@@ -146,6 +146,14 @@ __device__ __forceinline__ uint32_t block8_codes4(const float* x, float inverse,
 __device__ __forceinline__ float block8_value(uint32_t word, int i, float step) {
   return float(int8_t(word >> (8 * i))) * step;
 }
+// The values of the four codes of a word, in pairs.  A code's byte, its sign bit turned, in the
+// mantissa of 2^23 is 2^23 + 128 + the code; difference and product are exact.
+__device__ __forceinline__ void block8_pairs(uint32_t word, float step, F2& a, F2& b) {
+  const uint32_t u = word ^ 0x80808080u;
+  const F2 minus = f2(-8388736.0f), s = f2(step);
+  a = (f2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441))) + minus) * s;
+  b = (f2(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443))) + minus) * s;
+}
 // The element type's value: fp16 ends before the largest checkpointed values do.
 template <Elem E>
 __device__ __forceinline__ float block8_clip(float v) {

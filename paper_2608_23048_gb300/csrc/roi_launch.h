@@ -150,6 +150,7 @@ struct NormFwdCall {
   bool params32;      // gamma and beta in fp32, else in dtype
   float eps;
   int64_t rows, cols, ldx, ldy;
+  unsigned int* status;
   cudaStream_t stream;
 };
 
@@ -168,6 +169,7 @@ struct NormBwdCall {
   Elem dtype;
   bool layer, params32;
   int64_t rows, cols, lddy, ldx, lddx;
+  unsigned int* status;
   cudaStream_t stream;
 };
 

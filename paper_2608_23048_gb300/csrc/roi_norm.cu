@@ -8,23 +8,40 @@
 //   dgamma = sum over rows of dy xh,  dbeta = sum over rows of dy
 //
 // Bound by memory (one read of every input, one write of every output).  Everything is
-// computed in 32 bits; outputs are rounded once.
+// computed in 32 bits, two columns an instruction; outputs are rounded once.
 //
-// Forward: a CTA a row, the row in registers (each thread holds NV pieces of 8 elements), so
-// the squares are summed around the mean already known and x is read once.  Rows past 16384
-// columns are read again for each step instead.
-// Backward: a team of threads a row, each thread with the same 8 columns of every row it
-// sees, so that the sums of dgamma and dbeta stay in its registers; two rows are reduced at a
-// time and the next two are loaded before.  The teams' and then the CTAs' sums are added in a
-// fixed order (through shared memory, and by a second launch): no atomics, the same bits every
-// time.  Rows past 8192 columns go to a kernel for dx and one for the sums over rows.
-// Pieces are 8 consecutive columns where the rows allow 16-byte loads (VEC); elsewhere a
-// thread takes every blockDim-th column, so that a warp still reads 32 neighbours.
+// A team of warps takes a row at a time.  Its rows come through a ring in shared memory, which a warp of
+// its own fills by bulk copies far ahead of their use, so that threads hold no rows on their way: an SM
+// keeps some 200 KB in flight.  A lane has runs of 8 consecutive columns; its warp's runs follow one
+// another.  gamma and beta lie in shared memory as fp32, for all rows of a CTA.
+//  - forward: the row in registers as it was read (RUN pieces a lane), so the squares are summed around
+//    the mean already known;
+//  - backward: a thread has the same columns of every row it sees, so that the sums of dgamma and dbeta
+//    stay in its registers.  The teams' and then the CTAs' sums are added in a fixed order (through
+//    shared memory, and by a second launch): no atomics, the same bits every time.
+// Rows that start anywhere are copied by the 16-byte granules around them (but for the matrix's own
+// ends) and shifted as they are read; they are written as roi_rows.cuh does.  Rows so wide that
+// two of them do not fit go to kernels that read them again for each step.
+#include <atomic>
+
 #include "roi_block8.cuh"
 #include "roi_launch.h"
+#include "roi_rows.cuh"
+#include "roi_tc.cuh"
 
 namespace roi {
 namespace {
+
+// The division of a launch's rows among teams, and of shared memory.
+struct Shape {
+  int nt;         // threads of a team
+  int teams;      // of a CTA
+  int depth;      // rows of a team's ring, 0 where two do not fit
+  int grid;
+  uint32_t stage; // bytes of a row in the ring
+  uint32_t params; // bytes of gamma (and beta) before the rings
+  size_t smem;
+};
 
 struct FwdArgs {
   const void* x;
@@ -39,6 +56,8 @@ struct FwdArgs {
   uint8_t* yscales;
   int64_t rows, cols, ldx, ldy;
   int64_t pitch, spitch;
+  Shape shape;
+  unsigned int* status;
   float eps;
   bool params32;  // gamma and beta in fp32, else in the type of x
   bool wait;
@@ -58,111 +77,16 @@ struct BwdArgs {
   float* part;  // [gridDim][1 or 2][part_cols] sums of a CTA's rows
   int64_t rows, cols, lddy, ldx, lddx;
   int64_t pitch, spitch, part_cols;
-  int teams;
+  Shape shape;
+  unsigned int* status;
   bool params32;
   bool wait;
 };
 
-// gamma or beta at 8 consecutive columns from c on, or at one column; `none` where not given.
-template <Elem E>
-__device__ __forceinline__ void param8(const void* p, bool p32, int64_t c, int64_t cols, float none, float (&v)[8]) {
-  using T = typename ElemType<E>::T;
-  if (p == nullptr) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = none;
-  } else if (c + 8 <= cols) {
-    if (p32) {
-      Raw8<Elem::kFp32> r;
-      r.load(static_cast<const float*>(p) + c);
-      r.get(v);
-    } else {
-      Raw8<E> r;
-      r.load(static_cast<const T*>(p) + c);
-      r.get(v);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      v[i] = c + i >= cols ? none : p32 ? __ldg(static_cast<const float*>(p) + c + i) : to_f32<E>(__ldg(static_cast<const T*>(p) + c + i));
-  }
-}
 template <Elem E>
 __device__ __forceinline__ float param1(const void* p, bool p32, int64_t c, float none) {
   using T = typename ElemType<E>::T;
   return p == nullptr ? none : p32 ? __ldg(static_cast<const float*>(p) + c) : to_f32<E>(__ldg(static_cast<const T*>(p) + c));
-}
-
-// Column of element k of piece i of thread `t` of `nt`.
-template <bool VEC>
-__device__ __forceinline__ int64_t column(int i, int k, int t, int nt) {
-  return VEC ? (int64_t(i) * nt + t) * 8 + k : (int64_t(i) * 8 + k) * nt + t;
-}
-
-template <Elem E, bool VEC>
-__device__ __forceinline__ void load_piece(const typename ElemType<E>::T* row, int64_t cols, int i, int t, int nt, float (&v)[8]) {
-  if constexpr (VEC) {
-    const int64_t c = column<true>(i, 0, t, nt);
-    if (c + 8 <= cols) {
-      Raw8<E> r;
-      r.load(row + c);
-      r.get(v);
-      return;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int64_t c = column<VEC>(i, k, t, nt);
-    v[k] = c < cols ? to_f32<E>(row[c]) : 0.0f;
-  }
-}
-
-template <Elem E, bool VEC>
-__device__ __forceinline__ void store_piece(typename ElemType<E>::T* row, int64_t cols, int i, int t, int nt, const float (&v)[8]) {
-  if constexpr (VEC) {
-    const int64_t c = column<true>(i, 0, t, nt);
-    if (c + 8 <= cols) {
-      Raw8<E> r;
-      r.set(v);
-      r.store(row + c);
-      return;
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    const int64_t c = column<VEC>(i, k, t, nt);
-    if (c < cols) row[c] = from_f32<E>(v[k]);
-  }
-}
-
-// One piece's part of a checkpoint row (all lanes of the warp call it; values past the last
-// column are 0).  VEC: a block is four neighbouring lanes; else a lane's k-th element belongs
-// to the warp's k-th block.
-template <bool VEC>
-__device__ __forceinline__ void save_piece(int8_t* codes, uint8_t* scales, int64_t pitch, int64_t spitch, int i, int t, int nt,
-                                           const float (&v)[8]) {
-  if constexpr (VEC) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) top = max(top, abs_bits(v[k]));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const uint32_t s = block8_scale(top);
-    const float inverse = block8_inverse(min(s, kScaleMax));
-    const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
-    const int64_t c = column<true>(i, 0, t, nt);
-    if (c < pitch)
-      *reinterpret_cast<uint2*>(codes + c) = make_uint2(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep));
-    if (c % 32 == 0 && c / 32 < spitch) scales[c / 32] = uint8_t(s);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const uint32_t s = block8_scale(__reduce_max_sync(0xffffffffu, abs_bits(v[k])));
-      const uint32_t q = block8_code(v[k], block8_inverse(min(s, kScaleMax)));
-      const int64_t c = column<false>(i, k, t, nt);
-      if (c < pitch) codes[c] = s == kScaleNaN ? int8_t(0) : int8_t(q);
-      if (c % 32 == 0 && c / 32 < spitch) scales[c / 32] = uint8_t(s);
-    }
-  }
 }
 
 __device__ __forceinline__ float warp_sum(float v) {
@@ -170,102 +94,116 @@ __device__ __forceinline__ float warp_sum(float v) {
   for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
   return v;
 }
-// Sum over the CTA, the same bits in every thread.  Two sets of slots in turn: a set is written
-// again only after the barrier of the sum in between.
-__device__ __forceinline__ float cta_sum(float v, float (&slots)[2][32], int& turn) {
-  v = warp_sum(v);
-  if (blockDim.x == 32) return v;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (lane == 0) slots[turn][warp] = v;
-  __syncthreads();
-  v = warp_sum(lane < int(blockDim.x >> 5) ? slots[turn][lane] : 0.0f);
-  turn ^= 1;
-  return v;
+
+// Eight columns in pairs.
+struct Piece {
+  F2 v[4];
+};
+__device__ __forceinline__ Piece pairs(const float (&f)[8]) {
+  Piece p;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p.v[k] = f2(f[2 * k], f[2 * k + 1]);
+  return p;
+}
+__device__ __forceinline__ float total(F2 s) { return lo(s) + hi(s); }
+// gamma or beta as fp32 in shared memory (the whole CTA; `n` is cols rounded up to a warp's pieces),
+// `none` where it is not given and past the last column.  Each 256 columns lie as the first four of
+// every lane's eight, then the others, so that a warp's loads meet on no bank.
+template <Elem E>
+__device__ __forceinline__ void stage_param(float* to, const void* p, bool p32, int cols, int n, float none) {
+  for (int c = threadIdx.x; c < n; c += blockDim.x)
+    to[(c & ~255) + (c & 4) * 32 + ((c & 255) >> 3) * 4 + (c & 3)] = c < cols ? param1<E>(p, p32, c, none) : none;
+}
+// Of the lane whose first column is c = 256 q + 8 lane.
+__device__ __forceinline__ Piece param(const float* p, int c) {
+  const float* at = p + (c & ~255) + ((c & 255) >> 1);
+  const float4 a = *reinterpret_cast<const float4*>(at), b = *reinterpret_cast<const float4*>(at + 128);
+  Piece q;
+  q.v[0] = f2(a.x, a.y), q.v[1] = f2(a.z, a.w), q.v[2] = f2(b.x, b.y), q.v[3] = f2(b.z, b.w);
+  return q;
 }
 
-constexpr int kFwdThreads = 512, kTeamThreads = 512;  // at most, of a CTA
-// NV > 0: the row in registers; NV = 0: read again for each step, `pieces` pieces a thread.
-template <Elem E, bool LAYER, bool VEC, int NV>
-__global__ void __launch_bounds__(kFwdThreads) roi_norm_fwd_kernel(FwdArgs a, int pieces) {
-  using T = typename ElemType<E>::T;
-  __shared__ float slots[2][32];
-  pdl_begin(a.wait);
-  const int t = threadIdx.x, nt = blockDim.x;
-  const int n = NV > 0 ? NV : pieces;
-  constexpr int kHeld = NV > 0 ? NV : 1;
-  const float inv_cols = 1.0f / float(a.cols);
-  int turn = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    float v[kHeld][8];
-    auto piece = [&](int i) -> float(&)[8] {
-      if (NV == 0) load_piece<E, VEC>(x, a.cols, i, t, nt, v[0]);
-      return v[NV > 0 ? i : 0];
-    };
-    if constexpr (NV > 0) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) load_piece<E, VEC>(x, a.cols, i, t, nt, v[i]);
-    }
-    float mean = 0.0f;
-    if constexpr (LAYER) {
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        float(&p)[8] = piece(i);
-        sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-      }
-      mean = cta_sum(sum, slots, turn) * inv_cols;
-    }
-    float squares = 0.0f;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      float(&p)[8] = piece(i);
-      float s = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        // columns past the last hold 0, which is not at distance 0 from the mean
-        const float d = LAYER && column<VEC>(i, k, t, nt) >= a.cols ? 0.0f : p[k] - mean;
-        s = __fmaf_rn(d, d, s);
-      }
-      squares += s;
-    }
-    const float rstd = 1.0f / sqrtf(cta_sum(squares, slots, turn) * inv_cols + a.eps);
-    if (t == 0) {
-      if (LAYER && a.mean != nullptr) a.mean[row] = mean;
-      if (a.rstd != nullptr) a.rstd[row] = rstd;
-    }
-    T* y = static_cast<T*>(a.y) + row * a.ldy;
-#pragma unroll
-    for (int i = 0; i < n; ++i) {
-      float(&p)[8] = piece(i);
-      float o[8];
-      if (a.xcodes != nullptr)
-        save_piece<VEC>(a.xcodes + row * a.pitch, a.xscales + row * a.spitch, a.pitch, a.spitch, i, t, nt, p);
-      if constexpr (VEC) {
-        const int64_t c = column<true>(i, 0, t, nt);
-        float g[8], b[8];
-        param8<E>(a.gamma, a.params32, c, a.cols, 1.0f, g);
-        param8<E>(a.beta, a.params32, c, a.cols, 0.0f, b);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = __fmaf_rn((p[k] - mean) * rstd, g[k], b[k]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int64_t c = column<false>(i, k, t, nt);
-          const bool in = c < a.cols;
-          o[k] = __fmaf_rn((p[k] - mean) * rstd, in ? param1<E>(a.gamma, a.params32, c, 1.0f) : 1.0f,
-                           in ? param1<E>(a.beta, a.params32, c, 0.0f) : 0.0f);
-        }
-      }
-      store_piece<E, VEC>(y, a.cols, i, t, nt, o);
-      if (a.ycodes != nullptr) {
-        // of y as it was rounded
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = column<VEC>(i, k, t, nt) < a.cols ? to_f32<E>(from_f32<E>(o[k])) : 0.0f;
-        save_piece<VEC>(a.ycodes + row * a.pitch, a.yscales + row * a.spitch, a.pitch, a.spitch, i, t, nt, o);
-      }
-    }
+// ---- a row in the ring ----
+// A matrix row's place: `m` bytes after the stage's start, as after a 16-byte boundary in memory.
+template <bool ANY>
+__device__ __forceinline__ uint32_t row_shift(const void* row) {
+  return ANY ? uint32_t(reinterpret_cast<uintptr_t>(row) & 15u) : 0u;
+}
+// What the bulk copy of a row of `bytes` takes: the granules around it, without those that begin before
+// the matrix's first or end after its last byte (`first`, `last`: its first and last row).
+struct Extent {
+  uintptr_t row, end, from, to;
+  __device__ __forceinline__ Extent(const void* p, uint32_t bytes, bool any, bool first, bool last) {
+    row = reinterpret_cast<uintptr_t>(p), end = row + bytes;
+    from = !any ? row : first ? (row + 15) & ~uintptr_t(15) : row & ~uintptr_t(15);
+    to = !any ? end : last ? end & ~uintptr_t(15) : (end + 15) & ~uintptr_t(15);
   }
+  __device__ __forceinline__ uint32_t bytes() const { return to > from ? uint32_t(to - from) : 0u; }
+  // (one thread) the copy, and before it what it leaves out at the matrix's ends
+  __device__ __forceinline__ void ends(uint8_t* st) const {
+    uint8_t* at = st + (row & 15);
+    for (uintptr_t p = row; p < from && p < end; ++p) at[p - row] = *reinterpret_cast<const uint8_t*>(p);
+    uintptr_t p = to > from ? to : from;
+    for (p = p < row ? row : p; p < end; ++p) at[p - row] = *reinterpret_cast<const uint8_t*>(p);
+  }
+  __device__ __forceinline__ void copy(uint8_t* st, uint64_t* bar) const {
+    if (to > from) bulk_g2s(st + (from - (row & ~uintptr_t(15))), reinterpret_cast<const void*>(from), uint32_t(to - from), bar);
+  }
+};
+// Zeros past the last column.
+template <Elem E>
+__device__ __forceinline__ void clear_past(RowWords<E, 8>& r, int c, int cols) {
+#pragma unroll
+  for (int i = 0; i < RowWords<E, 8>::kWords; ++i) {
+    const int k = E == Elem::kFp32 ? i : 2 * i;  // the word's first column
+    if (c + k >= cols) r.u[i] = 0;
+    else if (E != Elem::kFp32 && c + k + 1 >= cols) r.u[i] &= 0xffffu;
+  }
+}
+// Columns c .. c + 7 of a row whose stage starts at st (zeros past the last column).
+template <Elem E, bool ANY>
+__device__ __forceinline__ RowWords<E, 8> read_row(const uint8_t* st, uint32_t m, int c, int cols) {
+  constexpr int W = RowWords<E, 8>::kWords;
+  RowWords<E, 8> r;
+  if (c >= cols) {
+    r.zero();
+    return r;
+  }
+  const uint4* q = reinterpret_cast<const uint4*>(st + c * elem_bytes<E>());
+  uint32_t w[ANY ? W + 4 : W];
+#pragma unroll
+  for (int i = 0; i < (ANY ? W / 4 + 1 : W / 4); ++i) {
+    const uint4 v = q[i];
+    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  }
+  if constexpr (ANY) {
+    shift_words<W>(w, m, r.u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) r.u[i] = w[i];
+  }
+  // (a whole number of granules is one of pieces in 16 bits, and of half pieces in 32)
+  if ((ANY || E == Elem::kFp32) && c + 8 > cols) clear_past<E>(r, c, cols);
+  return r;
+}
+
+// One piece's part of a checkpoint row (all lanes of the warp call it; values past the last column
+// are 0): a block is four neighbouring lanes.
+template <Elem E>
+__device__ __forceinline__ void save_piece(int8_t* codes, uint8_t* scales, int64_t pitch, int64_t spitch, int c, const RowWords<E, 8>& r) {
+  float v[8];
+  r.get(v);
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = max(top, abs_bits(v[k]));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+  top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+  const uint32_t s = block8_scale(top);
+  const float inverse = block8_inverse(min(s, kScaleMax));
+  const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
+  if (c < pitch)
+    *reinterpret_cast<uint2*>(codes + c) = make_uint2(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep));
+  if (c % 32 == 0 && c / 32 < spitch) scales[c / 32] = uint8_t(s);
 }
 
 __device__ __forceinline__ void team_sync(int team, int nt) {
@@ -276,237 +214,409 @@ __device__ __forceinline__ void team_sync(int team, int nt) {
   }
 }
 
-// A thread's piece of one row of the backward's inputs, as it lies in memory.
-template <Elem E, bool VEC, bool CKPT>
-struct RowIn {
-  using T = typename ElemType<E>::T;
-  static constexpr int kEl = VEC ? 1 : 8;
-  Raw8<E> dy8, x8;
-  T dy1[kEl], x1[kEl];
-  uint2 q8;
-  int8_t q1[kEl];
-  uint8_t s1[kEl];
-
-  __device__ __forceinline__ void load(const BwdArgs& a, int64_t row, int piece, int t, int nt) {
-    const bool in = row < a.rows;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.lddy;
-    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
-    if constexpr (VEC) {
-      const int64_t c = column<true>(piece, 0, t, nt);
-      const bool whole = in && c + 8 <= a.cols;
-      if (whole) {
-        dy8.load(dy + c);
-        if constexpr (!CKPT) x8.load(x + c);
-      } else {
-        float v[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = in && c + k < a.cols ? to_f32<E>(dy[c + k]) : 0.0f;
-        dy8.set(v);
-        if constexpr (!CKPT) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = in && c + k < a.cols ? to_f32<E>(x[c + k]) : 0.0f;
-          x8.set(v);
-        }
-      }
-      if constexpr (CKPT) {
-        q8 = make_uint2(0, 0), s1[0] = 0;
-        if (in && c < a.pitch) {
-          q8 = __ldg(reinterpret_cast<const uint2*>(a.codes + row * a.pitch + c));
-          s1[0] = __ldg(a.scales + row * a.spitch + c / 32);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t c = column<false>(piece, k, t, nt);
-        const bool ok = in && c < a.cols;
-        dy1[k] = ok ? dy[c] : T(0);
-        if constexpr (CKPT) {
-          q1[k] = ok ? a.codes[row * a.pitch + c] : int8_t(0);
-          s1[k] = ok ? a.scales[row * a.spitch + c / 32] : uint8_t(0);
-        } else {
-          x1[k] = ok ? x[c] : T(0);
-        }
-      }
-    }
-  }
-  __device__ __forceinline__ void get(float (&dy)[8], float (&x)[8]) const {
-    if constexpr (VEC) {
-      dy8.get(dy);
-      if constexpr (CKPT) {
-        const float step = block8_step(s1[0]);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = block8_value(k < 4 ? q8.x : q8.y, k % 4, step);
-      } else {
-        x8.get(x);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        dy[k] = to_f32<E>(dy1[k]);
-        x[k] = CKPT ? float(q1[k]) * block8_step(s1[k]) : to_f32<E>(x1[k]);
-      }
-    }
-  }
+// Pieces a lane of the forward holds, and the most threads of a CTA: what keeps the registers that a
+// thread then has from spilling.
+constexpr int kRun = 4, kFwdThreads = 768;
+constexpr int kThreads = 1024, kMostTeams = 32, kMostNamed = 15, kMostDepth = 8;
+// Barriers, slots and flags of the teams.
+struct TeamState {
+  uint64_t full[kMostTeams][kMostDepth];   // the row has landed
+  uint64_t empty[kMostTeams][kMostDepth];  // every warp has read it
+  float slots[3][kThreads / 32][2];  // a set is written again two meetings later
+  int gave_up[kMostTeams];
 };
+// The barriers of the rings (the whole CTA).
+__device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
+  for (int i = threadIdx.x; i < s.teams * s.depth; i += blockDim.x) {
+    mbar_init(&ts.full[i / s.depth][i % s.depth], 1);
+    mbar_init(&ts.empty[i / s.depth][i % s.depth], s.nt / 32);
+  }
+  if (threadIdx.x < kMostTeams) ts.gave_up[threadIdx.x] = 0;
+  fence_mbar_init();
+  __syncthreads();
+}
+// The warp that fills the rings, a lane a team: `copy(team, stage, row, barrier)` sends a row's copies
+// off.  It gives up when no stage has become free for `lim`; what was sent off lands before it leaves.
+template <class Copy>
+__device__ __forceinline__ void fill_rings(TeamState& ts, const Shape& s, int64_t rows, uint64_t lim, unsigned int* status, Copy copy) {
+  const int team = threadIdx.x & 31;
+  const int64_t all = int64_t(gridDim.x) * s.teams;
+  int64_t row = team < s.teams ? int64_t(blockIdx.x) * s.teams + team : rows;
+  int at = 0, k = 0;
+  uint32_t pass = 0;  // parity of the phase that frees the stage
+  uint64_t since = 0;
+  while (__any_sync(0xffffffffu, row < rows)) {
+    const bool go = row < rows && (k < s.depth || mbar_test_wait(&ts.empty[team][at], pass));
+    if (go) {
+      copy(team, at, row, &ts.full[team][at]);
+      row += all;
+      if (k++ >= s.depth && at == s.depth - 1) pass ^= 1u;
+      at = at == s.depth - 1 ? 0 : at + 1;
+    }
+    if (__any_sync(0xffffffffu, go)) {
+      since = 0;
+    } else if (since == 0) {
+      since = global_timer_ns();
+    } else if (global_timer_ns() - since > lim) {
+      break;
+    }
+  }
+  const bool gave_up = __any_sync(0xffffffffu, row < rows);
+  if (gave_up || (team < s.teams && ts.gave_up[team] != 0)) {
+    // (a stage's phases end one after another, so the last rows of the ring stand for all)
+    for (int q = k > s.depth ? k - s.depth : 0; q < k; ++q) mbar_wait_bounded(&ts.full[team][q % s.depth], uint32_t(q / s.depth) & 1u);
+  }
+  if (gave_up && team == 0) atomicOr(status, kStatusTimeout);
+}
 
-// NP: pieces a thread; PAIR: rows a team reduces at a time.
-template <Elem E, bool LAYER, bool VEC, bool CKPT, int NP, int PAIR>
-__global__ void __launch_bounds__(kTeamThreads) roi_norm_bwd_kernel(BwdArgs a) {
+// RUN pieces a lane.
+template <Elem E, bool LAYER, bool ANY, int RUN>
+__global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads) roi_norm_fwd_kernel(FwdArgs a) {
   using T = typename ElemType<E>::T;
-  extern __shared__ float sums[];  // [1 or 2][NP][8][nt], the teams' sums (more than one team)
-  __shared__ float slots[2][kTeamThreads / 32][2 * PAIR];
+  extern __shared__ __align__(128) uint8_t smem[];  // gamma, beta; [teams][depth][stage]
+  __shared__ TeamState ts;
+  const int nt = a.shape.nt, team = threadIdx.x / nt, t = threadIdx.x - team * nt;
+  const int warps = nt >> 5, warp0 = team * warps, warp = t >> 5, lane = t & 31, depth = a.shape.depth;
+  const int cols = int(a.cols), padded = (cols + 255) / 256 * 256;
+  init_teams(ts, a.shape);
   pdl_begin(a.wait);
-  const int nt = blockDim.x / a.teams;
-  const int team = threadIdx.x / nt, t = threadIdx.x - team * nt;
-  const int warps = nt >> 5, warp0 = team * warps, lane = t & 31;
-  const float inv_cols = 1.0f / float(a.cols);
-  auto weight = [&](int i, float(&g)[8]) {
-    if constexpr (VEC) {
-      param8<E>(a.gamma, a.params32, column<true>(i, 0, t, nt), a.cols, 1.0f, g);
-    } else {
+  const uint64_t lim = ring_wait_limit(a.status);
+  float* gamma = reinterpret_cast<float*>(smem);
+  float* beta = gamma + padded;
+  stage_param<E>(gamma, a.gamma, a.params32, cols, padded, 1.0f);
+  if constexpr (LAYER) stage_param<E>(beta, a.beta, a.params32, cols, padded, 0.0f);
+  __syncthreads();
+  if (team == a.shape.teams) {
+    fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
+      uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
+      const bool first = row == 0, last = row == a.rows - 1;
+      const Extent x(static_cast<const T*>(a.x) + row * a.ldx, uint32_t(cols) * elem_bytes<E>(), ANY, first, last);
+      if (ANY && (first || last)) x.ends(st);
+      mbar_arrive_expect_tx(bar, x.bytes());
+      x.copy(st, bar);
+    });
+    return;
+  }
+  const int64_t all = int64_t(gridDim.x) * a.shape.teams, row0 = int64_t(blockIdx.x) * a.shape.teams + team;
+  const uint8_t* ring = smem + a.shape.params + size_t(team) * depth * a.shape.stage;
+  const int base = warp * RUN * 256, c0 = base + lane * 8;  // the warp's and the lane's first column
+  // columns that the pieces go up to: the row's, and a checkpoint's padding
+  const int end = a.xcodes != nullptr || a.ycodes != nullptr ? int(a.spitch) * 32 : cols;
+  const float inv_cols = 1.0f / float(cols);
+  int at = 0, turn = 0;
+  uint32_t pass = 0;
+  // sum over the team, the same bits in every thread
+  auto meet = [&](float v) {
+    v = warp_sum(v);
+    if (nt > 32 && lane == 0) ts.slots[turn][warp0 + warp][0] = v;
+    team_sync(team, nt);
+    if (nt > 32) v = warp_sum(lane < warps ? ts.slots[turn][warp0 + lane][0] : 0.0f);
+    turn = turn == 2 ? 0 : turn + 1;
+    return v;
+  };
+  for (int64_t row = row0; row < a.rows; row += all) {
+    if (!mbar_wait_ring(&ts.full[team][at], pass, lim)) ts.gave_up[team] = 1;
+    const uint8_t* st = ring + at * a.shape.stage;
+    const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.x) + row * a.ldx);
+    RowWords<E, 8> x[RUN];
+    F2 sum = f2(0.0f);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t c = column<false>(i, k, t, nt);
-        g[k] = c < a.cols ? param1<E>(a.gamma, a.params32, c, 1.0f) : 1.0f;
+    for (int i = 0; i < RUN; ++i) {
+      x[i] = read_row<E, ANY>(st, m, c0 + 256 * i, cols);
+      if constexpr (LAYER) {
+        float f[8];
+        x[i].get(f);
+        const Piece v = pairs(f);
+        sum = sum + ((v.v[0] + v.v[1]) + (v.v[2] + v.v[3]));
       }
     }
-  };
-  // with one piece a thread the weight stays in registers
-  float held[8], dg[NP][8], db[NP][8];
-  if constexpr (NP == 1) weight(0, held);
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ts.empty[team][at]);
+    float mean = 0.0f;
+    if constexpr (LAYER) mean = meet(total(sum)) * inv_cols;
+    const F2 minus = f2(-mean);
+    F2 squares = f2(0.0f);
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+      if (base + 256 * i >= cols) break;
+      float f[8];
+      x[i].get(f);
+      Piece v = pairs(f);
+      if constexpr (LAYER) {
+        // (columns past the last hold 0, which is not at distance 0 from the mean)
+        const int left = cols - (c0 + 256 * i);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v.v[k] = v.v[k] + minus;
+        if (left < 8) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v.v[k] = f2(2 * k < left ? lo(v.v[k]) : 0.0f, 2 * k + 1 < left ? hi(v.v[k]) : 0.0f);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) squares = vfma(v.v[k], v.v[k], squares);
+    }
+    const float rstd = 1.0f / sqrtf(meet(total(squares)) * inv_cols + a.eps);
+    if (ts.gave_up[team]) break;  // (the whole team)
+    if (t == 0) {
+      if (LAYER && a.mean != nullptr) a.mean[row] = mean;
+      if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+    if (a.xcodes != nullptr) {
+#pragma unroll
+      for (int i = 0; i < RUN; ++i)
+        if (base + 256 * i < end) save_piece<E>(a.xcodes + row * a.pitch, a.xscales + row * a.spitch, a.pitch, a.spitch, c0 + 256 * i, x[i]);
+    }
+    T* to = static_cast<T*>(a.y) + row * a.ldy;
+    const F2 r2 = f2(rstd);
+#pragma unroll
+    for (int i = 0; i < RUN; ++i) {
+      if (base + 256 * i >= cols) break;
+      const int c = c0 + 256 * i;
+      float f[8];
+      x[i].get(f);
+      Piece v = pairs(f);
+      const Piece g = param(gamma, c);
+      Piece b;
+      if constexpr (LAYER) b = param(beta, c);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (LAYER) v.v[k] = vfma((v.v[k] + minus) * r2, g.v[k], b.v[k]);
+        else v.v[k] = v.v[k] * r2 * g.v[k];
+        f[2 * k] = lo(v.v[k]), f[2 * k + 1] = hi(v.v[k]);
+      }
+      RowWords<E, 8> y;
+      y.set(f);
+      store_row<E, 8, !ANY>(to, c, cols, y, 32, i > 0 ? &x[i - 1] : nullptr, i + 1 < RUN && base + 256 * (i + 1) < cols);
+      x[i] = y;
+    }
+    if (a.ycodes != nullptr) {
+#pragma unroll
+      for (int i = 0; i < RUN; ++i) {
+        const int c = c0 + 256 * i;
+        if (base + 256 * i >= end) break;
+        if (base + 256 * i >= cols) x[i].zero();
+        // (a bias or a NaN may stand past the last column)
+        if (c + 8 > cols) clear_past<E>(x[i], c, cols);
+        save_piece<E>(a.ycodes + row * a.pitch, a.yscales + row * a.spitch, a.pitch, a.spitch, c, x[i]);
+      }
+    }
+    if (++at == depth) at = 0, pass ^= 1u;
+  }
+  if (ts.gave_up[team] && t == 0) atomicOr(a.status, kStatusTimeout);
+}
+
+// First column of run i of a team's thread t, with NP runs a thread.
+template <int NP>
+__device__ __forceinline__ int column(int i, int t) { return ((t >> 5) * NP + i) * 256 + (t & 31) * 8; }
+
+constexpr int kBwdThreads = 512;
+
+template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP>
+__global__ void __launch_bounds__(kBwdThreads) roi_norm_bwd_kernel(BwdArgs a) {
+  using T = typename ElemType<E>::T;
+  extern __shared__ __align__(128) uint8_t smem[];  // gamma; [teams][depth][stage]; at the end the teams' sums
+  __shared__ TeamState ts;
+  const int nt = a.shape.nt, team = threadIdx.x / nt, t = threadIdx.x - team * nt;
+  const int warps = nt >> 5, warp0 = team * warps, warp = t >> 5, lane = t & 31, depth = a.shape.depth;
+  const int cols = int(a.cols), padded = (cols + 255) / 256 * 256;
+  init_teams(ts, a.shape);
+  pdl_begin(a.wait);
+  const uint64_t lim = ring_wait_limit(a.status);
+  const uint32_t room = (uint32_t(cols + 7) / 8 * 8) * elem_bytes<E>() + (ANY ? 32u : 0u);  // of dy, before x
+  float* gamma = reinterpret_cast<float*>(smem);
+  stage_param<E>(gamma, a.gamma, a.params32, cols, padded, 1.0f);
+  __syncthreads();
+  const int teams = a.shape.teams;
+  const bool sums_wanted = a.dgamma != nullptr || a.dbeta != nullptr;
+  if (team == teams) {
+    fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
+      uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
+      const bool first = row == 0, last = row == a.rows - 1;
+      const uint32_t row_bytes = uint32_t(cols) * elem_bytes<E>();
+      const Extent dy(static_cast<const T*>(a.dy) + row * a.lddy, row_bytes, ANY, first, last);
+      if (ANY && (first || last)) dy.ends(st);
+      if constexpr (CKPT) {
+        const Extent scales(a.scales + row * a.spitch, uint32_t(a.spitch), true, first, last);
+        if (first || last) scales.ends(st + room + a.pitch);
+        mbar_arrive_expect_tx(bar, dy.bytes() + uint32_t(a.pitch) + scales.bytes());
+        bulk_g2s(st + room, a.codes + row * a.pitch, uint32_t(a.pitch), bar);
+        scales.copy(st + room + a.pitch, bar);
+      } else {
+        const Extent x(static_cast<const T*>(a.x) + row * a.ldx, row_bytes, ANY, first, last);
+        if (ANY && (first || last)) x.ends(st + room);
+        mbar_arrive_expect_tx(bar, dy.bytes() + x.bytes());
+        x.copy(st + room, bar);
+      }
+      dy.copy(st, bar);
+    });
+    // the barriers of the others' sums
+    if (sums_wanted) {
+      __syncthreads();
+      for (int q = 0; q < teams && teams > 1; ++q) __syncthreads();
+    }
+    return;
+  }
+  const float inv_cols = 1.0f / float(cols);
+  const int64_t all = int64_t(gridDim.x) * teams, row0 = int64_t(blockIdx.x) * teams + team;
+  const uint8_t* ring = smem + a.shape.params + size_t(team) * depth * a.shape.stage;
+
+  Piece dg[NP], db[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) dg[i][k] = db[i][k] = 0.0f;
-
-  const int64_t all = int64_t(gridDim.x) * a.teams;
-  int64_t row = int64_t(blockIdx.x) * a.teams + team;
-  RowIn<E, VEC, CKPT> next[PAIR][NP];
-  float next_mean[PAIR], next_rstd[PAIR];
-  auto load = [&](int64_t from) {
-#pragma unroll
-    for (int r = 0; r < PAIR; ++r) {
-      const int64_t at = from + r * all;
-      next_mean[r] = LAYER && at < a.rows ? __ldg(a.mean + at) : 0.0f;
-      next_rstd[r] = at < a.rows ? __ldg(a.rstd + at) : 0.0f;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) next[r][i].load(a, at, i, t, nt);
+    for (int k = 0; k < 4; ++k) dg[i].v[k] = db[i].v[k] = f2(0.0f);
+  float next_mean = LAYER && row0 < a.rows ? __ldg(a.mean + row0) : 0.0f, next_rstd = row0 < a.rows ? __ldg(a.rstd + row0) : 0.0f;
+  int at = 0, turn = 0;
+  uint32_t pass = 0;
+  T* to = static_cast<T*>(a.dx) + row0 * a.lddx;
+  for (int64_t row = row0; row < a.rows; row += all) {
+    const float rstd = next_rstd;
+    const F2 r2 = f2(rstd), minus = f2(-next_mean);
+    const int64_t after = row + all;
+    if (after < a.rows) {
+      next_rstd = __ldg(a.rstd + after);
+      if constexpr (LAYER) next_mean = __ldg(a.mean + after);
     }
-  };
-  load(row);
-  int turn = 0;
-  for (; row < a.rows; row += PAIR * all) {
-    RowIn<E, VEC, CKPT> cur[PAIR][NP];
-    float mean[PAIR], rstd[PAIR];
+    if (!mbar_wait_ring(&ts.full[team][at], pass, lim)) ts.gave_up[team] = 1;
+    const uint8_t* st = ring + at * a.shape.stage;
+    const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.dy) + row * a.lddy);
+    const uint32_t ms = CKPT ? row_shift<true>(a.scales + row * a.spitch) : 0u;
+    const uint32_t mx = CKPT ? 0u : row_shift<ANY>(static_cast<const T*>(a.x) + row * a.ldx);
+    // this thread's columns: dy, and xh (past the last column dy is 0)
+    auto get = [&](int i, Piece& dy, Piece& xh) {
+      const int c = column<NP>(i, t);
+      float f[8];
+      read_row<E, ANY>(st, m, c, cols).get(f);
+      dy = pairs(f);
+      if constexpr (CKPT) {
+        uint2 w = make_uint2(0, 0);
+        float step = 0.0f;
+        if (c < int(a.pitch)) {
+          w = *reinterpret_cast<const uint2*>(st + room + c);
+          step = block8_step(st[room + a.pitch + ms + c / 32]);
+        }
+        block8_pairs(w.x, step, xh.v[0], xh.v[1]);
+        block8_pairs(w.y, step, xh.v[2], xh.v[3]);
+      } else {
+        read_row<E, ANY>(st + room, mx, c, cols).get(f);
+        xh = pairs(f);
+      }
 #pragma unroll
-    for (int r = 0; r < PAIR; ++r) {
-      mean[r] = next_mean[r], rstd[r] = next_rstd[r];
+      for (int k = 0; k < 4; ++k) {
+        if constexpr (LAYER) xh.v[k] = xh.v[k] + minus;
+        xh.v[k] = xh.v[k] * r2;
+      }
+    };
+    F2 s1 = f2(0.0f), s2 = f2(0.0f);
+    Piece w[NP], xh[NP];  // dy gamma, and the normalised input
 #pragma unroll
-      for (int i = 0; i < NP; ++i) cur[r][i] = next[r][i];
-    }
-    load(row + PAIR * all);
-    float c[2 * PAIR];
+    for (int i = 0; i < NP; ++i) {
+      if (column<NP>(i, t) - lane * 8 >= cols) break;  // (the whole warp)
+      Piece dy;
+      get(i, dy, xh[i]);
+      const Piece g = param(gamma, column<NP>(i, t));
 #pragma unroll
-    for (int r = 0; r < PAIR; ++r) {
-      float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        float dy[8], x[8], g[8];
-        if constexpr (NP > 1) weight(i, g);
-        cur[r][i].get(dy, x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float gk = NP > 1 ? g[k] : held[k];
-          const float p = dy[k] * ((x[k] - mean[r]) * rstd[r]);
-          dg[i][k] += p;
-          if constexpr (LAYER) db[i][k] += dy[k];
-          c1 = __fmaf_rn(p, gk, c1);
-          if constexpr (LAYER) c2 = __fmaf_rn(dy[k], gk, c2);
+      for (int k = 0; k < 4; ++k) {
+        w[i].v[k] = dy.v[k] * g.v[k];
+        dg[i].v[k] = vfma(dy.v[k], xh[i].v[k], dg[i].v[k]);
+        s1 = vfma(w[i].v[k], xh[i].v[k], s1);
+        if constexpr (LAYER) {
+          db[i].v[k] = db[i].v[k] + dy.v[k];
+          s2 = s2 + w[i].v[k];
         }
       }
-      c[2 * r] = warp_sum(c1);
-      c[2 * r + 1] = LAYER ? warp_sum(c2) : 0.0f;
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&ts.empty[team][at]);
+    float c1 = warp_sum(total(s1)), c2 = LAYER ? warp_sum(total(s2)) : 0.0f;
+    if (nt > 32 && lane == 0) {
+      ts.slots[turn][warp0 + warp][0] = c1;
+      if constexpr (LAYER) ts.slots[turn][warp0 + warp][1] = c2;
+    }
+    team_sync(team, nt);
+    if (ts.gave_up[team]) break;  // (the whole team)
     if (nt > 32) {
-      if (lane == 0) {
-#pragma unroll
-        for (int q = 0; q < 2 * PAIR; ++q) slots[turn][warp0 + (t >> 5)][q] = c[q];
-      }
-      team_sync(team, nt);
-#pragma unroll
-      for (int q = 0; q < 2 * PAIR; ++q) c[q] = 0.0f;
-      for (int w = 0; w < warps; ++w) {
-#pragma unroll
-        for (int q = 0; q < 2 * PAIR; ++q) c[q] += slots[turn][warp0 + w][q];
-      }
-      turn ^= 1;
+      c1 = warp_sum(lane < warps ? ts.slots[turn][warp0 + lane][0] : 0.0f);
+      if constexpr (LAYER) c2 = warp_sum(lane < warps ? ts.slots[turn][warp0 + lane][1] : 0.0f);
+      turn = turn == 2 ? 0 : turn + 1;
     }
+    // dx = rstd a - rstd mean(a) - xh (rstd mean(a xh))
+    const F2 k1 = f2(-(c1 * inv_cols) * rstd), k2 = f2(-(c2 * inv_cols) * rstd);
+    RowWords<E, 8> before;
 #pragma unroll
-    for (int r = 0; r < PAIR; ++r) {
-      const int64_t at = row + r * all;
-      if (at >= a.rows) break;
-      const float m1 = c[2 * r] * inv_cols, m2 = c[2 * r + 1] * inv_cols;
+    for (int i = 0; i < NP; ++i) {
+      const int c = column<NP>(i, t);
+      if (c - lane * 8 >= cols) break;
+      float o[8];
 #pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        float dy[8], x[8], g[8], o[8];
-        if constexpr (NP > 1) weight(i, g);
-        cur[r][i].get(dy, x);
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          float d = __fmaf_rn((mean[r] - x[k]) * rstd[r], m1, dy[k] * (NP > 1 ? g[k] : held[k]));
-          if constexpr (LAYER) d -= m2;
-          o[k] = d * rstd[r];
-        }
-        store_piece<E, VEC>(static_cast<T*>(a.dx) + at * a.lddx, a.cols, i, t, nt, o);
+      for (int k = 0; k < 4; ++k) {
+        const F2 d = vfma(xh[i].v[k], k1, LAYER ? vfma(w[i].v[k], r2, k2) : w[i].v[k] * r2);
+        o[2 * k] = lo(d), o[2 * k + 1] = hi(d);
       }
+      RowWords<E, 8> d;
+      d.set(o);
+      store_row<E, 8, !ANY>(to, c, cols, d, 32, i > 0 ? &before : nullptr, i + 1 < NP && column<NP>(i + 1, t) - lane * 8 < cols);
+      if (ANY) before = d;
     }
+    to += all * a.lddx;
+    if (++at == depth) at = 0, pass ^= 1u;
   }
-
-  if (a.dgamma == nullptr && a.dbeta == nullptr) return;
-  // the teams' sums in their order, then this CTA's to its place among the partial sums (the
-  // outputs themselves where it is the only CTA)
+  if (ts.gave_up[team] && t == 0) atomicOr(a.status, kStatusTimeout);
+  if (!sums_wanted) return;
+  __syncthreads();  // the rings are done with
+  // the teams' sums in their order, then this CTA's to its place among the partial sums (the outputs
+  // themselves where it is the only CTA)
+  float* sums = reinterpret_cast<float*>(smem);  // [1 or 2][NP][8][nt]
   float* part = a.part + int64_t(blockIdx.x) * (LAYER ? 2 : 1) * a.part_cols;
   float* to_g = gridDim.x == 1 ? a.dgamma : part;
   float* to_b = gridDim.x == 1 ? a.dbeta : part + a.part_cols;
-  for (int q = 0; q < a.teams && a.teams > 1; ++q) {
+  float g8[NP][8], b8[NP][8];
+#pragma unroll
+  for (int i = 0; i < NP; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      g8[i][k] = k % 2 == 0 ? lo(dg[i].v[k / 2]) : hi(dg[i].v[k / 2]);
+      b8[i][k] = k % 2 == 0 ? lo(db[i].v[k / 2]) : hi(db[i].v[k / 2]);
+    }
+  for (int q = 0; q < teams && teams > 1; ++q) {
     if (q == team) {
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int at = (8 * i + k) * nt + t;
+          const int s = (8 * i + k) * nt + t;
           if (q > 0) {
-            dg[i][k] += sums[at];
-            if constexpr (LAYER) db[i][k] += sums[8 * NP * nt + at];
+            g8[i][k] += sums[s];
+            if constexpr (LAYER) b8[i][k] += sums[8 * NP * nt + s];
           }
-          sums[at] = dg[i][k];
-          if constexpr (LAYER) sums[8 * NP * nt + at] = db[i][k];
+          sums[s] = g8[i][k];
+          if constexpr (LAYER) sums[8 * NP * nt + s] = b8[i][k];
         }
       }
     }
     __syncthreads();
   }
-  if (team == a.teams - 1) {
+  if (team == teams - 1) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int64_t c = column<VEC>(i, k, t, nt);
-        if (c < a.cols) {
-          if (to_g != nullptr) to_g[c] = dg[i][k];
-          if (LAYER && to_b != nullptr) to_b[c] = db[i][k];
+        const int c = column<NP>(i, t) + k;
+        if (c < cols) {
+          if (to_g != nullptr) to_g[c] = g8[i][k];
+          if (LAYER && to_b != nullptr) to_b[c] = b8[i][k];
         }
       }
     }
   }
 }
 
-// out[c] = the sum of the `parts` partial rows at c, in a fixed order: eight threads a column
-// take every eighth row, and their sums are added in their order.  kinds: 1 (dgamma) or 2.
-__global__ void __launch_bounds__(256) roi_norm_sum_kernel(const float* part, int parts, int kinds, int64_t part_cols, int64_t cols,
+constexpr int kSumSegments = 16;
+// out[c] = the sum of the `parts` partial rows at c, in a fixed order: sixteen threads a column
+// take every sixteenth row, and their sums are added in their order.  kinds: 1 (dgamma) or 2.
+__global__ void __launch_bounds__(32 * kSumSegments) roi_norm_sum_kernel(const float* part, int parts, int kinds, int64_t part_cols, int64_t cols,
                                                            float* dgamma, float* dbeta) {
-  __shared__ float sums[8][33];
+  __shared__ float sums[kSumSegments][33];
   pdl_begin(true);  // the partial sums of the launch before
   const int lane = threadIdx.x & 31, seg = threadIdx.x >> 5;
   const int64_t blocks = (cols + 31) / 32;
@@ -515,19 +625,82 @@ __global__ void __launch_bounds__(256) roi_norm_sum_kernel(const float* part, in
   if (c < cols) {
     const float* p = part + kind * part_cols + c;
     const int64_t stride = kinds * part_cols;
-#pragma unroll 8
-    for (int q = seg; q < parts; q += 8) s += p[q * stride];
+#pragma unroll 10
+    for (int q = seg; q < parts; q += kSumSegments) s += p[q * stride];
   }
   sums[seg][lane] = s;
   __syncthreads();
   if (seg == 0 && c < cols) {
-    for (int q = 1; q < 8; ++q) s += sums[q][lane];
+    for (int q = 1; q < kSumSegments; ++q) s += sums[q][lane];
     float* out = kind == 0 ? dgamma : dbeta;
     if (out != nullptr) out[c] = s;
   }
 }
 
-// ---- rows past 8192 columns ----
+// ---- rows too wide for a ring ----
+// Sum over the CTA, the same bits in every thread.  Two sets of slots in turn: a set is written
+// again only after the barrier of the sum in between.
+__device__ __forceinline__ float cta_sum(float v, float (&slots)[2][32], int& turn) {
+  v = warp_sum(v);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (lane == 0) slots[turn][warp] = v;
+  __syncthreads();
+  v = warp_sum(lane < int(blockDim.x >> 5) ? slots[turn][lane] : 0.0f);
+  turn ^= 1;
+  return v;
+}
+
+template <Elem E, bool LAYER>
+__global__ void __launch_bounds__(kThreads) roi_norm_fwd_wide_kernel(FwdArgs a) {
+  using T = typename ElemType<E>::T;
+  __shared__ float slots[2][32];
+  pdl_begin(a.wait);
+  const int cols = int(a.cols), lane = threadIdx.x & 31;
+  const int end = a.xcodes != nullptr || a.ycodes != nullptr ? int(a.spitch) * 32 : cols;
+  const float inv_cols = 1.0f / float(cols);
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const T* x = static_cast<const T*>(a.x) + row * a.ldx;
+    T* y = static_cast<T*>(a.y) + row * a.ldy;
+    float mean = 0.0f;
+    if constexpr (LAYER) {
+      float s = 0.0f;
+#pragma unroll 4
+      for (int c = threadIdx.x; c < cols; c += blockDim.x) s += to_f32<E>(x[c]);
+      mean = cta_sum(s, slots, turn) * inv_cols;
+    }
+    float s = 0.0f;
+#pragma unroll 4
+    for (int c = threadIdx.x; c < cols; c += blockDim.x) {
+      const float d = to_f32<E>(x[c]) - mean;
+      s = __fmaf_rn(d, d, s);
+    }
+    const float rstd = 1.0f / sqrtf(cta_sum(s, slots, turn) * inv_cols + a.eps);
+    if (threadIdx.x == 0) {
+      if (LAYER && a.mean != nullptr) a.mean[row] = mean;
+      if (a.rstd != nullptr) a.rstd[row] = rstd;
+    }
+    // a warp a block of 32 columns, a lane a column
+    for (int c = threadIdx.x; c - lane < end; c += blockDim.x) {
+      const float v = c < cols ? to_f32<E>(x[c]) : 0.0f;
+      float o = 0.0f;
+      if (c < cols) {
+        const T r = from_f32<E>(__fmaf_rn((v - mean) * rstd, param1<E>(a.gamma, a.params32, c, 1.0f),
+                                          LAYER ? param1<E>(a.beta, a.params32, c, 0.0f) : 0.0f));
+        y[c] = r;
+        o = to_f32<E>(r);
+      }
+      auto save = [&](int8_t* codes, uint8_t* scales, float w) {
+        const uint32_t q = block8_scale(__reduce_max_sync(0xffffffffu, abs_bits(w)));
+        if (c < a.pitch) codes[row * a.pitch + c] = q == kScaleNaN ? int8_t(0) : int8_t(block8_code(w, block8_inverse(min(q, kScaleMax))));
+        if (lane == 0) scales[row * a.spitch + c / 32] = uint8_t(q);
+      };
+      if (a.xcodes != nullptr) save(a.xcodes, a.xscales, v);
+      if (a.ycodes != nullptr) save(a.ycodes, a.yscales, o);
+    }
+  }
+}
+
 template <Elem E, bool CKPT>
 __device__ __forceinline__ float x_at(const BwdArgs& a, int64_t row, int64_t c) {
   using T = typename ElemType<E>::T;
@@ -582,36 +755,76 @@ __global__ void __launch_bounds__(256) roi_norm_bwd_wide_sums_kernel(BwdArgs a) 
   if constexpr (LAYER) part[a.part_cols + c] = db;
 }
 
-bool aligned_rows(const void* p, int64_t ld, int64_t rows, int bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && (rows <= 1 || ld * bytes % 16 == 0);
+// Rows of whole granules.
+bool on_granules(const void* p, int64_t ld, int64_t rows, int64_t cols, int bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && cols * bytes % 16 == 0 && (rows <= 1 || ld * bytes % 16 == 0);
 }
 
-constexpr int64_t kHeldPieces = 4 * kFwdThreads;    // forward: what a CTA holds in registers
-constexpr int64_t kTeamCols = 2 * kTeamThreads * 8;  // backward: two pieces a thread
+// Shared memory that a CTA may take, less what the kernels declare.
+constexpr size_t kMostSmem = 232448 - 1024 - sizeof(TeamState);
 
-// Threads of a CTA or team for so many pieces, a whole number of warps.
-int threads_for(int64_t pieces, int most) {
-  const int64_t t = (pieces + 31) / 32 * 32;
-  return int(t < 32 ? 32 : t > most ? most : t);
+// `run` pieces of 256 columns a warp, at most `threads` threads; `least`: bytes that must be there.
+Shape shape_of(int64_t rows, int64_t cols, int64_t pieces, int run, int threads, size_t stage, size_t params, size_t least) {
+  Shape s;
+  s.stage = uint32_t(stage);
+  s.params = uint32_t(params);
+  const int64_t warps = (pieces + run - 1) / run;
+  s.depth = 0;
+  if (warps * 32 > threads - 32 || params + 2 * stage > kMostSmem || least > kMostSmem) return s;
+  s.nt = int(warps) * 32;
+  int64_t teams = (threads - 32) / s.nt;  // (a warp fills the rings)
+  const int64_t most = s.nt == 32 ? kMostTeams : kMostNamed, fit = int64_t((kMostSmem - params) / (2 * stage));
+  if (teams > most) teams = most;
+  if (teams > fit) teams = fit;
+  // no more teams than rows need
+  const int64_t cap = sm_count();
+  const int64_t need = (rows + cap - 1) / cap;
+  if (teams > need) teams = need;
+  s.teams = int(teams);
+  const int64_t depth = int64_t((kMostSmem - params) / (stage * size_t(teams)));
+  s.depth = int(depth > kMostDepth ? kMostDepth : depth);
+  const int64_t want = (rows + teams - 1) / teams;
+  s.grid = int(want < cap ? want : cap);
+  // no deeper than a team has rows
+  const int64_t each = (rows + s.grid * teams - 1) / (s.grid * teams);
+  if (s.depth > each) s.depth = int(each);
+  s.smem = params + stage * size_t(s.depth) * size_t(teams);
+  if (s.smem < least) s.smem = least;
+  return s;
 }
 
-template <Elem E, bool LAYER, bool VEC>
-int fwd(const NormFwdCall& c, const FwdArgs& a) {
+// Dynamic shared memory past the default limit, once for a kernel and device.
+template <class K>
+bool allow_smem(K kern, std::atomic<bool> (&done)[64]) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  if (done[dev].load(std::memory_order_acquire)) return true;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMostSmem)) != cudaSuccess) return false;
+  done[dev].store(true, std::memory_order_release);
+  return true;
+}
+
+template <Elem E, bool LAYER, bool ANY, int RUN>
+int fwd_run(const NormFwdCall& c, const FwdArgs& a) {
+  static std::atomic<bool> done[64];
+  auto kern = roi_norm_fwd_kernel<E, LAYER, ANY, RUN>;
+  if (!allow_smem(kern, done)) return -1;
+  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + 32, a.shape.smem, c.stream, a.wait, a);
+}
+
+template <Elem E, bool LAYER, bool ANY>
+int fwd(const NormFwdCall& c, FwdArgs& a) {
   // the padding of a checkpoint's scales is written too
-  const int64_t pieces = c.xcodes != nullptr || c.ycodes != nullptr ? a.spitch * 4 : (a.cols + 7) / 8;
-  int64_t grid = a.rows;
-  if (pieces > kHeldPieces) {
-    const int64_t cap = int64_t(sm_count()) * 4;
-    return launch_maybe_pdl(roi_norm_fwd_kernel<E, LAYER, VEC, 0>, int(grid < cap ? grid : cap), kFwdThreads, 0, c.stream,
-                            a.wait, a, int((pieces + kFwdThreads - 1) / kFwdThreads));
-  }
-  // few rows: one piece a thread, so that a row's loads and sums take the least time
-  const bool few = a.rows <= 2 * sm_count() && pieces <= kFwdThreads;
-  const int threads = threads_for(few ? pieces : (pieces + 3) / 4, kFwdThreads);
-  const int64_t cap = int64_t(sm_count()) * 32;
-  if (grid > cap) grid = cap;
-  return few ? launch_maybe_pdl(roi_norm_fwd_kernel<E, LAYER, VEC, 1>, int(grid), threads, 0, c.stream, a.wait, a, 1)
-             : launch_maybe_pdl(roi_norm_fwd_kernel<E, LAYER, VEC, 4>, int(grid), threads, 0, c.stream, a.wait, a, 4);
+  const int64_t end = c.xcodes != nullptr || c.ycodes != nullptr ? a.spitch * 32 : a.cols;
+  const int64_t pieces = (end + 255) / 256;
+  const size_t stage = size_t(a.cols + 7) / 8 * 8 * elem_bytes<E>() + (ANY ? 32 : 0);
+  const size_t params = size_t((a.cols + 255) / 256 * 256) * 4 * (LAYER ? 2 : 1);
+  // few rows: as many warps as there are pieces, so that a row's sums take the least time
+  const bool few = a.rows <= 2 * sm_count() && pieces < 32;
+  a.shape = shape_of(a.rows, a.cols, pieces, few ? 1 : kRun, few ? kThreads : kFwdThreads, stage, params, 0);
+  if (a.shape.depth > 0) return few ? fwd_run<E, LAYER, ANY, 1>(c, a) : fwd_run<E, LAYER, ANY, kRun>(c, a);
+  const int64_t cap = int64_t(sm_count()) * 2;
+  return launch_maybe_pdl(roi_norm_fwd_wide_kernel<E, LAYER>, int(a.rows < cap ? a.rows : cap), kThreads, 0, c.stream, a.wait, a);
 }
 
 template <Elem E>
@@ -621,59 +834,55 @@ int fwd_type(const NormFwdCall& c) {
   a.xcodes = c.xcodes, a.xscales = c.xscales, a.ycodes = c.ycodes, a.yscales = c.yscales;
   a.rows = c.rows, a.cols = c.cols, a.ldx = c.ldx, a.ldy = c.ldy;
   a.pitch = block8_pitch(c.cols), a.spitch = block8_scale_pitch(c.cols);
+  a.status = c.status;
   a.eps = c.eps;
   a.params32 = c.params32;
   a.wait = lone_pdl(c.stream);
-  const bool vec = aligned_rows(c.x, c.ldx, c.rows, elem_bytes<E>()) && aligned_rows(c.y, c.ldy, c.rows, elem_bytes<E>());
-  if (c.layer) return vec ? fwd<E, true, true>(c, a) : fwd<E, true, false>(c, a);
-  return vec ? fwd<E, false, true>(c, a) : fwd<E, false, false>(c, a);
+  const int b = elem_bytes<E>();
+  const bool any = !on_granules(c.x, c.ldx, c.rows, c.cols, b) || !on_granules(c.y, c.ldy, c.rows, c.cols, b);
+  if (c.layer) return any ? fwd<E, true, true>(c, a) : fwd<E, true, false>(c, a);
+  return any ? fwd<E, false, true>(c, a) : fwd<E, false, false>(c, a);
 }
 
-// CTAs of the backward, the teams in each (as many as 512 threads hold) and the pieces a
-// thread takes.  The partial sums are as many rows as there are CTAs.
-struct BwdShape {
-  int pieces, nt, teams, grid;
-};
-BwdShape bwd_shape(int64_t rows, int64_t cols) {
-  BwdShape s;
-  const int64_t pieces = (cols + 7) / 8;
-  s.pieces = pieces > kTeamThreads ? 2 : 1;
-  s.nt = threads_for((pieces + s.pieces - 1) / s.pieces, kTeamThreads);
-  s.teams = kTeamThreads / s.nt > 15 ? 15 : kTeamThreads / s.nt;
-  const int64_t want = (rows + s.teams - 1) / s.teams;
-  const int64_t cap = sm_count();
-  s.grid = int(want < cap ? want : cap);
-  return s;
-}
-int64_t wide_parts(int64_t rows) { return rows < 64 ? (rows < 1 ? 1 : rows) : 64; }
+int64_t wide_parts(int64_t rows) { return rows < 64 ? rows : 64; }
 
 int sum_parts(const BwdArgs& a, int parts, int kinds, cudaStream_t stream) {
   const int64_t grid = (a.cols + 31) / 32 * kinds;
-  return launch_maybe_pdl(roi_norm_sum_kernel, int(grid), 256, 0, stream, true, static_cast<const float*>(a.part), parts, kinds,
-                          a.part_cols, a.cols, a.dgamma, a.dbeta);
+  return launch_maybe_pdl(roi_norm_sum_kernel, int(grid), 32 * kSumSegments, 0, stream, true, static_cast<const float*>(a.part), parts,
+                          kinds, a.part_cols, a.cols, a.dgamma, a.dbeta);
 }
 
-template <Elem E, bool LAYER, bool CKPT>
-int bwd(const NormBwdCall& c, BwdArgs a, bool vec) {
+template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP>
+int bwd_run(const NormBwdCall& c, const BwdArgs& a) {
+  static std::atomic<bool> done[64];
+  auto kern = roi_norm_bwd_kernel<E, LAYER, CKPT, ANY, NP>;
+  if (!allow_smem(kern, done)) return -1;
+  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + 32, a.shape.smem, c.stream, a.wait, a);
+}
+
+template <Elem E, bool LAYER, bool CKPT, bool ANY>
+int bwd(const NormBwdCall& c, BwdArgs& a) {
   const bool sums = a.dgamma != nullptr || a.dbeta != nullptr;
   const int kinds = LAYER ? 2 : 1;
-  if (a.cols > kTeamCols) {
+  const size_t rowb = size_t(a.cols + 7) / 8 * 8 * elem_bytes<E>() + (ANY ? 32 : 0);
+  const size_t stage = rowb + (CKPT ? (size_t(a.pitch + a.spitch) + 15) / 16 * 16 + 32 : rowb);
+  const size_t params = size_t((a.cols + 255) / 256 * 256) * 4;
+  const int64_t pieces = (a.cols + 255) / 256;
+  const int np = pieces > 1 ? 2 : 1;
+  // (the teams' sums take the place of the rings)
+  a.shape = shape_of(a.rows, a.cols, pieces, np, kBwdThreads, stage, params, size_t(kinds) * 8 * size_t((pieces + np - 1) / np * np) * 32 * 4);
+  if (a.shape.depth == 0) {
     const int64_t cap = int64_t(sm_count()) * 2;
-    int n = launch_maybe_pdl(roi_norm_bwd_wide_kernel<E, LAYER, CKPT>, int(a.rows < cap ? a.rows : cap), 1024, 0, c.stream, a.wait, a);
+    const int n = launch_maybe_pdl(roi_norm_bwd_wide_kernel<E, LAYER, CKPT>, int(a.rows < cap ? a.rows : cap), 1024, 0, c.stream, a.wait, a);
     if (n < 0 || !sums) return n;
     const int parts = int(wide_parts(a.rows));
     roi_norm_bwd_wide_sums_kernel<E, LAYER, CKPT><<<dim3(unsigned((a.cols + 255) / 256), unsigned(parts)), 256, 0, c.stream>>>(a);
     if (cudaGetLastError() != cudaSuccess || sum_parts(a, parts, kinds, c.stream) < 0) return -1;
     return 3;
   }
-  const BwdShape s = bwd_shape(a.rows, a.cols);
-  a.teams = s.teams;
-  const size_t smem = s.teams > 1 && sums ? size_t(kinds) * 8 * s.pieces * s.nt * 4 : 0;
-  auto kern = s.pieces == 1 ? (vec ? roi_norm_bwd_kernel<E, LAYER, true, CKPT, 1, 2> : roi_norm_bwd_kernel<E, LAYER, false, CKPT, 1, 1>)
-                            : (vec ? roi_norm_bwd_kernel<E, LAYER, true, CKPT, 2, 1> : roi_norm_bwd_kernel<E, LAYER, false, CKPT, 2, 1>);
-  const int n = launch_maybe_pdl(kern, s.grid, s.nt * s.teams, smem, c.stream, a.wait, a);
-  if (n < 0 || !sums || s.grid == 1) return n;
-  return sum_parts(a, s.grid, kinds, c.stream) < 0 ? -1 : 2;
+  const int n = np == 1 ? bwd_run<E, LAYER, CKPT, ANY, 1>(c, a) : bwd_run<E, LAYER, CKPT, ANY, 2>(c, a);
+  if (n < 0 || !sums || a.shape.grid == 1) return n;
+  return sum_parts(a, a.shape.grid, kinds, c.stream) < 0 ? -1 : 2;
 }
 
 template <Elem E>
@@ -683,22 +892,26 @@ int bwd_type(const NormBwdCall& c) {
   a.dx = c.dx, a.dgamma = c.dgamma, a.dbeta = c.dbeta, a.part = static_cast<float*>(c.workspace);
   a.rows = c.rows, a.cols = c.cols, a.lddy = c.lddy, a.ldx = c.ldx, a.lddx = c.lddx;
   a.pitch = block8_pitch(c.cols), a.spitch = block8_scale_pitch(c.cols), a.part_cols = (c.cols + 3) / 4 * 4;
-  a.teams = 1;
+  a.status = c.status;
   a.params32 = c.params32;
   a.wait = lone_pdl(c.stream);
   const int b = elem_bytes<E>();
-  const bool vec = aligned_rows(c.dy, c.lddy, c.rows, b) && aligned_rows(c.dx, c.lddx, c.rows, b) &&
-                   (c.x == nullptr || aligned_rows(c.x, c.ldx, c.rows, b));
-  if (c.layer) return c.x == nullptr ? bwd<E, true, true>(c, a, vec) : bwd<E, true, false>(c, a, vec);
-  return c.x == nullptr ? bwd<E, false, true>(c, a, vec) : bwd<E, false, false>(c, a, vec);
+  const bool any = !on_granules(c.dy, c.lddy, c.rows, c.cols, b) || !on_granules(c.dx, c.lddx, c.rows, c.cols, b) ||
+                   (c.x != nullptr && !on_granules(c.x, c.ldx, c.rows, c.cols, b));
+  if (c.layer) {
+    if (c.x == nullptr) return any ? bwd<E, true, true, true>(c, a) : bwd<E, true, true, false>(c, a);
+    return any ? bwd<E, true, false, true>(c, a) : bwd<E, true, false, false>(c, a);
+  }
+  if (c.x == nullptr) return any ? bwd<E, false, true, true>(c, a) : bwd<E, false, true, false>(c, a);
+  return any ? bwd<E, false, false, true>(c, a) : bwd<E, false, false, false>(c, a);
 }
 
 }  // namespace
 
+// (one partial row a CTA, at most one CTA an SM; 64 for the widest rows)
 size_t norm_bwd_workspace_bytes(int64_t rows, int64_t cols) {
-  const int64_t part_cols = (cols + 3) / 4 * 4;
-  const int64_t parts = cols > kTeamCols ? wide_parts(rows) : bwd_shape(rows, cols).grid;
-  return size_t(parts) * 2 * size_t(part_cols) * 4;
+  const int64_t most = sm_count() > 64 ? sm_count() : 64;
+  return size_t(rows < most ? rows : most) * 2 * size_t((cols + 3) / 4 * 4) * 4;
 }
 
 int launch_norm_fwd(const NormFwdCall& c) {

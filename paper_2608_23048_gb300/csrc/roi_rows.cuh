@@ -126,15 +126,22 @@ struct Window {
 
 // All lanes of a warp, in groups of `width` (a power of two) with a row each: lane l of a group
 // puts its N elements at columns c = c_0 + N l on.  Lanes may lie past the end (cols < 0: no row).
+// A warp that goes along a row piece by piece (width 32) gives the piece before in `prev`, whose
+// last lane's end belongs to lane 0's first granule, and says with `more` that another follows.
 template <Elem E, int N, bool ALIGNED>
-__device__ __forceinline__ void store_row(typename ElemType<E>::T* row, int64_t c, int64_t cols, const RowWords<E, N>& r, int width = 32) {
+__device__ __forceinline__ void store_row(typename ElemType<E>::T* row, int64_t c, int64_t cols, const RowWords<E, N>& r, int width = 32,
+                                          const RowWords<E, N>* prev = nullptr, bool more = false) {
   constexpr int W = RowWords<E, N>::kWords, kPer = 16 / elem_bytes<E>();  // elements of a granule
   const int64_t left = cols - c;
   typename ElemType<E>::T* p = row + c;
   uint32_t s[W + 4];  // the end of the lane before, and this lane's words
   if constexpr (!ALIGNED) {
+    const int lane = threadIdx.x & (width - 1);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = __shfl_up_sync(0xffffffffu, r.u[W - 4 + i], 1, width);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t own = r.u[W - 4 + i];
+      s[i] = __shfl_sync(0xffffffffu, prev != nullptr && lane == width - 1 ? prev->u[W - 4 + i] : own, (lane + width - 1) & (width - 1), width);
+    }
 #pragma unroll
     for (int i = 0; i < W; ++i) s[4 + i] = r.u[i];
   }
@@ -151,24 +158,25 @@ __device__ __forceinline__ void store_row(typename ElemType<E>::T* row, int64_t 
     }
   } else if constexpr (!ALIGNED) {
     const int lane = threadIdx.x & (width - 1);
+    const bool first = lane == 0 && prev == nullptr;  // nothing comes before
     RowWords<E, N> g;  // the granules from p - m on
     shift_words<W>(s, 16u - m, g.u);
     const int before = int(m) / elem_bytes<E>();  // elements of the lane before
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) {
       const int from = i * kPer - before;  // the granule's first column, relative to c
-      if ((i > 0 || lane > 0) && left >= from + kPer) {
+      if ((i > 0 || !first) && left >= from + kPer) {
         reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) - m)[i] =
             make_uint4(g.u[4 * i], g.u[4 * i + 1], g.u[4 * i + 2], g.u[4 * i + 3]);
-      } else {
+      } else if (left > from) {
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
           const int k = from + e;
-          if ((i > 0 || lane > 0 || k >= 0) && k < left) p[k] = g.at(i * kPer + e);
+          if ((i > 0 || !first || k >= 0) && k < left) p[k] = g.at(i * kPer + e);
         }
       }
     }
-    if (lane == width - 1) {  // its end has no lane after it
+    if (lane == width - 1 && !more) {  // its end has no lane after it
 #pragma unroll
       for (int k = N - kPer; k < N; ++k)
         if (k >= N - before && k < left) p[k] = r.at(k);
