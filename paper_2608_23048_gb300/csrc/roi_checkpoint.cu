@@ -55,20 +55,16 @@ __device__ __forceinline__ void walk(int64_t row0, int64_t rem0, uint32_t i, int
   }
 }
 
-// Codes and scale of the piece whose values are v (all lanes of the warp); `q` is its place in the row.
-__device__ __forceinline__ void save_piece(const SaveArgs& a, const float (&v)[16], int64_t row, int64_t q) {
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) top = max(top, abs_bits(v[i]));
+// Codes and scale of a piece (all lanes of the warp); `q` is its place in the row.
+template <Elem E>
+__device__ __forceinline__ void save_piece(const SaveArgs& a, const RowWords<E, 16>& r, int64_t row, int64_t q) {
+  uint32_t top = max_bits(r);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   const uint32_t s = block8_scale(top);
-  const float inverse = block8_inverse(min(s, kScaleMax));
-  const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
+  uint32_t w[4];
+  block8_codes(r, top, s, w);
   if (row < a.rows && q < a.pieces) {
-    if (16 * q < a.pitch)
-      *reinterpret_cast<uint4*>(a.codes + row * a.pitch + 16 * q) =
-          make_uint4(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep), block8_codes4(v + 8, inverse, keep),
-                     block8_codes4(v + 12, inverse, keep));
+    if (16 * q < a.pitch) *reinterpret_cast<uint4*>(a.codes + row * a.pitch + 16 * q) = make_uint4(w[0], w[1], w[2], w[3]);
     if ((q & 1) == 0) a.scales[row * a.spitch + (q >> 1)] = uint8_t(s);
   }
 }
@@ -109,9 +105,7 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_kernel(SaveArgs 
     }
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      float v[16];
-      r[u].get(v);
-      save_piece(a, v, row[u], j[u]);
+      save_piece<E>(a, r[u], row[u], j[u]);
     }
   }
 }
@@ -186,10 +180,8 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_rows_kernel(Save
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       RowWords<E, 16> r;
-      float v[16];
       x[u].get(r);
-      r.get(v);
-      save_piece(a, v, row[u], j[u]);
+      save_piece<E>(a, r, row[u], j[u]);
     }
   }
 }
@@ -239,7 +231,7 @@ bool in_sectors(const void* p, int64_t ld, int64_t rows, int bytes) {
 // goes over it in segments.  Returns the tiles of the launch.
 template <class Args>
 int64_t by_rows(Args& a) {
-  a.width = 1;
+  a.width = 8;
   while (a.width < 32 && a.width < a.pieces) a.width *= 2;
   a.segments = int((a.pieces + 31) / 32);
   const int64_t per = 32 / a.width;

@@ -36,6 +36,7 @@ namespace {
 struct Shape {
   int nt;         // threads of a team
   int teams;      // of a CTA
+  int fillers;    // warps that fill the rings, after the teams
   int depth;      // rows of a team's ring, 0 where two do not fit
   int grid;
   uint32_t stage; // bytes of a row in the ring
@@ -191,18 +192,13 @@ __device__ __forceinline__ RowWords<E, 8> read_row(const uint8_t* st, uint32_t m
 // are 0): a block is four neighbouring lanes.
 template <Elem E>
 __device__ __forceinline__ void save_piece(int8_t* codes, uint8_t* scales, int64_t pitch, int64_t spitch, int c, const RowWords<E, 8>& r) {
-  float v[8];
-  r.get(v);
-  uint32_t top = 0;
-#pragma unroll
-  for (int k = 0; k < 8; ++k) top = max(top, abs_bits(v[k]));
+  uint32_t top = max_bits(r);
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
   top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
   const uint32_t s = block8_scale(top);
-  const float inverse = block8_inverse(min(s, kScaleMax));
-  const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
-  if (c < pitch)
-    *reinterpret_cast<uint2*>(codes + c) = make_uint2(block8_codes4(v, inverse, keep), block8_codes4(v + 4, inverse, keep));
+  uint32_t w[2];
+  block8_codes(r, top, s, w);
+  if (c < pitch) *reinterpret_cast<uint2*>(codes + c) = make_uint2(w[0], w[1]);
   if (c % 32 == 0 && c / 32 < spitch) scales[c / 32] = uint8_t(s);
 }
 
@@ -216,7 +212,10 @@ __device__ __forceinline__ void team_sync(int team, int nt) {
 
 // Pieces a lane of the forward holds, and the most threads of a CTA: what keeps the registers that a
 // thread then has from spilling.
-constexpr int kRun = 4, kFwdThreads = 768;
+template <Elem E>
+constexpr int kRun = E == Elem::kFp32 ? 2 : 4;
+template <bool LAYER, bool ANY>
+constexpr int kFwdThreads = LAYER && ANY ? 640 : 768;
 constexpr int kThreads = 1024, kMostTeams = 32, kMostNamed = 15, kMostDepth = 8;
 // Barriers, slots and flags of the teams.
 struct TeamState {
@@ -235,11 +234,12 @@ __device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
   fence_mbar_init();
   __syncthreads();
 }
-// The warp that fills the rings, a lane a team: `copy(team, stage, row, barrier)` sends a row's copies
-// off.  It gives up when no stage has become free for `lim`; what was sent off lands before it leaves.
+// A warp that fills rings, a lane a team: `copy(team, stage, row, barrier)` sends a row's copies off.  It
+// gives up when no stage has become free for `lim`; what was sent off lands before it leaves.  (A
+// copy takes a warp some 70 cycles to send off, so the many teams of narrow rows have several.)
 template <class Copy>
 __device__ __forceinline__ void fill_rings(TeamState& ts, const Shape& s, int64_t rows, uint64_t lim, unsigned int* status, Copy copy) {
-  const int team = threadIdx.x & 31;
+  const int team = int(threadIdx.x & 31) * s.fillers + (int(threadIdx.x) - s.teams * s.nt) / 32;
   const int64_t all = int64_t(gridDim.x) * s.teams;
   int64_t row = team < s.teams ? int64_t(blockIdx.x) * s.teams + team : rows;
   int at = 0, k = 0;
@@ -266,12 +266,12 @@ __device__ __forceinline__ void fill_rings(TeamState& ts, const Shape& s, int64_
     // (a stage's phases end one after another, so the last rows of the ring stand for all)
     for (int q = k > s.depth ? k - s.depth : 0; q < k; ++q) mbar_wait_bounded(&ts.full[team][q % s.depth], uint32_t(q / s.depth) & 1u);
   }
-  if (gave_up && team == 0) atomicOr(status, kStatusTimeout);
+  if (gave_up && (threadIdx.x & 31) == 0) atomicOr(status, kStatusTimeout);
 }
 
 // RUN pieces a lane.
 template <Elem E, bool LAYER, bool ANY, int RUN>
-__global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads) roi_norm_fwd_kernel(FwdArgs a) {
+__global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>) roi_norm_fwd_kernel(FwdArgs a) {
   using T = typename ElemType<E>::T;
   extern __shared__ __align__(128) uint8_t smem[];  // gamma, beta; [teams][depth][stage]
   __shared__ TeamState ts;
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads) roi_norm_fw
   stage_param<E>(gamma, a.gamma, a.params32, cols, padded, 1.0f);
   if constexpr (LAYER) stage_param<E>(beta, a.beta, a.params32, cols, padded, 0.0f);
   __syncthreads();
-  if (team == a.shape.teams) {
+  if (team >= a.shape.teams) {
     fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
       uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
       const bool first = row == 0, last = row == a.rows - 1;
@@ -409,10 +409,11 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads) roi_norm_fw
 template <int NP>
 __device__ __forceinline__ int column(int i, int t) { return ((t >> 5) * NP + i) * 256 + (t & 31) * 8; }
 
-constexpr int kBwdThreads = 512;
 
-template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP>
-__global__ void __launch_bounds__(kBwdThreads) roi_norm_bwd_kernel(BwdArgs a) {
+// THREADS: what leaves two pieces a thread their registers, 512 with the sums of dbeta and 640 without
+// (two teams at 3584 columns); 1024 for one piece, and for rows too wide for these.
+template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP, int THREADS>
+__global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
   using T = typename ElemType<E>::T;
   extern __shared__ __align__(128) uint8_t smem[];  // gamma; [teams][depth][stage]; at the end the teams' sums
   __shared__ TeamState ts;
@@ -428,7 +429,7 @@ __global__ void __launch_bounds__(kBwdThreads) roi_norm_bwd_kernel(BwdArgs a) {
   __syncthreads();
   const int teams = a.shape.teams;
   const bool sums_wanted = a.dgamma != nullptr || a.dbeta != nullptr;
-  if (team == teams) {
+  if (team >= teams) {
     fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
       uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
       const bool first = row == 0, last = row == a.rows - 1;
@@ -780,6 +781,9 @@ Shape shape_of(int64_t rows, int64_t cols, int64_t pieces, int run, int threads,
   const int64_t cap = sm_count();
   const int64_t need = (rows + cap - 1) / cap;
   if (teams > need) teams = need;
+  // a filling warp for every eight teams
+  s.fillers = int((teams + 7) / 8);
+  while (teams * s.nt + s.fillers * 32 > threads) --teams;
   s.teams = int(teams);
   const int64_t depth = int64_t((kMostSmem - params) / (stage * size_t(teams)));
   s.depth = int(depth > kMostDepth ? kMostDepth : depth);
@@ -809,7 +813,7 @@ int fwd_run(const NormFwdCall& c, const FwdArgs& a) {
   static std::atomic<bool> done[64];
   auto kern = roi_norm_fwd_kernel<E, LAYER, ANY, RUN>;
   if (!allow_smem(kern, done)) return -1;
-  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + 32, a.shape.smem, c.stream, a.wait, a);
+  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + a.shape.fillers * 32, a.shape.smem, c.stream, a.wait, a);
 }
 
 template <Elem E, bool LAYER, bool ANY>
@@ -821,8 +825,8 @@ int fwd(const NormFwdCall& c, FwdArgs& a) {
   const size_t params = size_t((a.cols + 255) / 256 * 256) * 4 * (LAYER ? 2 : 1);
   // few rows: as many warps as there are pieces, so that a row's sums take the least time
   const bool few = a.rows <= 2 * sm_count() && pieces < 32;
-  a.shape = shape_of(a.rows, a.cols, pieces, few ? 1 : kRun, few ? kThreads : kFwdThreads, stage, params, 0);
-  if (a.shape.depth > 0) return few ? fwd_run<E, LAYER, ANY, 1>(c, a) : fwd_run<E, LAYER, ANY, kRun>(c, a);
+  a.shape = shape_of(a.rows, a.cols, pieces, few ? 1 : kRun<E>, few ? kThreads : kFwdThreads<LAYER, ANY>, stage, params, 0);
+  if (a.shape.depth > 0) return few ? fwd_run<E, LAYER, ANY, 1>(c, a) : fwd_run<E, LAYER, ANY, kRun<E>>(c, a);
   const int64_t cap = int64_t(sm_count()) * 2;
   return launch_maybe_pdl(roi_norm_fwd_wide_kernel<E, LAYER>, int(a.rows < cap ? a.rows : cap), kThreads, 0, c.stream, a.wait, a);
 }
@@ -852,12 +856,12 @@ int sum_parts(const BwdArgs& a, int parts, int kinds, cudaStream_t stream) {
                           kinds, a.part_cols, a.cols, a.dgamma, a.dbeta);
 }
 
-template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP>
+template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP, int THREADS>
 int bwd_run(const NormBwdCall& c, const BwdArgs& a) {
   static std::atomic<bool> done[64];
-  auto kern = roi_norm_bwd_kernel<E, LAYER, CKPT, ANY, NP>;
+  auto kern = roi_norm_bwd_kernel<E, LAYER, CKPT, ANY, NP, THREADS>;
   if (!allow_smem(kern, done)) return -1;
-  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + 32, a.shape.smem, c.stream, a.wait, a);
+  return launch_maybe_pdl(kern, a.shape.grid, a.shape.nt * a.shape.teams + a.shape.fillers * 32, a.shape.smem, c.stream, a.wait, a);
 }
 
 template <Elem E, bool LAYER, bool CKPT, bool ANY>
@@ -870,7 +874,10 @@ int bwd(const NormBwdCall& c, BwdArgs& a) {
   const int64_t pieces = (a.cols + 255) / 256;
   const int np = pieces > 1 ? 2 : 1;
   // (the teams' sums take the place of the rings)
-  a.shape = shape_of(a.rows, a.cols, pieces, np, kBwdThreads, stage, params, size_t(kinds) * 8 * size_t((pieces + np - 1) / np * np) * 32 * 4);
+  const size_t least = size_t(kinds) * 8 * size_t((pieces + np - 1) / np * np) * 32 * 4;
+  const int64_t nt = (pieces + np - 1) / np * 32;
+  const int threads = np == 1 || nt > 608 ? 1024 : LAYER && nt <= 240 ? 512 : 640;
+  a.shape = shape_of(a.rows, a.cols, pieces, np, threads, stage, params, least);
   if (a.shape.depth == 0) {
     const int64_t cap = int64_t(sm_count()) * 2;
     const int n = launch_maybe_pdl(roi_norm_bwd_wide_kernel<E, LAYER, CKPT>, int(a.rows < cap ? a.rows : cap), 1024, 0, c.stream, a.wait, a);
@@ -880,7 +887,11 @@ int bwd(const NormBwdCall& c, BwdArgs& a) {
     if (cudaGetLastError() != cudaSuccess || sum_parts(a, parts, kinds, c.stream) < 0) return -1;
     return 3;
   }
-  const int n = np == 1 ? bwd_run<E, LAYER, CKPT, ANY, 1>(c, a) : bwd_run<E, LAYER, CKPT, ANY, 2>(c, a);
+  int n;
+  if (np == 1) n = bwd_run<E, LAYER, CKPT, ANY, 1, 1024>(c, a);
+  else if (threads == 1024) n = bwd_run<E, LAYER, CKPT, ANY, 2, 1024>(c, a);
+  else if (!LAYER || threads == 640) n = bwd_run<E, LAYER, CKPT, ANY, 2, 640>(c, a);
+  else n = bwd_run<E, true, CKPT, ANY, 2, 512>(c, a);
   if (n < 0 || !sums || a.shape.grid == 1) return n;
   return sum_parts(a, a.shape.grid, kinds, c.stream) < 0 ? -1 : 2;
 }

@@ -75,6 +75,46 @@ struct RowWords {
   }
 };
 
+// The bits, as float32, of the largest magnitude (a NaN's are above all).
+template <Elem E, int N>
+__device__ __forceinline__ uint32_t max_bits(const RowWords<E, N>& r) {
+  constexpr int W = RowWords<E, N>::kWords;
+  if constexpr (E == Elem::kFp32) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i) top = max(top, r.u[i] & 0x7fffffffu);
+    return top;
+  } else {
+    // two halves a step; as integers, magnitudes are in the order of their bits
+    uint32_t t = r.u[0] & 0x7fff7fffu;
+#pragma unroll
+    for (int i = 1; i < W; ++i) t = __vmaxu2(t, r.u[i] & 0x7fff7fffu);
+    const uint32_t half = max(t >> 16, t & 0xffffu);
+    return abs_bits(to_f32<E>(uint16_t(half)));
+  }
+}
+// The codes of a piece of a block whose largest magnitude has the bits `top` and whose scale byte is s (all lanes).
+template <Elem E, int N>
+__device__ __forceinline__ void block8_codes(const RowWords<E, N>& r, uint32_t top, uint32_t s, uint32_t (&w)[N / 4]) {
+  const float inverse = block8_inverse(min(s, kScaleMax));
+  const uint32_t keep = s == kScaleNaN ? 0u : 0xffffffffu;
+  float v[N];
+  r.get(v);
+  // only a magnitude past 127 steps can round past the last code: rare, and the same for the block
+  if (__any_sync(0xffffffffu, !(__uint_as_float(top) * inverse <= 127.0f))) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = block8_codes4(v + 4 * i, inverse, keep);
+  } else {
+    const F2 k = f2(inverse), magic = f2(12582912.0f);
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+      const F2 a = vfma(f2(v[4 * i], v[4 * i + 1]), k, magic), b = vfma(f2(v[4 * i + 2], v[4 * i + 3]), k, magic);
+      w[i] = __byte_perm(__byte_perm(__float_as_uint(lo(a)), __float_as_uint(hi(a)), 0x0040),
+                         __byte_perm(__float_as_uint(lo(b)), __float_as_uint(hi(b)), 0x0040), 0x5410);
+    }
+  }
+}
+
 // N elements from column c of a row on, on their way: ALIGNED (rows start on 16-byte boundaries) as
 // they are, else the granules around them.
 template <Elem E, int N, bool ALIGNED>
@@ -135,12 +175,15 @@ __device__ __forceinline__ void store_row(typename ElemType<E>::T* row, int64_t 
   const int64_t left = cols - c;
   typename ElemType<E>::T* p = row + c;
   uint32_t s[W + 4];  // the end of the lane before, and this lane's words
+  const int lane = threadIdx.x & (width - 1);
+  uint32_t h[4], e[4];  // the group's first and last granule of words, in all its lanes
   if constexpr (!ALIGNED) {
-    const int lane = threadIdx.x & (width - 1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t own = r.u[W - 4 + i];
       s[i] = __shfl_sync(0xffffffffu, prev != nullptr && lane == width - 1 ? prev->u[W - 4 + i] : own, (lane + width - 1) & (width - 1), width);
+      if (prev == nullptr) h[i] = __shfl_sync(0xffffffffu, r.u[i], 0, width);
+      if (!more) e[i] = __shfl_sync(0xffffffffu, own, width - 1, width);
     }
 #pragma unroll
     for (int i = 0; i < W; ++i) s[4 + i] = r.u[i];
@@ -157,30 +200,33 @@ __device__ __forceinline__ void store_row(typename ElemType<E>::T* row, int64_t 
         if (i < left) p[i] = r.at(i);
     }
   } else if constexpr (!ALIGNED) {
-    const int lane = threadIdx.x & (width - 1);
-    const bool first = lane == 0 && prev == nullptr;  // nothing comes before
     RowWords<E, N> g;  // the granules from p - m on
     shift_words<W>(s, 16u - m, g.u);
     const int before = int(m) / elem_bytes<E>();  // elements of the lane before
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) {
       const int from = i * kPer - before;  // the granule's first column, relative to c
-      if ((i > 0 || !first) && left >= from + kPer) {
+      const bool head = i == 0 && lane == 0 && prev == nullptr;
+      if (!head && left >= from + kPer) {
         reinterpret_cast<uint4*>(reinterpret_cast<uintptr_t>(p) - m)[i] =
             make_uint4(g.u[4 * i], g.u[4 * i + 1], g.u[4 * i + 2], g.u[4 * i + 3]);
-      } else if (left > from) {
+      } else if (!head && left > from) {
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-          const int k = from + e;
-          if ((i > 0 || !first || k >= 0) && k < left) p[k] = g.at(i * kPer + e);
-        }
+        for (int k = 0; k < kPer; ++k)
+          if (from + k < left) p[from + k] = g.at(i * kPer + k);
       }
     }
-    if (lane == width - 1 && !more) {  // its end has no lane after it
-#pragma unroll
-      for (int k = N - kPer; k < N; ++k)
-        if (k >= N - before && k < left) p[k] = r.at(k);
-    }
+    // what has no lane before or after it, an element a lane (groups have eight lanes at least)
+    auto element = [&](const uint32_t (&w)[4]) {
+      const int at = E == Elem::kFp32 ? lane : lane >> 1;
+      const uint32_t v = at == 0 ? w[0] : at == 1 ? w[1] : at == 2 ? w[2] : w[3];
+      if constexpr (E == Elem::kFp32) return __uint_as_float(v);
+      else return uint16_t(lane & 1 ? v >> 16 : v);
+    };
+    const int64_t left0 = left + int64_t(lane) * N;  // of lane 0
+    if (prev == nullptr && lane < kPer - before && lane < left0) (p - lane * N)[lane] = element(h);
+    const int64_t k = int64_t(width) * N - kPer + lane;  // relative to lane 0
+    if (!more && lane < kPer && lane >= kPer - before && k < left0) (p - lane * N)[k] = element(e);
   }
 }
 
