@@ -52,68 +52,6 @@ __device__ __forceinline__ typename ElemType<E>::T from_f32(float v) {
   if constexpr (E == Elem::kFp32) return v;
 }
 
-// Eight consecutive elements as they lie in memory (16-byte aligned).
-template <Elem E>
-struct Raw8 {
-  uint4 w[elem_bytes<E>() / 2];
-  __device__ __forceinline__ void load(const typename ElemType<E>::T* p) {
-#pragma unroll
-    for (int i = 0; i < elem_bytes<E>() / 2; ++i) w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
-  }
-  __device__ __forceinline__ void store(typename ElemType<E>::T* p) const {
-#pragma unroll
-    for (int i = 0; i < elem_bytes<E>() / 2; ++i) reinterpret_cast<uint4*>(p)[i] = w[i];
-  }
-  __device__ __forceinline__ void zero() {
-#pragma unroll
-    for (int i = 0; i < elem_bytes<E>() / 2; ++i) w[i] = make_uint4(0, 0, 0, 0);
-  }
-  __device__ __forceinline__ uint32_t word(int i) const {
-    const uint4& q = w[i / 4];
-    return i % 4 == 0 ? q.x : i % 4 == 1 ? q.y : i % 4 == 2 ? q.z : q.w;
-  }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    if constexpr (E == Elem::kFp32) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(word(i));
-    } else if constexpr (E == Elem::kBf16) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(word(i) << 16);
-        v[2 * i + 1] = __uint_as_float(word(i) & 0xffff0000u);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t u = word(i);
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u));
-        v[2 * i] = f.x, v[2 * i + 1] = f.y;
-      }
-    }
-  }
-  __device__ __forceinline__ void set(const float (&v)[8]) {
-    uint32_t u[elem_bytes<E>() * 2];
-    if constexpr (E == Elem::kFp32) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (E == Elem::kBf16) {
-          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-          u[i] = *reinterpret_cast<const uint32_t*>(&b);
-        } else {
-          const __half2 h = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
-          u[i] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < elem_bytes<E>() / 2; ++i)
-      w[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-  }
-};
-
 // The scale byte of a block from the bits of its largest magnitude (a NaN's bits are above
 // an infinity's, so their maximum as integers finds both).
 constexpr uint32_t kInfBits = 0x7f800000u;
@@ -141,10 +79,6 @@ __device__ __forceinline__ uint32_t block8_codes4(const float* x, float inverse,
   const uint32_t a = __byte_perm(block8_code(x[0], inverse), block8_code(x[1], inverse), 0x0040);
   const uint32_t b = __byte_perm(block8_code(x[2], inverse), block8_code(x[3], inverse), 0x0040);
   return __byte_perm(a, b, 0x5410) & keep;
-}
-// The value of code byte `i` of a word of codes.
-__device__ __forceinline__ float block8_value(uint32_t word, int i, float step) {
-  return float(int8_t(word >> (8 * i))) * step;
 }
 // The values of the four codes of a word, in pairs.  A code's byte, its sign bit turned, in the
 // mantissa of 2^23 is 2^23 + 128 + the code; difference and product are exact.

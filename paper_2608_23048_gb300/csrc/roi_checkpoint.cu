@@ -74,7 +74,12 @@ __device__ __forceinline__ void load_piece(const uint4& q, uint32_t s, RowWords<
   const uint32_t w[4] = {q.x, q.y, q.z, q.w};
   float v[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v[i] = block8_clip<E>(block8_value(w[i / 4], i % 4, step));
+  for (int i = 0; i < 4; ++i) {
+    F2 a, b;
+    block8_pairs(w[i], step, a, b);
+    v[4 * i] = block8_clip<E>(lo(a)), v[4 * i + 1] = block8_clip<E>(hi(a));
+    v[4 * i + 2] = block8_clip<E>(lo(b)), v[4 * i + 3] = block8_clip<E>(hi(b));
+  }
   r.set(v);
 }
 

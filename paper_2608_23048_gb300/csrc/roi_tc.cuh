@@ -123,53 +123,32 @@ __host__ __device__ constexpr uint32_t tc_idesc_bf16_f32_mn(int m, int n) {
   return tc_idesc_bf16_f32(m, n) | (1u << 15) | (1u << 16);
 }
 
-template <int CG>
-__device__ __forceinline__ void tc_alloc_group(uint32_t* dst_smem, uint32_t ncols) {
-  if constexpr (CG == 1) {
-    tc_alloc(dst_smem, ncols);
-  } else {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst_smem)),
-                 "r"(ncols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-  }
+// TMEM of a pair: one warp of each CTA allocates, and frees, the same columns in both.
+__device__ __forceinline__ void tc_alloc_pair(uint32_t* dst_smem, uint32_t ncols) {
+  asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(dst_smem)), "r"(ncols)
+               : "memory");
+  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
 }
-template <int CG>
-__device__ __forceinline__ void tc_dealloc_group(uint32_t taddr, uint32_t ncols) {
-  if constexpr (CG == 1) {
-    tc_dealloc(taddr, ncols);
-  } else {
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
-  }
+__device__ __forceinline__ void tc_dealloc_pair(uint32_t taddr, uint32_t ncols) {
+  asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
-// One M x N x 16 step; with a pair, issued by one thread of the even CTA for both (M and N
-// over the pair: each CTA holds half of A's rows, half of B's, and half of D's rows).
-template <int CG>
-__device__ __forceinline__ void tc_mma_bf16_group(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                                  bool accumulate) {
-  if constexpr (CG == 1) {
-    tc_mma_bf16(d_tmem, a_desc, b_desc, idesc, accumulate);
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(uint32_t(accumulate))
-        : "memory");
-  }
+// One M x N x 16 step of a pair, issued by one thread of the even CTA for both (M and N over the
+// pair: each CTA holds half of A's rows, half of B's, and half of D's rows).
+__device__ __forceinline__ void tc_mma_bf16_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                 bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(uint32_t(accumulate))
+      : "memory");
 }
-// The mbarrier (of both CTAs of a pair) receives one arrival when every MMA this thread issued
-// so far is done.
-template <int CG>
-__device__ __forceinline__ void tc_commit_group(uint64_t* bar) {
-  if constexpr (CG == 1) {
-    tc_commit(bar);
-  } else {
-    asm volatile(
-        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
-            smem_addr(bar)),
-        "h"(uint16_t(3))
-        : "memory");
-  }
+// The mbarrier of both CTAs receives one arrival when every MMA this thread issued so far is done.
+__device__ __forceinline__ void tc_commit_pair(uint64_t* bar) {
+  asm volatile(
+      "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(
+          smem_addr(bar)),
+      "h"(uint16_t(3))
+      : "memory");
 }
 // 32 consecutive fp32 columns of this warp's 32 TMEM lanes.
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t (&v)[32]) {

@@ -4,19 +4,26 @@
 // on the way into shared memory; its values have 7 bits and a sign, so bf16 holds them exactly
 // and the product is that of dY with the checkpoint's own values.
 //
-// One or two CTAs (CG; a pair shares its MMAs, cta_group::2) own a tile of 128 CG outputs x
-// 128 CG inputs; each CTA holds 128 outputs of dY, 128 inputs of x^ and, in TMEM, 128 rows of
-// the sums, 128 CG columns wide.  Both operands are MN-major (a token's row is contiguous
-// along outputs or inputs), in tiles of 64 tokens with 128-byte swizzle.
+// A pair of CTAs shares its MMAs (cta_group::2) and owns a tile of 256 outputs x 256 inputs; each CTA
+// holds 128 outputs of dY, 128 inputs of x^ and, in TMEM, 128 rows of the sums, 256 columns wide.
+// Both operands are MN-major (a token's row is contiguous along outputs or inputs), in tiles of 64
+// tokens with 128-byte swizzle.
 //
-// Roles of the 14 warps of a CTA, each a loop over the same list of tiles and chunks of tokens:
-//   warp 0        stages dY and the codes of a chunk by TMA (rows past the last token, and
-//                 columns past the last, as zeros), `full`
-//   warps 2 - 9   turn the codes into bf16 in the layout of the MMA, `ready`
-//   warp 1        issues four MMAs of 16 tokens a chunk (in a pair, the even CTA's for both),
-//                 commits them to `empty` and after the last chunk to `sum`
-//   warps 10 - 13 read the sums from TMEM and write them out, `free`, while the next tile's
+// Roles of the 18 warps of a CTA, each a loop over the same list of tiles and chunks of 64 tokens:
+//   warp 0        stages dY by TMA (rows past the last token, columns past the last as zeros)
+//   warp 12       stages the codes by TMA, and their scales by asynchronous copies of words
+//   warps 2 - 11  five sets of two, each every fifth chunk: codes to bf16 in the layout of the MMA,
+//                 into one of three slots; with warp 13, which says so of dY, they make a chunk `ready`
+//   warp 1        of the even CTA: four MMAs of 16 tokens a chunk for both; commits them to `dy_empty`,
+//                 which frees dY's stage and the slot, and after the last chunk to `sum`
+//   warps 14 - 17 read the sums from TMEM and write them out, `free`, while the next tile's
 //                 MMAs go to the other half of TMEM
+// What it took to feed the tensor cores (8192 tokens, 18944 x 3584; the measured cuBLAS rate would be
+// 589 us): codes and scales through registers of the converting warps, a cluster-wide release a
+// chunk 1888 us; without that release 982; two sets of converting warps and the scales staged apart
+// 867; even bytes converted where they are 727; rings of their own and loops of whole warps
+// around the MMAs, so that descriptors stay in uniform registers, 631; whole sectors out 583 to 600,
+// which is 1860 to 1910 TFLOP/s.  Under a long load the clock falls with the power (681 us).
 // Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
 //
 // Tiles go to the groups (CTAs or pairs) in rounds.  In the last, partial round the tokens of
@@ -33,24 +40,18 @@ namespace roi {
 namespace {
 
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
+constexpr int kSide = 2 * kEdge;           // of a pair's tile
 constexpr int kChunk = 64;                 // tokens a stage
-#ifndef ROI_WGRAD_CODES
-#define ROI_WGRAD_CODES 10
-#define ROI_WGRAD_DY 5
-#define ROI_WGRAD_SLOTS 3
-#define ROI_WGRAD_SETS 5
-#define ROI_WGRAD_WARPS 2
-#endif
 // Rings: codes and scales, dY, and converted x^ (where nothing waits for memory in between).
-constexpr int kCodeStages = ROI_WGRAD_CODES, kDyStages = ROI_WGRAD_DY, kSlots = ROI_WGRAD_SLOTS;
+constexpr int kCodeStages = 10, kDyStages = 5, kSlots = 3;
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
 constexpr uint32_t kCodes = kChunk * kEdge;
 constexpr uint32_t kScales = kChunk * 4;   // a word of four blocks a token
 constexpr uint32_t kOffSlots = kDyStages * kOperand, kOffCodes = kOffSlots + kSlots * kOperand;
 constexpr uint32_t kOffScales = kOffCodes + kCodeStages * kCodes, kOffBars = kOffScales + kCodeStages * kScales;
-constexpr int kSets = ROI_WGRAD_SETS;            // sets of warps that turn codes into bf16, each every kSets-th chunk
-constexpr int kConvertWarps = ROI_WGRAD_WARPS;   // of a set
+constexpr int kSets = 5;            // sets of warps that turn codes into bf16, each every kSets-th chunk
+constexpr int kConvertWarps = 2;    // of a set
 // A wait for a phase of a barrier takes the one before to be over.  Copies may land out of their
 // order, so a set waits for every phase of its code stages itself; dY's stages end in order, and a
 // set that waits for one has seen a chunk end that is at most kSets before.
@@ -61,7 +62,11 @@ constexpr int kWarpCodes = 2 + kConvertWarps * kSets, kWarpNotice = kWarpCodes +
 constexpr int kThreads = 32 * (kWarpNotice + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBars = 2 * kCodeStages + 2 * kDyStages + kSlots + 2 + 2;
-constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 16;  // from a 1024-byte boundary on
+constexpr uint32_t kOffMisc = kOffBars + kBars * 8;
+// 32 rows of 16 sums for each of the four warps that write, where outputs are not whole sectors.
+constexpr int kBlock = 16, kBlockPitch = kBlock + 1;
+constexpr uint32_t kOffBlocks = kOffMisc + 16, kSmem = kOffBlocks + 4 * 32 * kBlockPitch * 4;  // from a 1024-byte boundary on
+static_assert(kOffBlocks % 4 == 0 && kSmem + 1024 <= 232448, "shared memory");
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
 // partial sums is written and read again.
 constexpr int kMinRange = 8, kSplitCost = 8;
@@ -70,17 +75,17 @@ struct WgradArgs {
   const uint8_t* scales;
   uint16_t* dWm;  // nullable
   float* acc;     // nullable
-  float* part;    // [2 * ranges][32 CG][128 CG][4] (split): four columns of all rows after one another
+  float* part;    // [2 * ranges][kSide / 4][kSide][4] (split): four columns of all rows after one another
   int64_t T, rows, cols, spitch;
   int tiles_m, tiles_n;
   bool n_first;   // consecutive tiles run along the inputs
   int chunks;     // of a whole tile
-  int groups;     // CTAs or pairs
+  int groups;     // pairs of CTAs
   int rounds;     // whole rounds of tiles
   int rest;       // tiles of the last round
   int ranges;     // ranges of its tokens, 0 where they are not cut
   unsigned int* status;
-  bool wide;      // rows of the outputs are whole 32-byte sectors
+  bool wide;      // rows of the outputs are whole 32-byte sectors, in sixteens of columns
   bool wait;
 };
 
@@ -121,11 +126,11 @@ __device__ __forceinline__ bool work_of(const WgradArgs& a, int g, int i, Work& 
   return true;
 }
 
-__device__ __forceinline__ void tile_origin(const WgradArgs& a, int tile, int edge, int64_t& m0, int64_t& n0) {
+__device__ __forceinline__ void tile_origin(const WgradArgs& a, int tile, int64_t& m0, int64_t& n0) {
   const int m = a.n_first ? tile / a.tiles_n : tile % a.tiles_m;
   const int n = a.n_first ? tile % a.tiles_n : tile / a.tiles_m;
-  m0 = int64_t(m) * edge;
-  n0 = int64_t(n) * edge;
+  m0 = int64_t(m) * kSide;
+  n0 = int64_t(n) * kSide;
 }
 
 // Two codes to two bf16, times the block's power of two: the codes in the low bytes of the
@@ -180,63 +185,59 @@ __device__ __forceinline__ void load32(const void* p, float (&v)[8]) {
 }
 
 // 32 columns of a row of the sums, from column n on (a multiple of 32): added to acc, and
-// written out.  A lane has a row of its own, so it stores whole sectors where it can.
-__device__ __forceinline__ void store_sums(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
+// written out, where columns come in sixteens.  A lane has a row of its own and stores whole sectors.
+__device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
   const int64_t at = m * a.cols + n;
-  if (a.wide) {  // (columns come in sixteens)
-    if (a.acc != nullptr) {
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        if (n + 8 * q >= a.cols) break;
-        float x[8];
-        uint32_t w[8];
-        load32(a.acc + at + 8 * q, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += x[e]);
-        store32(a.acc + at + 8 * q, w);
-      }
-    }
-    if (a.dWm != nullptr) {
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        if (n + 16 * q >= a.cols) break;
-        uint32_t w[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
-        store32(a.dWm + at + 16 * q, w);
-      }
-    }
-  } else if (a.cols % 8 == 0) {
+  if (a.acc != nullptr) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (n + 8 * q >= a.cols) break;
-      float* s = v + 8 * q;
-      if (a.acc != nullptr) {
-        float4* p = reinterpret_cast<float4*>(a.acc + at + 8 * q);
-        const float4 x = p[0], y = p[1];
-        s[0] += x.x, s[1] += x.y, s[2] += x.z, s[3] += x.w;
-        s[4] += y.x, s[5] += y.y, s[6] += y.z, s[7] += y.w;
-        p[0] = make_float4(s[0], s[1], s[2], s[3]);
-        p[1] = make_float4(s[4], s[5], s[6], s[7]);
-      }
-      if (a.dWm != nullptr) {
-        *reinterpret_cast<uint4*>(a.dWm + at + 8 * q) =
-            make_uint4(pack_bf16x2(s[0], s[1]), pack_bf16x2(s[2], s[3]), pack_bf16x2(s[4], s[5]), pack_bf16x2(s[6], s[7]));
-      }
-    }
-  } else {
+      float x[8];
+      uint32_t w[8];
+      load32(a.acc + at + 8 * q, x);
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-      if (n + k < a.cols) {
-        if (a.acc != nullptr) a.acc[at + k] = v[k] += a.acc[at + k];
-        if (a.dWm != nullptr) a.dWm[at + k] = __bfloat16_as_ushort(__float2bfloat16_rn(v[k]));
+      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += x[e]);
+      store32(a.acc + at + 8 * q, w);
+    }
+  }
+  if (a.dWm != nullptr) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      if (n + 16 * q >= a.cols) break;
+      uint32_t w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = pack_bf16x2(v[16 * q + 2 * e], v[16 * q + 2 * e + 1]);
+      store32(a.dWm + at + 16 * q, w);
+    }
+  }
+}
+// Any other width (the whole warp, rows m0 on): 16 columns at a time through shared memory, so that
+// sixteen lanes write neighbours.  (With a row a lane, a 2-byte store touched 32 lines: 254 us for
+// a layer of 12 that now takes a fifth of it.)
+__device__ __forceinline__ void store_block(const WgradArgs& a, float* block, int64_t m0, int64_t n, const float (&v)[32]) {
+  const int lane = threadIdx.x & 31, c = lane & 15;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (n + kBlock * h >= a.cols) break;
+    __syncwarp();
+#pragma unroll
+    for (int e = 0; e < kBlock; ++e) block[lane * kBlockPitch + e] = v[kBlock * h + e];
+    __syncwarp();
+    const int64_t col = n + kBlock * h + c;
+    if (col < a.cols) {
+#pragma unroll 4
+      for (int r = lane >> 4; r < 32; r += 2) {
+        if (m0 + r >= a.rows) break;
+        const int64_t at = (m0 + r) * a.cols + col;
+        float x = block[r * kBlockPitch + c];
+        if (a.acc != nullptr) a.acc[at] = x += a.acc[at];
+        if (a.dWm != nullptr) a.dWm[at] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
       }
     }
   }
 }
 
-template <int CG>
-__global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -245,8 +246,8 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   uint64_t *ready = dy_empty + kDyStages, *sum = ready + kSlots, *free = sum + 2;
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t rank = CG == 1 ? 0u : cluster_rank();
-  const int g = blockIdx.x / CG;
+  const uint32_t rank = cluster_rank();
+  const int g = blockIdx.x / 2;
 
   if (tid == 0) {
     for (int s = 0; s < kCodeStages; ++s) {
@@ -257,18 +258,18 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       mbar_init(dy_full + s, 1);
       mbar_init(dy_empty + s, 1);
     }
-    for (int s = 0; s < kSlots; ++s) mbar_init(ready + s, (kConvertWarps + 1) * CG);
+    for (int s = 0; s < kSlots; ++s) mbar_init(ready + s, (kConvertWarps + 1) * 2);
     for (int b = 0; b < 2; ++b) {
       mbar_init(sum + b, 1);
-      mbar_init(free + b, 4 * CG);
+      mbar_init(free + b, 4 * 2);
     }
     misc[1] = 1u;
     fence_mbar_init();
   }
-  if (warp == 0) tc_alloc_group<CG>(misc, kTmemCols);
+  if (warp == 0) tc_alloc_pair(misc, kTmemCols);
   tc_fence_before();
   __syncthreads();
-  if constexpr (CG > 1) cluster_sync();
+  cluster_sync();
   tc_fence_after();
   const uint32_t tmem = misc[0];
   pdl_begin(a.wait);
@@ -288,7 +289,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   };
   if (warp == 0) {
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      tile_origin(a, w.tile, m0, n0);
       const int m = int(m0) + int(rank) * kEdge;
       for (int c = w.c0; c < w.c1; ++c, ++issued, ring.next()) {
         ok = mbar_wait_ring_cluster(dy_empty + ring.at, ring.pass ^ 1u, lim);
@@ -306,7 +307,7 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
   } else if (warp == kWarpCodes) {
     // codes, and scales: two tokens a lane, a word of four blocks each
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      tile_origin(a, w.tile, m0, n0);
       const int64_t n = n0 + int64_t(rank) * kEdge;
       const bool in = n / 32 < a.spitch;  // (a row's scales end with whole words)
       int64_t row = int64_t(w.c0) * kChunk + lane;
@@ -341,13 +342,13 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      const uint32_t idesc = tc_idesc_bf16_f32_mn(kEdge * CG, kEdge * CG);
+      const uint32_t idesc = tc_idesc_bf16_f32_mn(kSide, kSide);
       // descriptors of the first stage and slot; addresses count in units of 16 bytes
       const uint64_t dy0 = tc_smem_desc_mn128(smem_addr(smem), kHalf), x0 = tc_smem_desc_mn128(smem_addr(smem + kOffSlots), kHalf);
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         const int b = i & 1;
         ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
-        const uint32_t d = tmem + uint32_t(b) * (kEdge * CG);
+        const uint32_t d = tmem + uint32_t(b) * kSide;
         for (int c = w.c0; ok && c < w.c1; ++c, ++committed, ring.next(), slot.next()) {
           ok = mbar_wait_ring_cluster(ready + slot.at, slot.pass, lim);
           if (!ok) break;
@@ -356,9 +357,9 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
           if (elect_one()) {
 #pragma unroll
             for (int k = 0; k < kChunk / 16; ++k)
-              tc_mma_bf16_group<CG>(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, k > 0 || c > w.c0);
-            tc_commit_group<CG>(dy_empty + ring.at);
-            if (c == w.c1 - 1) tc_commit_group<CG>(sum + b);
+              tc_mma_bf16_pair(d, dy + k * (2048 / 16), x + k * (2048 / 16), idesc, k > 0 || c > w.c0);
+            tc_commit_pair(dy_empty + ring.at);
+            if (c == w.c1 - 1) tc_commit_pair(sum + b);
           }
           __syncwarp();
         }
@@ -415,20 +416,22 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
       ok = mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim);
       if (!ok) break;
       tc_fence_after();
-      tile_origin(a, w.tile, kEdge * CG, m0, n0);
+      tile_origin(a, w.tile, m0, n0);
       const int r = int(rank) * kEdge + quarter * 32 + lane;  // row of the tile
       const int64_t m = m0 + r;
-      float4* part = reinterpret_cast<float4*>(a.part) + int64_t(w.slot) * (kEdge * CG) * (kEdge * CG / 4) + r;
-      for (int q = 0; q < kEdge * CG / 32; ++q) {
+      float4* part = reinterpret_cast<float4*>(a.part) + int64_t(w.slot) * kSide * (kSide / 4) + r;
+      for (int q = 0; q < kSide / 32; ++q) {
         uint32_t u[32];
-        tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * (kEdge * CG) + 32 * q), u);
+        tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * kSide + 32 * q), u);
         float v[32];
         input_order(u, v);
         if (w.slot >= 0) {
 #pragma unroll
-          for (int e = 0; e < 32; e += 4) part[(8 * q + e / 4) * (kEdge * CG)] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-        } else if (m < a.rows && n0 + 32 * q < a.cols) {
-          store_sums(a, m, n0 + 32 * q, v);
+          for (int e = 0; e < 32; e += 4) part[(8 * q + e / 4) * kSide] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        } else if (a.wide) {
+          if (m < a.rows && n0 + 32 * q < a.cols) store_sectors(a, m, n0 + 32 * q, v);
+        } else if (n0 + 32 * q < a.cols) {
+          store_block(a, reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 32 * kBlockPitch, m - lane, n0 + 32 * q, v);
         }
       }
       tc_fence_before();
@@ -454,22 +457,21 @@ __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(kThreads, 1)
     __syncthreads();
   }
   tc_fence_after();
-  if constexpr (CG > 1) cluster_sync();
-  if (warp == 0) tc_dealloc_group<CG>(tmem, kTmemCols);
+  cluster_sync();
+  if (warp == 0) tc_dealloc_pair(tmem, kTmemCols);
 }
 
 // The tiles of the last round whose tokens were cut: their partial sums in the order of the
 // ranges.  A CTA takes 32 rows of a tile: a lane reads four columns of its row (a warp 512
 // consecutive bytes), and the rows are written out through shared memory.
 constexpr int kJoinRows = 32;
-template <int CG>
 __global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
-  constexpr int kSide = kEdge * CG, kQuads = kSide / 4, kEach = kQuads / 8;
+  constexpr int kQuads = kSide / 4, kEach = kQuads / 8;
   __shared__ float rows[kJoinRows][kSide + 4];
   pdl_begin(true);  // the partial sums of the launch before
   const int tile = blockIdx.x / (kSide / kJoinRows), r0 = blockIdx.x % (kSide / kJoinRows) * kJoinRows;
   int64_t m0, n0;
-  tile_origin(a, a.rounds * a.groups + tile, kSide, m0, n0);
+  tile_origin(a, a.rounds * a.groups + tile, m0, n0);
   m0 += r0;
   if (m0 >= a.rows) return;
   // the ranges that hold the tile's first and last chunk
@@ -537,14 +539,9 @@ __global__ void __launch_bounds__(256) roi_wgrad_empty_kernel(uint16_t* dWm, con
     dWm[i] = __bfloat16_as_ushort(__float2bfloat16_rn(acc == nullptr ? 0.0f : acc[i]));
 }
 
-#ifndef ROI_WGRAD_GROUP
-#define ROI_WGRAD_GROUP 2
-#endif
-constexpr int kGroup = ROI_WGRAD_GROUP;
-
 // The division of the work among the groups, and the bytes of partial sums it needs.
 size_t plan(int64_t T, int64_t rows, int64_t cols, WgradArgs& a) {
-  constexpr int64_t side = kEdge * kGroup;
+  constexpr int64_t side = kSide;
   a.T = T;
   a.rows = rows;
   a.cols = cols;
@@ -552,7 +549,7 @@ size_t plan(int64_t T, int64_t rows, int64_t cols, WgradArgs& a) {
   a.tiles_n = int((cols + side - 1) / side);
   a.n_first = 2 * rows >= cols;  // the larger operand (dY in 2 bytes, codes in one) is read through once
   a.chunks = int((T + kChunk - 1) / kChunk);
-  a.groups = sm_count() / kGroup;
+  a.groups = sm_count() / 2;
   if (a.groups < 1) a.groups = 1;
   const int64_t tiles = int64_t(a.tiles_m) * a.tiles_n;
   a.rounds = int(tiles / a.groups);
@@ -621,7 +618,7 @@ int launch_wgrad(const WgradCall& c) {
       !make_tensor_map(&tm_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.codes, uint64_t(pitch), uint64_t(c.T), uint64_t(pitch), kEdge,
                        kChunk, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return -1;
-  auto kern = roi_wgrad_kernel<kGroup>;
+  auto kern = roi_wgrad_kernel;
   constexpr size_t smem = kSmem + 1024;
   static std::atomic<bool> set[64];
   int dev = 0;
@@ -631,10 +628,10 @@ int launch_wgrad(const WgradCall& c) {
     set[dev].store(true, std::memory_order_release);
   }
   const int64_t busy = a.rounds > 0 ? a.groups : a.ranges > 0 ? a.ranges : a.rest;
-  if (launch_maybe_pdl(kern, int(busy) * kGroup, kThreads, smem, c.stream, wait, tm_dy, tm_codes, a) < 0) return -1;
+  if (launch_maybe_pdl(kern, int(busy) * 2, kThreads, smem, c.stream, wait, tm_dy, tm_codes, a) < 0) return -1;
   ++launched;
   if (a.ranges > 0) {
-    if (launch_maybe_pdl(roi_wgrad_join_kernel<kGroup>, a.rest * (kEdge * kGroup / kJoinRows), 256, 0, c.stream, true, a) < 0) return -1;
+    if (launch_maybe_pdl(roi_wgrad_join_kernel, a.rest * (kSide / kJoinRows), 256, 0, c.stream, true, a) < 0) return -1;
     ++launched;
   }
   return launched;

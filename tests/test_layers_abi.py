@@ -88,3 +88,22 @@ def test_wgrad(L):
     assert f(ws=F + 8, n=64) == ALIGN
     assert f(out=A) == ALIAS and f(acc=D) == ALIAS and f(out=B + 16) == ALIAS and f(ld=65, ws=A, n=1 << 20) == ALIAS
     assert f(rows=0, dY=0, q=0, s=0, out=0, acc=0) == OK
+
+
+def test_registers_of_the_weight_gradient():
+    """18 warps on four schedulers leave a thread 96 registers; the converting warps hold 64 of them as
+    outputs, and a spill in their loop costs more than any tile shape gains."""
+    import os
+    import re
+
+    from paper_2608_23048_gb300 import _build
+    try:
+        _build.nvcc()
+    except RuntimeError:
+        pytest.skip("needs nvcc")
+    if not os.path.exists(_build.log_of("roi_wgrad.cu")):
+        _build.build(force=True)
+    with open(_build.log_of("roi_wgrad.cu")) as f:
+        found = re.findall(r"Compiling entry function '\w*roi_wgrad_kernel\w*'[^\n]*\n[^\n]*\n\s*(\d+) bytes stack frame, (\d+) "
+                           r"bytes spill stores[^\n]*\n[^\n]*Used (\d+) registers", f.read())
+    assert found == [("0", "0", found[0][2])] and int(found[0][2]) <= 96, found
