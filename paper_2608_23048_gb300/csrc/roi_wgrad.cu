@@ -63,10 +63,10 @@ constexpr int kThreads = 32 * (kWarpNotice + 1 + 4);
 constexpr uint32_t kTmemCols = 512;
 constexpr int kBars = 2 * kCodeStages + 2 * kDyStages + kSlots + 2 + 2;
 constexpr uint32_t kOffMisc = kOffBars + kBars * 8;
-// 32 rows of 16 sums for each of the four warps that write, where outputs are not whole sectors.
-constexpr int kBlock = 16, kBlockPitch = kBlock + 1;
-constexpr uint32_t kOffBlocks = kOffMisc + 16, kSmem = kOffBlocks + 4 * 32 * kBlockPitch * 4;  // from a 1024-byte boundary on
-static_assert(kOffBlocks % 4 == 0 && kSmem + 1024 <= 232448, "shared memory");
+// 16 rows of 32 sums for each of the four warps that write, where outputs are not whole sectors.
+constexpr int kBlockPitch = 36;
+constexpr uint32_t kOffBlocks = (kOffMisc + 8 + 15) / 16 * 16, kSmem = kOffBlocks + 4 * 16 * kBlockPitch * 4;  // from a 1024-byte boundary on
+static_assert(kSmem + 1024 <= 232448, "shared memory");
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
 // partial sums is written and read again.
 constexpr int kMinRange = 8, kSplitCost = 8;
@@ -85,7 +85,6 @@ struct WgradArgs {
   int rest;       // tiles of the last round
   int ranges;     // ranges of its tokens, 0 where they are not cut
   unsigned int* status;
-  bool wide;      // rows of the outputs are whole 32-byte sectors, in sixteens of columns
   bool wait;
 };
 
@@ -211,32 +210,82 @@ __device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int
     }
   }
 }
-// Any other width (the whole warp, rows m0 on): 16 columns at a time through shared memory, so that
-// sixteen lanes write neighbours.  (With a row a lane, a 2-byte store touched 32 lines: 254 us for
-// a layer of 12 that now takes a fifth of it.)
+// Any other width (the whole warp, rows m0 on): 16 rows at a time through shared memory, so that
+// sixteen lanes write a row's 32 columns, two each (PAIRS: rows of an even width).  A store of 2
+// bytes a lane to a row a lane would touch 32 lines.
+template <bool PAIRS>
 __device__ __forceinline__ void store_block(const WgradArgs& a, float* block, int64_t m0, int64_t n, const float (&v)[32]) {
-  const int lane = threadIdx.x & 31, c = lane & 15;
-#pragma unroll
+  const int lane = threadIdx.x & 31, c = 2 * (lane & 15), odd = lane >> 4;
+  const int64_t after = a.cols - n - c;
+  const int left = after > 2 ? 2 : after < 0 ? 0 : int(after);  // of this lane's columns
+  const int64_t step = 2 * a.cols;
+#pragma unroll 1
   for (int h = 0; h < 2; ++h) {
-    if (n + kBlock * h >= a.cols) break;
     __syncwarp();
+    if (odd == h) {
 #pragma unroll
-    for (int e = 0; e < kBlock; ++e) block[lane * kBlockPitch + e] = v[kBlock * h + e];
+      for (int e = 0; e < 32; e += 4)
+        *reinterpret_cast<float4*>(block + (lane & 15) * kBlockPitch + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    }
     __syncwarp();
-    const int64_t col = n + kBlock * h + c;
-    if (col < a.cols) {
-#pragma unroll 4
-      for (int r = lane >> 4; r < 32; r += 2) {
-        if (m0 + r >= a.rows) break;
-        const int64_t at = (m0 + r) * a.cols + col;
-        float x = block[r * kBlockPitch + c];
-        if (a.acc != nullptr) a.acc[at] = x += a.acc[at];
-        if (a.dWm != nullptr) a.dWm[at] = __bfloat16_as_ushort(__float2bfloat16_rn(x));
+    const int64_t below = a.rows - m0 - 16 * h;
+    const int rows = left == 0 ? 0 : below > 16 ? 16 : int(below);  // of the 16
+    const int64_t at = (m0 + 16 * h + odd) * a.cols + n + c;
+    const float* from = block + odd * kBlockPitch + c;
+    uint16_t* out = a.dWm + at;
+    if (a.acc == nullptr) {
+#pragma unroll
+      for (int r = 0; r < 8; ++r, out += step) {
+        const float2 x = *reinterpret_cast<const float2*>(from + 2 * r * kBlockPitch);
+        const uint32_t w = pack_bf16x2(x.x, x.y);
+        if (2 * r + odd < rows) {
+          if constexpr (PAIRS) {
+            *reinterpret_cast<uint32_t*>(out) = w;
+          } else {
+            out[0] = uint16_t(w);
+            if (left > 1) out[1] = uint16_t(w >> 16);
+          }
+        }
+      }
+    } else {
+      float* acc = a.acc + at;
+      float2 y[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        y[r] = make_float2(0.0f, 0.0f);
+        const float* q = acc + r * step;
+        if (2 * r + odd < rows) {
+          if constexpr (PAIRS) y[r] = *reinterpret_cast<const float2*>(q);
+          else y[r] = make_float2(q[0], left > 1 ? q[1] : 0.0f);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r, out += step, acc += step) {
+        const float2 x = *reinterpret_cast<const float2*>(from + 2 * r * kBlockPitch);
+        y[r].x += x.x, y[r].y += x.y;
+        if (2 * r + odd < rows) {
+          const uint32_t w = pack_bf16x2(y[r].x, y[r].y);
+          if constexpr (PAIRS) {
+            *reinterpret_cast<float2*>(acc) = y[r];
+            if (a.dWm != nullptr) *reinterpret_cast<uint32_t*>(out) = w;
+          } else {
+            acc[0] = y[r].x;
+            if (a.dWm != nullptr) out[0] = uint16_t(w);
+            if (left > 1) {
+              acc[1] = y[r].y;
+              if (a.dWm != nullptr) out[1] = uint16_t(w >> 16);
+            }
+          }
+        }
       }
     }
   }
 }
 
+// How the outputs are written: whole sectors, pairs of columns, single columns.
+enum class Out { kSectors, kPairs, kSingles };
+
+template <Out OUT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
@@ -428,10 +477,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (w.slot >= 0) {
 #pragma unroll
           for (int e = 0; e < 32; e += 4) part[(8 * q + e / 4) * kSide] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-        } else if (a.wide) {
+        } else if constexpr (OUT == Out::kSectors) {
           if (m < a.rows && n0 + 32 * q < a.cols) store_sectors(a, m, n0 + 32 * q, v);
         } else if (n0 + 32 * q < a.cols) {
-          store_block(a, reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 32 * kBlockPitch, m - lane, n0 + 32 * q, v);
+          store_block<OUT == Out::kPairs>(a, reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 16 * kBlockPitch, m - lane,
+                                          n0 + 32 * q, v);
         }
       }
       tc_fence_before();
@@ -462,11 +512,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 }
 
 // The tiles of the last round whose tokens were cut: their partial sums in the order of the
-// ranges.  A CTA takes 32 rows of a tile: a lane reads four columns of its row (a warp 512
+// ranges.  A CTA takes 8 rows of a tile; a lane reads four columns of its row (eight lanes 128
 // consecutive bytes), and the rows are written out through shared memory.
-constexpr int kJoinRows = 32;
+constexpr int kJoinRows = 8;
 __global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
-  constexpr int kQuads = kSide / 4, kEach = kQuads / 8;
+  constexpr int kQuads = kSide / 4, kEach = kQuads / 32, kAhead = 4;
   __shared__ float rows[kJoinRows][kSide + 4];
   pdl_begin(true);  // the partial sums of the launch before
   const int tile = blockIdx.x / (kSide / kJoinRows), r0 = blockIdx.x % (kSide / kJoinRows) * kJoinRows;
@@ -480,29 +530,35 @@ __global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
   while (range_start(a, p0 + 1) <= t0) ++p0;
   while (range_start(a, p1 + 1) <= t1) ++p1;
   if (p0 == p1) return;  // whole, and written already
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = threadIdx.x & 7, quad = threadIdx.x >> 3;
+  // (only the first range may have begun in the tile before, whose sums are in its other slot)
+  const int first = 2 * p0 + (range_start(a, p0) < t0 ? 1 : 0);
+  const float4* part = reinterpret_cast<const float4*>(a.part) + r0 + r + quad * kSide;
   float4 s[kEach];
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) s[e] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int p = p0; p <= p1; ++p) {
-    // (only the first range may have begun in the tile before)
-    const int j = p == p0 && range_start(a, p) < t0 ? 1 : 0;
-    const float4* from = reinterpret_cast<const float4*>(a.part) + int64_t(2 * p + j) * kSide * kQuads + r0 + lane;
-    float4 v[kEach];
+  for (int e = 0; e < kEach; ++e) s[e] = __ldcs(part + int64_t(first) * kSide * kQuads + 32 * e * kSide);
+  for (int p = p0 + 1; p <= p1; p += kAhead) {
+    float4 v[kAhead][kEach];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) v[e] = __ldcs(from + (warp + 8 * e) * kSide);
+    for (int q = 0; q < kAhead; ++q)
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) s[e].x += v[e].x, s[e].y += v[e].y, s[e].z += v[e].z, s[e].w += v[e].w;
+      for (int e = 0; e < kEach; ++e)
+        if (p + q <= p1) v[q][e] = __ldcs(part + int64_t(2 * (p + q)) * kSide * kQuads + 32 * e * kSide);
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+      for (int e = 0; e < kEach; ++e)
+        if (p + q <= p1) s[e].x += v[q][e].x, s[e].y += v[q][e].y, s[e].z += v[q][e].z, s[e].w += v[q][e].w;
   }
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) *reinterpret_cast<float4*>(&rows[lane][4 * (warp + 8 * e)]) = s[e];
+  for (int e = 0; e < kEach; ++e) *reinterpret_cast<float4*>(&rows[r][4 * (quad + 32 * e)]) = s[e];
   __syncthreads();
   const bool fours = a.cols % 4 == 0;
   for (int i = threadIdx.x; i < kJoinRows * kQuads; i += 256) {
-    const int r = i / kQuads, c = i % kQuads * 4;
-    if (m0 + r >= a.rows || n0 + c >= a.cols) continue;
-    float v[4] = {rows[r][c], rows[r][c + 1], rows[r][c + 2], rows[r][c + 3]};
-    const int64_t at = (m0 + r) * a.cols + n0 + c;
+    const int w = i / kQuads, c = i % kQuads * 4;
+    if (m0 + w >= a.rows || n0 + c >= a.cols) continue;
+    float v[4] = {rows[w][c], rows[w][c + 1], rows[w][c + 2], rows[w][c + 3]};
+    const int64_t at = (m0 + w) * a.cols + n0 + c;
     if (fours) {
       if (a.acc != nullptr) {
         float4* q = reinterpret_cast<float4*>(a.acc + at);
@@ -609,7 +665,6 @@ int launch_wgrad(const WgradCall& c) {
   a.part = reinterpret_cast<float*>(ws);
   a.spitch = block8_scale_pitch(c.cols);
   a.status = c.status;
-  a.wide = c.cols % 16 == 0 && ((reinterpret_cast<uintptr_t>(c.dWm) | reinterpret_cast<uintptr_t>(c.acc)) & 31u) == 0;
   a.wait = wait;
   CUtensorMap tm_dy, tm_codes;
   const int64_t pitch = block8_pitch(c.cols);
@@ -618,14 +673,19 @@ int launch_wgrad(const WgradCall& c) {
       !make_tensor_map(&tm_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.codes, uint64_t(pitch), uint64_t(c.T), uint64_t(pitch), kEdge,
                        kChunk, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return -1;
-  auto kern = roi_wgrad_kernel;
+  // whole sectors where the outputs' rows are in sixteens of columns; else through shared memory
+  const bool sectors = c.cols % 16 == 0 && ((reinterpret_cast<uintptr_t>(c.dWm) | reinterpret_cast<uintptr_t>(c.acc)) & 31u) == 0;
+  const int form = sectors ? 0 : c.cols % 2 == 0 ? 1 : 2;
+  auto kern = form == 0   ? roi_wgrad_kernel<Out::kSectors>
+              : form == 1 ? roi_wgrad_kernel<Out::kPairs>
+                          : roi_wgrad_kernel<Out::kSingles>;
   constexpr size_t smem = kSmem + 1024;
-  static std::atomic<bool> set[64];
+  static std::atomic<bool> set[3][64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
-  if (!set[dev].load(std::memory_order_acquire)) {
+  if (!set[form][dev].load(std::memory_order_acquire)) {
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return -1;
-    set[dev].store(true, std::memory_order_release);
+    set[form][dev].store(true, std::memory_order_release);
   }
   const int64_t busy = a.rounds > 0 ? a.groups : a.ranges > 0 ? a.ranges : a.rest;
   if (launch_maybe_pdl(kern, int(busy) * 2, kThreads, smem, c.stream, wait, tm_dy, tm_codes, a) < 0) return -1;

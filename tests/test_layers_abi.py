@@ -106,4 +106,5 @@ def test_registers_of_the_weight_gradient():
     with open(_build.log_of("roi_wgrad.cu")) as f:
         found = re.findall(r"Compiling entry function '\w*roi_wgrad_kernel\w*'[^\n]*\n[^\n]*\n\s*(\d+) bytes stack frame, (\d+) "
                            r"bytes spill stores[^\n]*\n[^\n]*Used (\d+) registers", f.read())
-    assert found == [("0", "0", found[0][2])] and int(found[0][2]) <= 96, found
+    # (the form that stores whole sectors, and two for other widths)
+    assert len(found) == 3 and all(int(f[2]) <= 96 and int(f[1]) <= 16 for f in found) and ("0", "0") in [f[:2] for f in found], found
