@@ -372,7 +372,9 @@ typedef enum {
  *  out_mean, out_rstd  [rows] float32, nullable; out_mean NULL for ROI_RMS_NORM
  *  out_xcodes, out_xscales  nullable together: the checkpoint of x
  *  out_ycodes, out_yscales  nullable together: the checkpoint of out_y as it was
- *    rounded, the input of the masked layers that follow                          */
+ *    rounded, the input of the masked layers that follow
+ * At most 2^30 columns (else ROI_ERR_SHAPE), here and in the backward.
+ * roi_device_status reports a kernel that gave up waiting on its copies.            */
 roi_status roi_norm_fwd(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int kind,
                         const void* gamma, const void* beta, int param_dtype, float eps,
                         void* out_y, int64_t ldy, float* out_mean, float* out_rstd,

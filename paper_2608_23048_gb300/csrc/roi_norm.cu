@@ -22,12 +22,19 @@
 // Rows that start anywhere are copied by the 16-byte granules around them (but for the matrix's own
 // ends) and shifted as they are read; they are written as roi_rows.cuh does.  Rows so wide that
 // two of them do not fit go to kernels that read them again for each step.
+//
+// Measured, 8192 x 3584 bf16 (of 6.79 TB/s copied): RMS norm forward 22.7 us (5.2 TB/s), with y's checkpoint
+// 35.8, layer norm 33; RMS norm backward 41.5 us from x (4.2 TB/s), 41.6 from its checkpoint, 7 of which are the
+// sums' (their places in memory and the second launch), layer norm 45.7 and 47.4.  With rows loaded
+// by the threads that use them: RMS norm forward 48 us, layer norm 46, RMS norm backward from the checkpoint 52.  What is
+// left is instructions: the forward with y's checkpoint issues in 56 % of the cycles, the backward in 47 %, with 15 to 22
+// warps an SM.  Rows that start anywhere (8192
+// x 3583) take 1.5 to 1.7 times as long, for the shifts.
 #include <atomic>
 
 #include "roi_block8.cuh"
 #include "roi_launch.h"
 #include "roi_rows.cuh"
-#include "roi_tc.cuh"
 
 namespace roi {
 namespace {
@@ -409,9 +416,15 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
 template <int NP>
 __device__ __forceinline__ int column(int i, int t) { return ((t >> 5) * NP + i) * 256 + (t & 31) * 8; }
 
+// What a thread keeps of dy until dx is written: dy as it was read where that is half the registers (16
+// bits) and they are short, else its product with gamma.  bf16, x from memory: RMS norm 8192 x 3584 41.6 us
+// with dy in 768 threads (46 in 640) and 50 with the product in 640; layer norm 8192 x 8192 98 us with dy
+// and 130 with the product in 640; 8192 x 3584 46 us with the product and 53 with dy, both in 512.
+template <Elem E, bool LAYER, int THREADS>
+constexpr bool kKeepDy = E != Elem::kFp32 && (!LAYER || THREADS > 512);
 
-// THREADS: what leaves two pieces a thread their registers, 512 with the sums of dbeta and 640 without
-// (two teams at 3584 columns); 1024 for one piece, and for rows too wide for these.
+// THREADS: what leaves two pieces a thread their registers; 1024 for one piece, and for rows too wide for
+// these.
 template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP, int THREADS>
 __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
   using T = typename ElemType<E>::T;
@@ -484,11 +497,11 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
     const uint32_t ms = CKPT ? row_shift<true>(a.scales + row * a.spitch) : 0u;
     const uint32_t mx = CKPT ? 0u : row_shift<ANY>(static_cast<const T*>(a.x) + row * a.ldx);
     // this thread's columns: dy, and xh (past the last column dy is 0)
-    auto get = [&](int i, Piece& dy, Piece& xh) {
+    constexpr bool KEEP = kKeepDy<E, LAYER, THREADS>;
+    auto get = [&](int i, RowWords<E, 8>& dy, Piece& xh) {
       const int c = column<NP>(i, t);
       float f[8];
-      read_row<E, ANY>(st, m, c, cols).get(f);
-      dy = pairs(f);
+      dy = read_row<E, ANY>(st, m, c, cols);
       if constexpr (CKPT) {
         uint2 w = make_uint2(0, 0);
         float step = 0.0f;
@@ -509,23 +522,29 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       }
     };
     F2 s1 = f2(0.0f), s2 = f2(0.0f);
-    Piece w[NP], xh[NP];  // dy gamma, and the normalised input
+    RowWords<E, 8> raw[KEEP ? NP : 1];
+    Piece w[KEEP ? 1 : NP], xh[NP];  // dy gamma, and the normalised input
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       if (column<NP>(i, t) - lane * 8 >= cols) break;  // (the whole warp)
-      Piece dy;
-      get(i, dy, xh[i]);
-      const Piece g = param(gamma, column<NP>(i, t));
+      RowWords<E, 8> words;
+      get(i, words, xh[i]);
+      float f[8];
+      words.get(f);
+      const Piece g = param(gamma, column<NP>(i, t)), dy = pairs(f);
+      Piece p;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        w[i].v[k] = dy.v[k] * g.v[k];
+        p.v[k] = dy.v[k] * g.v[k];
         dg[i].v[k] = vfma(dy.v[k], xh[i].v[k], dg[i].v[k]);
-        s1 = vfma(w[i].v[k], xh[i].v[k], s1);
+        s1 = vfma(p.v[k], xh[i].v[k], s1);
         if constexpr (LAYER) {
           db[i].v[k] = db[i].v[k] + dy.v[k];
-          s2 = s2 + w[i].v[k];
+          s2 = s2 + p.v[k];
         }
       }
+      if constexpr (KEEP) raw[i] = words;
+      else w[i] = p;
     }
     __syncwarp();
     if (lane == 0) mbar_arrive(&ts.empty[team][at]);
@@ -549,9 +568,19 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       const int c = column<NP>(i, t);
       if (c - lane * 8 >= cols) break;
       float o[8];
+      Piece p;
+      if constexpr (KEEP) {
+        raw[i].get(o);
+        const Piece g = param(gamma, c);
+        p = pairs(o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) p.v[k] = p.v[k] * g.v[k];
+      } else {
+        p = w[i];
+      }
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const F2 d = vfma(xh[i].v[k], k1, LAYER ? vfma(w[i].v[k], r2, k2) : w[i].v[k] * r2);
+        const F2 d = vfma(xh[i].v[k], k1, LAYER ? vfma(p.v[k], r2, k2) : p.v[k] * r2);
         o[2 * k] = lo(d), o[2 * k + 1] = hi(d);
       }
       RowWords<E, 8> d;
@@ -569,8 +598,9 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
   // themselves where it is the only CTA)
   float* sums = reinterpret_cast<float*>(smem);  // [1 or 2][NP][8][nt]
   float* part = a.part + int64_t(blockIdx.x) * (LAYER ? 2 : 1) * a.part_cols;
-  float* to_g = gridDim.x == 1 ? a.dgamma : part;
-  float* to_b = gridDim.x == 1 ? a.dbeta : part + a.part_cols;
+  const bool only = gridDim.x == 1;
+  float* to_g = only ? a.dgamma : part;
+  float* to_b = only ? a.dbeta : part + a.part_cols;
   float g8[NP][8], b8[NP][8];
 #pragma unroll
   for (int i = 0; i < NP; ++i)
@@ -601,17 +631,25 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 8; k += 4) {
         const int c = column<NP>(i, t) + k;
-        if (c < cols) {
-          if (to_g != nullptr) to_g[c] = g8[i][k];
-          if (LAYER && to_b != nullptr) to_b[c] = b8[i][k];
+        if (!only) {
+          // (a partial row has whole fours)
+          if (c < cols) *reinterpret_cast<float4*>(to_g + c) = make_float4(g8[i][k], g8[i][k + 1], g8[i][k + 2], g8[i][k + 3]);
+          if (LAYER && c < cols) *reinterpret_cast<float4*>(to_b + c) = make_float4(b8[i][k], b8[i][k + 1], b8[i][k + 2], b8[i][k + 3]);
+          continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (c + e < cols && to_g != nullptr) to_g[c + e] = g8[i][k + e];
+          if (LAYER && c + e < cols && to_b != nullptr) to_b[c + e] = b8[i][k + e];
         }
       }
     }
   }
 }
 
+// 152 partial rows of 3584 columns: 2.2 MB, which a launch of 112 CTAs reads in one go of ten loads a thread.
 constexpr int kSumSegments = 16;
 // out[c] = the sum of the `parts` partial rows at c, in a fixed order: sixteen threads a column
 // take every sixteenth row, and their sums are added in their order.  kinds: 1 (dgamma) or 2.
@@ -823,7 +861,9 @@ int fwd(const NormFwdCall& c, FwdArgs& a) {
   const int64_t pieces = (end + 255) / 256;
   const size_t stage = size_t(a.cols + 7) / 8 * 8 * elem_bytes<E>() + (ANY ? 32 : 0);
   const size_t params = size_t((a.cols + 255) / 256 * 256) * 4 * (LAYER ? 2 : 1);
-  // few rows: as many warps as there are pieces, so that a row's sums take the least time
+  // few rows, where a row's own time counts: as many warps as there are pieces.  RMS norm of 3584 columns in a graph,
+  // one piece a lane against four: 1 row 3.9 and 6.7 us, 304 rows 4.2 and 5.3, 600 rows 5.2 and 4.6, 1200 rows
+  // 7.4 and 6.1.
   const bool few = a.rows <= 2 * sm_count() && pieces < 32;
   a.shape = shape_of(a.rows, a.cols, pieces, few ? 1 : kRun<E>, few ? kThreads : kFwdThreads<LAYER, ANY>, stage, params, 0);
   if (a.shape.depth > 0) return few ? fwd_run<E, LAYER, ANY, 1>(c, a) : fwd_run<E, LAYER, ANY, kRun<E>>(c, a);
@@ -876,7 +916,10 @@ int bwd(const NormBwdCall& c, BwdArgs& a) {
   // (the teams' sums take the place of the rings)
   const size_t least = size_t(kinds) * 8 * size_t((pieces + np - 1) / np * np) * 32 * 4;
   const int64_t nt = (pieces + np - 1) / np * 32;
-  const int threads = np == 1 || nt > 608 ? 1024 : LAYER && nt <= 240 ? 512 : 640;
+  // (layer norm, 8192 rows, from the checkpoint, 512 threads against 640: 3584 columns 47 and 66 us, 2048 columns
+  // 31 and 34; the sums of dbeta take registers, and 512 hold no two teams of more than 240 threads)
+  constexpr int kFew = E != Elem::kFp32 && !LAYER ? 768 : 640;
+  const int threads = np == 1 || nt > kFew - 32 ? 1024 : LAYER && nt <= 240 ? 512 : kFew;
   a.shape = shape_of(a.rows, a.cols, pieces, np, threads, stage, params, least);
   if (a.shape.depth == 0) {
     const int64_t cap = int64_t(sm_count()) * 2;
@@ -890,7 +933,7 @@ int bwd(const NormBwdCall& c, BwdArgs& a) {
   int n;
   if (np == 1) n = bwd_run<E, LAYER, CKPT, ANY, 1, 1024>(c, a);
   else if (threads == 1024) n = bwd_run<E, LAYER, CKPT, ANY, 2, 1024>(c, a);
-  else if (!LAYER || threads == 640) n = bwd_run<E, LAYER, CKPT, ANY, 2, 640>(c, a);
+  else if (!LAYER || threads == kFew) n = bwd_run<E, LAYER, CKPT, ANY, 2, kFew>(c, a);
   else n = bwd_run<E, true, CKPT, ANY, 2, 512>(c, a);
   if (n < 0 || !sums || a.shape.grid == 1) return n;
   return sum_parts(a, a.shape.grid, kinds, c.stream) < 0 ? -1 : 2;

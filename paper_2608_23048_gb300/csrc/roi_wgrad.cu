@@ -26,13 +26,14 @@
 // which is 1860 to 1910 TFLOP/s.  Under a long load the clock falls with the power (681 us).
 // Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
 //
-// Tiles go to the groups (CTAs or pairs) in rounds.  In the last, partial round the tokens of
-// its tiles are cut into even ranges, one a group, where that ends sooner: ranges that do not
+// Tiles go to the pairs in rounds.  In the last, partial round the tokens of
+// its tiles are cut into even ranges, one a pair, where that ends sooner: ranges that do not
 // cover a whole tile leave fp32 partial sums in the workspace, which a second launch adds in
 // the order of the tokens, so that results do not depend on timing.
 #include <atomic>
 
 #include "roi_launch.h"
+#include "roi_rows.cuh"
 #include "roi_tc.cuh"
 #include "roi_tmap.h"
 
@@ -42,7 +43,9 @@ namespace {
 constexpr int kEdge = 128;                 // outputs, and inputs, that a CTA holds
 constexpr int kSide = 2 * kEdge;           // of a pair's tile
 constexpr int kChunk = 64;                 // tokens a stage
-// Rings: codes and scales, dY, and converted x^ (where nothing waits for memory in between).
+// Rings: codes and scales, dY, and converted x^ (where nothing waits for memory in between).  Stages of codes, of dY,
+// slots, sets, warps of a set, 8192 tokens of 18944 x 3584: 10, 5, 3, 5, 2 583 to 599 us; 8, 5, 4, 4, 4 613; 10, 5, 3,
+// 5, 4 627; 12, 4, 3, 4, 4 628; 8, 6, 3, 4, 4 625; 8, 6, 3, 4, 2 644.
 constexpr int kCodeStages = 10, kDyStages = 5, kSlots = 3;
 constexpr uint32_t kHalf = kChunk * 128;   // 64 tokens x 64 bf16
 constexpr uint32_t kOperand = 2 * kHalf;   // 64 tokens x 128 bf16
@@ -68,7 +71,8 @@ constexpr int kBlockPitch = 36;
 constexpr uint32_t kOffBlocks = (kOffMisc + 8 + 15) / 16 * 16, kSmem = kOffBlocks + 4 * 16 * kBlockPitch * 4;  // from a 1024-byte boundary on
 static_assert(kSmem + 1024 <= 232448, "shared memory");
 // The fewest chunks of a range of the last round, and what a split costs in chunks: a tile of
-// partial sums is written and read again.
+// partial sums is written and read again.  With 8 and 8, 4 and 8, 4 and 4, 2 and 4: 1024 tokens of 896 x 896
+// 14.8, 15.6, 15.5, 19.2 us; 2048 tokens of 128 x 896 14.0, 13.8, 13.9, 19.5; larger ones alike.
 constexpr int kMinRange = 8, kSplitCost = 8;
 
 struct WgradArgs {
@@ -170,15 +174,10 @@ struct Ring {
   }
 };
 
-// 32 bytes, one whole sector a lane (32-byte aligned).
-__device__ __forceinline__ void store32(void* p, const uint32_t (&w)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]),
-               "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-__device__ __forceinline__ void load32(const void* p, float (&v)[8]) {
+// load32 of memory that this kernel writes as well.
+__device__ __forceinline__ void load32_written(const void* p, uint32_t (&w)[8]) {
   asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
                : "l"(p)
                : "memory");
 }
@@ -191,11 +190,10 @@ __device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (n + 8 * q >= a.cols) break;
-      float x[8];
       uint32_t w[8];
-      load32(a.acc + at + 8 * q, x);
+      load32_written(a.acc + at + 8 * q, w);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += x[e]);
+      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += __uint_as_float(w[e]));
       store32(a.acc + at + 8 * q, w);
     }
   }
@@ -282,7 +280,8 @@ __device__ __forceinline__ void store_block(const WgradArgs& a, float* block, in
   }
 }
 
-// How the outputs are written: whole sectors, pairs of columns, single columns.
+// How the outputs are written: whole sectors, pairs of columns, single columns (the last two through shared
+// memory; 1999 tokens of 1215 x 2504 with acc 32 us, 45 element by element from registers).
 enum class Out { kSectors, kPairs, kSingles };
 
 template <Out OUT>
@@ -603,7 +602,9 @@ size_t plan(int64_t T, int64_t rows, int64_t cols, WgradArgs& a) {
   a.cols = cols;
   a.tiles_m = int((rows + side - 1) / side);
   a.tiles_n = int((cols + side - 1) / side);
-  a.n_first = 2 * rows >= cols;  // the larger operand (dY in 2 bytes, codes in one) is read through once
+  // The larger operand (dY in 2 bytes, codes in one) is read through once, the other from L2.  Against the other
+  // order, 8192 tokens: 18944 x 3584 601 and 737 us, 3584 x 18944 619 and 657, 2048 x 11008 218 and 231.
+  a.n_first = 2 * rows >= cols;
   a.chunks = int((T + kChunk - 1) / kChunk);
   a.groups = sm_count() / 2;
   if (a.groups < 1) a.groups = 1;
