@@ -404,7 +404,8 @@ roi_status roi_norm_bwd(const void* dy, int dtype, int64_t rows, int64_t cols, i
 /* Weight gradient of a masked linear layer Y = X Wm^T from the checkpoint of X:
  *   dWm[r, c] = sum_t float(dY[t, r]) * x[t, c]  (+ acc[r, c])
  * x the values that the checkpoint stands for; products exact, sums in fp32, on the
- * tensor cores.  The result is what roi_mask_bwd takes as dWm.
+ * tensor cores (for acc in pieces of at most 2816 tokens, added with rounding).
+ * The result is what roi_mask_bwd takes as dWm.  T, rows and cols at most 2^30.
  *  dY        [T, rows] bf16, row stride lddy; 16-byte aligned
  *  codes, scales  the checkpoint of X [T, cols]
  *  out_dWm   [rows, cols] bf16, nullable: the sum, rounded

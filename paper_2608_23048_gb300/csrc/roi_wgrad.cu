@@ -75,6 +75,13 @@ static_assert(kSmem + 1024 <= 232448, "shared memory");
 // 14.8, 15.6, 15.5, 19.2 us; 2048 tokens of 128 x 896 14.0, 13.8, 13.9, 19.5; larger ones alike.
 constexpr int kMinRange = 8, kSplitCost = 8;
 
+// The most chunks that TMEM sums unbroken for acc.  The tensor cores drop the bits below their sum's last
+// instead of rounding, all towards zero, which grows with the tokens: 4.3e-7 of the sum's norm at 2000
+// tokens, 1.1e-6 at 4000, 6.8e-6 at 16000, where an fp32 product has 5e-7.  So longer sums are added to
+// acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 871 us with acc, in three pieces, and 593
+// without, where the result is rounded to bf16, 4000 times as coarse, and the sum stays whole.
+constexpr int kMostChunks = 44;
+
 struct WgradArgs {
   const uint8_t* scales;
   uint16_t* dWm;  // nullable
@@ -84,6 +91,7 @@ struct WgradArgs {
   int tiles_m, tiles_n;
   bool n_first;   // consecutive tiles run along the inputs
   int chunks;     // of a whole tile
+  int unbroken;   // the most chunks of a sum in TMEM
   int groups;     // pairs of CTAs
   int rounds;     // whole rounds of tiles
   int rest;       // tiles of the last round
@@ -92,41 +100,55 @@ struct WgradArgs {
   bool wait;
 };
 
+// A sum in TMEM: some consecutive chunks of a tile.
 struct Work {
-  int tile, c0, c1;  // tile and its chunks
-  int slot;          // place of its partial sums, -1 where it is whole
+  int tile, c0, c1;  // tile and chunks
+  int slot;          // place of its partial sums, -1 where they go to the outputs
+  bool first, last;  // of the pieces that are added to one place
 };
 
 __host__ __device__ inline int64_t range_start(const WgradArgs& a, int64_t r) {
   return r * (int64_t(a.rest) * a.chunks) / a.ranges;
 }
 
-// The i-th piece of work of group g; false after the last.
+// Piece `i` of the sum over chunks c0 .. c1, in even pieces; false, and `i` less their number, after the last.
+__device__ __forceinline__ bool piece_of(const WgradArgs& a, int c0, int c1, int& i, Work& w) {
+  const int n = (c1 - c0 + a.unbroken - 1) / a.unbroken;
+  if (i >= n) {
+    i -= n;
+    return false;
+  }
+  const int each = (c1 - c0) / n, more = (c1 - c0) % n;
+  w.c0 = c0 + each * i + (i < more ? i : more);
+  w.c1 = w.c0 + each + (i < more ? 1 : 0);
+  w.first = i == 0;
+  w.last = i == n - 1;
+  return true;
+}
+
+// The i-th sum of group g; false after the last.
 __device__ __forceinline__ bool work_of(const WgradArgs& a, int g, int i, Work& w) {
   w.slot = -1;
-  w.c0 = 0;
-  w.c1 = a.chunks;
-  if (i < a.rounds) {
-    w.tile = i * a.groups + g;
-    return true;
+  const int pieces = (a.chunks + a.unbroken - 1) / a.unbroken, round = i / pieces;
+  if (a.ranges == 0 ? round < a.rounds + (g < a.rest ? 1 : 0) : round < a.rounds) {
+    w.tile = round * a.groups + g;
+    i -= round * pieces;
+    return piece_of(a, 0, a.chunks, i, w);
   }
-  const int j = i - a.rounds;
-  if (a.ranges == 0) {
-    w.tile = a.rounds * a.groups + g;
-    return j == 0 && g < a.rest;
-  }
-  if (g >= a.ranges || j > 1) return false;
+  if (g >= a.ranges) return false;
+  i -= a.rounds * pieces;
   // a range is no longer than a tile: it touches two tiles at most
   const int64_t begin = range_start(a, g), end = range_start(a, g + 1);
   const int first = int(begin / a.chunks);
-  const int64_t t0 = int64_t(first + j) * a.chunks;  // the tile's first chunk among all
-  const int64_t from = begin > t0 ? begin : t0, to = end < t0 + a.chunks ? end : t0 + a.chunks;
-  if (from >= to) return false;
-  w.tile = a.rounds * a.groups + first + j;
-  w.c0 = int(from - t0);
-  w.c1 = int(to - t0);
-  if (w.c0 != 0 || w.c1 != a.chunks) w.slot = 2 * g + j;
-  return true;
+  for (int j = 0; j < 2; ++j) {
+    const int64_t t0 = int64_t(first + j) * a.chunks;  // the tile's first chunk among all
+    const int64_t from = begin > t0 ? begin : t0, to = end < t0 + a.chunks ? end : t0 + a.chunks;
+    if (from >= to) return false;
+    w.tile = a.rounds * a.groups + first + j;
+    w.slot = to - from < a.chunks ? 2 * g + j : -1;
+    if (piece_of(a, int(from - t0), int(to - t0), i, w)) return true;
+  }
+  return false;
 }
 
 __device__ __forceinline__ void tile_origin(const WgradArgs& a, int tile, int64_t& m0, int64_t& n0) {
@@ -182,9 +204,16 @@ __device__ __forceinline__ void load32_written(const void* p, uint32_t (&w)[8]) 
                : "memory");
 }
 
+// (volatile: eight of them at once would take registers that the warps that write do not have)
+__device__ __forceinline__ float4 load_written(const float4* p) {
+  float4 x;
+  asm volatile("ld.global.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "l"(p) : "memory");
+  return x;
+}
+
 // 32 columns of a row of the sums, from column n on (a multiple of 32): added to acc, and
 // written out, where columns come in sixteens.  A lane has a row of its own and stores whole sectors.
-__device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int64_t n, float (&v)[32]) {
+__device__ __forceinline__ void store_sectors(const WgradArgs& a, bool last, int64_t m, int64_t n, float (&v)[32]) {
   const int64_t at = m * a.cols + n;
   if (a.acc != nullptr) {
 #pragma unroll
@@ -197,7 +226,7 @@ __device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int
       store32(a.acc + at + 8 * q, w);
     }
   }
-  if (a.dWm != nullptr) {
+  if (last && a.dWm != nullptr) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
       if (n + 16 * q >= a.cols) break;
@@ -212,7 +241,7 @@ __device__ __forceinline__ void store_sectors(const WgradArgs& a, int64_t m, int
 // sixteen lanes write a row's 32 columns, two each (PAIRS: rows of an even width).  A store of 2
 // bytes a lane to a row a lane would touch 32 lines.
 template <bool PAIRS>
-__device__ __forceinline__ void store_block(const WgradArgs& a, float* block, int64_t m0, int64_t n, const float (&v)[32]) {
+__device__ __forceinline__ void store_block(const WgradArgs& a, bool last, float* block, int64_t m0, int64_t n, const float (&v)[32]) {
   const int lane = threadIdx.x & 31, c = 2 * (lane & 15), odd = lane >> 4;
   const int64_t after = a.cols - n - c;
   const int left = after > 2 ? 2 : after < 0 ? 0 : int(after);  // of this lane's columns
@@ -247,6 +276,7 @@ __device__ __forceinline__ void store_block(const WgradArgs& a, float* block, in
       }
     } else {
       float* acc = a.acc + at;
+      const bool write = last && a.dWm != nullptr;
       float2 y[8];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
@@ -265,13 +295,13 @@ __device__ __forceinline__ void store_block(const WgradArgs& a, float* block, in
           const uint32_t w = pack_bf16x2(y[r].x, y[r].y);
           if constexpr (PAIRS) {
             *reinterpret_cast<float2*>(acc) = y[r];
-            if (a.dWm != nullptr) *reinterpret_cast<uint32_t*>(out) = w;
+            if (write) *reinterpret_cast<uint32_t*>(out) = w;
           } else {
             acc[0] = y[r].x;
-            if (a.dWm != nullptr) out[0] = uint16_t(w);
+            if (write) out[0] = uint16_t(w);
             if (left > 1) {
               acc[1] = y[r].y;
-              if (a.dWm != nullptr) out[1] = uint16_t(w >> 16);
+              if (write) out[1] = uint16_t(w >> 16);
             }
           }
         }
@@ -474,12 +504,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         float v[32];
         input_order(u, v);
         if (w.slot >= 0) {
+          if (!w.first) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 4) {
+              const float4 x = load_written(part + (8 * q + e / 4) * kSide);
+              v[e] += x.x, v[e + 1] += x.y, v[e + 2] += x.z, v[e + 3] += x.w;
+            }
+          }
 #pragma unroll
           for (int e = 0; e < 32; e += 4) part[(8 * q + e / 4) * kSide] = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         } else if constexpr (OUT == Out::kSectors) {
-          if (m < a.rows && n0 + 32 * q < a.cols) store_sectors(a, m, n0 + 32 * q, v);
+          if (m < a.rows && n0 + 32 * q < a.cols) store_sectors(a, w.last, m, n0 + 32 * q, v);
         } else if (n0 + 32 * q < a.cols) {
-          store_block<OUT == Out::kPairs>(a, reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 16 * kBlockPitch, m - lane,
+          store_block<OUT == Out::kPairs>(a, w.last, reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 16 * kBlockPitch, m - lane,
                                           n0 + 32 * q, v);
         }
       }
@@ -663,6 +700,7 @@ int launch_wgrad(const WgradCall& c) {
   a.scales = c.scales;
   a.dWm = c.dWm;
   a.acc = c.acc;
+  a.unbroken = c.acc != nullptr && a.chunks > kMostChunks ? kMostChunks : a.chunks;
   a.part = reinterpret_cast<float*>(ws);
   a.spitch = block8_scale_pitch(c.cols);
   a.status = c.status;
