@@ -78,7 +78,7 @@ constexpr int kMinRange = 8, kSplitCost = 8;
 // The most chunks that TMEM sums unbroken for acc.  The tensor cores drop the bits below their sum's last
 // instead of rounding, all towards zero, which grows with the tokens: 4.3e-7 of the sum's norm at 2000
 // tokens, 1.1e-6 at 4000, 6.8e-6 at 16000, where an fp32 product has 5e-7.  So longer sums are added to
-// acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 871 us with acc, in three pieces, and 593
+// acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 841 us with acc, in three pieces, and 590
 // without, where the result is rounded to bf16, 4000 times as coarse, and the sum stays whole.
 constexpr int kMostChunks = 44;
 
@@ -217,13 +217,17 @@ __device__ __forceinline__ void store_sectors(const WgradArgs& a, bool last, int
   const int64_t at = m * a.cols + n;
   if (a.acc != nullptr) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (n + 8 * q >= a.cols) break;
-      uint32_t w[8];
-      load32_written(a.acc + at + 8 * q, w);
+    for (int q = 0; q < 4; q += 2) {
+      if (n + 8 * q >= a.cols) break;  // (columns come in sixteens)
+      uint32_t w[2][8];
+      load32_written(a.acc + at + 8 * q, w[0]);
+      load32_written(a.acc + at + 8 * q + 8, w[1]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e] += __uint_as_float(w[e]));
-      store32(a.acc + at + 8 * q, w);
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[h][e] = __float_as_uint(v[8 * (q + h) + e] += __uint_as_float(w[h][e]));
+        store32(a.acc + at + 8 * (q + h), w[h]);
+      }
     }
   }
   if (last && a.dWm != nullptr) {
@@ -311,7 +315,7 @@ __device__ __forceinline__ void store_block(const WgradArgs& a, bool last, float
 }
 
 // How the outputs are written: whole sectors, pairs of columns, single columns (the last two through shared
-// memory; 1999 tokens of 1215 x 2504 with acc 32 us, 45 element by element from registers).
+// memory; 1999 tokens of 1215 x 2504 with acc 35 us, 45 element by element from registers).
 enum class Out { kSectors, kPairs, kSingles };
 
 template <Out OUT>
@@ -491,12 +495,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     const int quarter = warp & 3;
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       const int b = i & 1;
-      ok = mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim);
-      if (!ok) break;
-      tc_fence_after();
       tile_origin(a, w.tile, m0, n0);
       const int r = int(rank) * kEdge + quarter * 32 + lane;  // row of the tile
       const int64_t m = m0 + r;
+      if (a.acc != nullptr && w.slot < 0 && m < a.rows) {
+        // acc's row comes into L2 while the sum is formed (with two loads at a time, 3000 tokens of 18944 x 3584:
+        // 428 us, 488 with neither)
+        for (int q = 0; q < kSide / 32 && n0 + 32 * q < a.cols; ++q)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(a.acc + m * a.cols + n0 + 32 * q));
+      }
+      ok = mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim);
+      if (!ok) break;
+      tc_fence_after();
       float4* part = reinterpret_cast<float4*>(a.part) + int64_t(w.slot) * kSide * (kSide / 4) + r;
       for (int q = 0; q < kSide / 32; ++q) {
         uint32_t u[32];
