@@ -624,13 +624,23 @@ __global__ void __launch_bounds__(256) roi_wgrad_join_kernel(WgradArgs a) {
   }
 }
 
-// dY with rows that are not multiples of 16 bytes apart, laid out again with rows that are.
+// dY with rows that are not multiples of 16 bytes apart, laid out again with rows that are: `width` threads (a power of
+// two) a row, each eight columns at a time by the granules around them.  16000 tokens of
+// 3000 x 200: 81 us with this launch, 126 where it went element by element, 36 where dY's rows are aligned.
 __global__ void __launch_bounds__(256) roi_wgrad_align_kernel(const uint16_t* src, int64_t ld, uint16_t* dst, int64_t pitch, int64_t T,
-                                                              int64_t cols, bool wait) {
+                                                              int64_t cols, int width, bool wait) {
+  using E = ElemType<Elem::kBf16>::T;
   pdl_begin(wait);
-  for (int64_t t = blockIdx.x; t < T; t += gridDim.x) {
-#pragma unroll 8
-    for (int64_t c = threadIdx.x; c < cols; c += 256) dst[t * pitch + c] = src[t * ld + c];
+  const int per = 256 / width, j = threadIdx.x & (width - 1);
+  for (int64_t t = int64_t(blockIdx.x) * per + threadIdx.x / width; t < T; t += int64_t(gridDim.x) * per) {
+#pragma unroll 2
+    for (int64_t c = 8 * j; c < cols; c += 8 * width) {
+      Window<Elem::kBf16, 8, false> x;
+      x.load(reinterpret_cast<const E*>(src) + t * ld, c, cols);
+      RowWords<Elem::kBf16, 8> r;
+      x.get(r);
+      *reinterpret_cast<uint4*>(dst + t * pitch + c) = make_uint4(r.u[0], r.u[1], r.u[2], r.u[3]);
+    }
   }
 }
 
@@ -695,8 +705,11 @@ int launch_wgrad(const WgradCall& c) {
     // the copy lies at the workspace's start, the partial sums behind it
     ld = aligned_pitch(c.rows);
     const int64_t cap = int64_t(sm_count()) * 8;
-    launched = launch_maybe_pdl(roi_wgrad_align_kernel, int(c.T < cap ? c.T : cap), 256, 0, c.stream, wait, c.dY, c.lddy,
-                                reinterpret_cast<uint16_t*>(ws), ld, c.T, c.rows, wait);
+    int width = 8;
+    while (width < 256 && width * 8 < c.rows) width *= 2;
+    const int64_t blocks = (c.T + 256 / width - 1) / (256 / width);
+    launched = launch_maybe_pdl(roi_wgrad_align_kernel, int(blocks < cap ? blocks : cap), 256, 0, c.stream, wait, c.dY, c.lddy,
+                                reinterpret_cast<uint16_t*>(ws), ld, c.T, c.rows, width, wait);
     if (launched < 0) return -1;
     dY = reinterpret_cast<const uint16_t*>(ws);
     const size_t used = wgrad_copy_bytes(c.T, c.rows, c.lddy);
