@@ -79,8 +79,13 @@ constexpr int kMinRange = 8, kSplitCost = 8;
 // instead of rounding, all towards zero, which grows with the tokens: 4.3e-7 of the sum's norm at 2000
 // tokens, 1.1e-6 at 4000, 6.8e-6 at 16000, where an fp32 product has 5e-7.  So longer sums are added to
 // acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 841 us with acc, in three pieces, and 590
-// without, where the result is rounded to bf16, 4000 times as coarse, and the sum stays whole.
+// without, where the result is rounded to bf16, 4000 times as coarse.
 constexpr int kMostChunks = 44;
+// The same for a bf16 result alone.  Unbroken, its error against the nearest bf16 number's (1.66e-3 of the norm) is
+// 1.0001 times as large at 32768 tokens, 1.01 at 262144, 1.2 at a million and 3 at four million.  Longer sums are broken
+// off at 32768 tokens and their total is kept in the other half of TMEM, so that the MMAs wait while a piece is added
+// (65536 tokens of 9728 x 3584, one after another: 2723 to 2776 us whole, 2764 to 2775 in two pieces).
+constexpr int kMostAlone = 512;
 
 struct WgradArgs {
   const uint8_t* scales;
@@ -318,9 +323,18 @@ __device__ __forceinline__ void store_block(const WgradArgs& a, bool last, float
 // memory; 1999 tokens of 1215 x 2504 with acc 35 us, 45 element by element from registers).
 enum class Out { kSectors, kPairs, kSingles };
 
-template <Out OUT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
+// The half of TMEM of sum i, and the parity of its turn there.  KEPT: all sums in the first, totals in the second.
+template <bool KEPT>
+__device__ __forceinline__ int half_of(int i) {
+  return KEPT ? 0 : i & 1;
+}
+template <bool KEPT>
+__device__ __forceinline__ uint32_t turn_of(int i) {
+  return uint32_t(KEPT ? i : i >> 1) & 1u;
+}
+
+template <Out OUT, bool KEPT>
+__device__ __forceinline__ void wgrad(const CUtensorMap& tm_dy, const CUtensorMap& tm_codes, const WgradArgs& a) {
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
@@ -428,8 +442,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       // descriptors of the first stage and slot; addresses count in units of 16 bytes
       const uint64_t dy0 = tc_smem_desc_mn128(smem_addr(smem), kHalf), x0 = tc_smem_desc_mn128(smem_addr(smem + kOffSlots), kHalf);
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-        const int b = i & 1;
-        ok = mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim);
+        const int b = half_of<KEPT>(i);
+        ok = mbar_wait_ring_cluster(free + b, turn_of<KEPT>(i) ^ 1u, lim);
         const uint32_t d = tmem + uint32_t(b) * kSide;
         for (int c = w.c0; ok && c < w.c1; ++c, ++committed, ring.next(), slot.next()) {
           ok = mbar_wait_ring_cluster(ready + slot.at, slot.pass, lim);
@@ -494,7 +508,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   } else {
     const int quarter = warp & 3;
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      const int b = i & 1;
+      const int b = half_of<KEPT>(i);
       tile_origin(a, w.tile, m0, n0);
       const int r = int(rank) * kEdge + quarter * 32 + lane;  // row of the tile
       const int64_t m = m0 + r;
@@ -504,15 +518,34 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         for (int q = 0; q < kSide / 32 && n0 + 32 * q < a.cols; ++q)
           asm volatile("prefetch.global.L2 [%0];" ::"l"(a.acc + m * a.cols + n0 + 32 * q));
       }
-      ok = mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim);
+      ok = mbar_wait_ring_cluster(sum + b, turn_of<KEPT>(i), lim);
       if (!ok) break;
       tc_fence_after();
       float4* part = reinterpret_cast<float4*>(a.part) + int64_t(w.slot) * kSide * (kSide / 4) + r;
       for (int q = 0; q < kSide / 32; ++q) {
         uint32_t u[32];
-        tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * kSide + 32 * q), u);
+        const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * kSide + 32 * q);
+        tc_ld32(from, u);
         float v[32];
         input_order(u, v);
+        if (KEPT && w.slot < 0 && !(w.first && w.last)) {
+          // (the total's columns are as they are written out)
+#pragma unroll
+          for (int h = 0; h < 32; h += 16) {
+            uint32_t t[16];
+            if (!w.first) {
+              tc_ld16(from + kSide + h, t);
+#pragma unroll
+              for (int e = 0; e < 16; ++e) v[h + e] += __uint_as_float(t[e]);
+            }
+            if (!w.last) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) t[e] = __float_as_uint(v[h + e]);
+              tc_st16(from + kSide + h, t);
+            }
+          }
+          if (!w.last) continue;
+        }
         if (w.slot >= 0) {
           if (!w.first) {
 #pragma unroll
@@ -555,6 +588,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   tc_fence_after();
   cluster_sync();
   if (warp == 0) tc_dealloc_pair(tmem, kTmemCols);
+}
+
+template <Out OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    roi_wgrad_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
+  wgrad<OUT, false>(tm_dy, tm_codes, a);
+}
+// (a kernel of its own: where the other held both ways, its epilogue spilled more, 35.2 -> 36.4 us for 1999 tokens of
+// 1215 x 2504 with acc)
+template <Out OUT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    roi_wgrad_long_kernel(const __grid_constant__ CUtensorMap tm_dy, const __grid_constant__ CUtensorMap tm_codes, WgradArgs a) {
+  wgrad<OUT, true>(tm_dy, tm_codes, a);
 }
 
 // The tiles of the last round whose tokens were cut: their partial sums in the order of the
@@ -723,7 +769,9 @@ int launch_wgrad(const WgradCall& c) {
   a.scales = c.scales;
   a.dWm = c.dWm;
   a.acc = c.acc;
-  a.unbroken = c.acc != nullptr && a.chunks > kMostChunks ? kMostChunks : a.chunks;
+  const int most = c.acc != nullptr ? kMostChunks : kMostAlone;
+  a.unbroken = a.chunks > most ? most : a.chunks;
+  const bool kept = c.acc == nullptr && a.chunks > most;
   a.part = reinterpret_cast<float*>(ws);
   a.spitch = block8_scale_pitch(c.cols);
   a.status = c.status;
@@ -737,12 +785,13 @@ int launch_wgrad(const WgradCall& c) {
     return -1;
   // whole sectors where the outputs' rows are in sixteens of columns; else through shared memory
   const bool sectors = c.cols % 16 == 0 && ((reinterpret_cast<uintptr_t>(c.dWm) | reinterpret_cast<uintptr_t>(c.acc)) & 31u) == 0;
-  const int form = sectors ? 0 : c.cols % 2 == 0 ? 1 : 2;
-  auto kern = form == 0   ? roi_wgrad_kernel<Out::kSectors>
-              : form == 1 ? roi_wgrad_kernel<Out::kPairs>
-                          : roi_wgrad_kernel<Out::kSingles>;
+  const int form = (sectors ? 0 : c.cols % 2 == 0 ? 1 : 2) + (kept ? 3 : 0);
+  constexpr decltype(&roi_wgrad_kernel<Out::kSectors>) forms[6] = {
+      roi_wgrad_kernel<Out::kSectors>,      roi_wgrad_kernel<Out::kPairs>,      roi_wgrad_kernel<Out::kSingles>,
+      roi_wgrad_long_kernel<Out::kSectors>, roi_wgrad_long_kernel<Out::kPairs>, roi_wgrad_long_kernel<Out::kSingles>};
+  auto kern = forms[form];
   constexpr size_t smem = kSmem + 1024;
-  static std::atomic<bool> set[3][64];
+  static std::atomic<bool> set[6][64];
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return -1;
   if (!set[form][dev].load(std::memory_order_acquire)) {
