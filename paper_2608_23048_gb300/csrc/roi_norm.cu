@@ -19,8 +19,8 @@
 //  - backward: a thread has the same columns of every row it sees, so that the sums of dgamma and dbeta
 //    stay in its registers.  The teams' and then the CTAs' sums are added in a fixed order (through
 //    shared memory, and by a second launch): no atomics, the same bits every time.
-// Rows that start anywhere are copied by the 16-byte granules around them (but for the matrix's own
-// ends) and shifted as they are read; they are written as roi_rows.cuh does.  Rows so wide that
+// Rows that start anywhere are copied by the 16-byte granules around them (those at the matrix's own
+// ends byte by byte) and shifted as they are read; they are written as roi_rows.cuh does.  Rows so wide that
 // two of them do not fit go to kernels that read them again for each step.
 //
 // Measured, 8192 x 3584 bf16 (of 6.79 TB/s copied): RMS norm forward 22.7 us (5.2 TB/s), with y's checkpoint
@@ -33,6 +33,7 @@
 #include <atomic>
 
 #include "roi_block8.cuh"
+#include "roi_extent.h"
 #include "roi_launch.h"
 #include "roi_rows.cuh"
 
@@ -137,27 +138,13 @@ template <bool ANY>
 __device__ __forceinline__ uint32_t row_shift(const void* row) {
   return ANY ? uint32_t(reinterpret_cast<uintptr_t>(row) & 15u) : 0u;
 }
-// What the bulk copy of a row of `bytes` takes: the granules around it, without those that begin before
-// the matrix's first or end after its last byte (`first`, `last`: its first and last row).
-struct Extent {
-  uintptr_t row, end, from, to;
-  __device__ __forceinline__ Extent(const void* p, uint32_t bytes, bool any, bool first, bool last) {
-    row = reinterpret_cast<uintptr_t>(p), end = row + bytes;
-    from = !any ? row : first ? (row + 15) & ~uintptr_t(15) : row & ~uintptr_t(15);
-    to = !any ? end : last ? end & ~uintptr_t(15) : (end + 15) & ~uintptr_t(15);
-  }
-  __device__ __forceinline__ uint32_t bytes() const { return to > from ? uint32_t(to - from) : 0u; }
-  // (one thread) the copy, and before it what it leaves out at the matrix's ends
-  __device__ __forceinline__ void ends(uint8_t* st) const {
-    uint8_t* at = st + (row & 15);
-    for (uintptr_t p = row; p < from && p < end; ++p) at[p - row] = *reinterpret_cast<const uint8_t*>(p);
-    uintptr_t p = to > from ? to : from;
-    for (p = p < row ? row : p; p < end; ++p) at[p - row] = *reinterpret_cast<const uint8_t*>(p);
-  }
-  __device__ __forceinline__ void copy(uint8_t* st, uint64_t* bar) const {
-    if (to > from) bulk_g2s(st + (from - (row & ~uintptr_t(15))), reinterpret_cast<const void*>(from), uint32_t(to - from), bar);
-  }
-};
+__device__ __forceinline__ void copy_row(const Extent& x, uint8_t* st, uint64_t* bar) {
+  if (x.bytes() > 0) bulk_g2s(st + x.offset(), reinterpret_cast<const void*>(x.from), x.bytes(), bar);
+}
+__device__ __forceinline__ Bounds bounds(const void* p, int64_t rows, int64_t pitch, uint32_t width) {
+  const uintptr_t begin = reinterpret_cast<uintptr_t>(p);
+  return {begin, begin + uintptr_t((rows - 1) * pitch) + width};
+}
 // Zeros past the last column.
 template <Elem E>
 __device__ __forceinline__ void clear_past(RowWords<E, 8>& r, int c, int cols) {
@@ -294,13 +281,14 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
   if constexpr (LAYER) stage_param<E>(beta, a.beta, a.params32, cols, padded, 0.0f);
   __syncthreads();
   if (team >= a.shape.teams) {
+    const uint32_t row_bytes = uint32_t(cols) * elem_bytes<E>();
+    const Bounds whole = bounds(a.x, a.rows, a.ldx * elem_bytes<E>(), row_bytes);
     fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
       uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
-      const bool first = row == 0, last = row == a.rows - 1;
-      const Extent x(static_cast<const T*>(a.x) + row * a.ldx, uint32_t(cols) * elem_bytes<E>(), ANY, first, last);
-      if (ANY && (first || last)) x.ends(st);
+      const Extent x(static_cast<const T*>(a.x) + row * a.ldx, row_bytes, ANY, whole);
+      if (ANY && x.cut()) x.ends(st);
       mbar_arrive_expect_tx(bar, x.bytes());
-      x.copy(st, bar);
+      copy_row(x, st, bar);
     });
     return;
   }
@@ -443,25 +431,26 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
   const int teams = a.shape.teams;
   const bool sums_wanted = a.dgamma != nullptr || a.dbeta != nullptr;
   if (team >= teams) {
+    const uint32_t row_bytes = uint32_t(cols) * elem_bytes<E>();
+    const Bounds all_dy = bounds(a.dy, a.rows, a.lddy * elem_bytes<E>(), row_bytes);
+    const Bounds all_x = CKPT ? bounds(a.scales, a.rows, a.spitch, uint32_t(a.spitch)) : bounds(a.x, a.rows, a.ldx * elem_bytes<E>(), row_bytes);
     fill_rings(ts, a.shape, a.rows, lim, a.status, [&](int of, int stage, int64_t row, uint64_t* bar) {
       uint8_t* st = smem + a.shape.params + (size_t(of) * depth + stage) * a.shape.stage;
-      const bool first = row == 0, last = row == a.rows - 1;
-      const uint32_t row_bytes = uint32_t(cols) * elem_bytes<E>();
-      const Extent dy(static_cast<const T*>(a.dy) + row * a.lddy, row_bytes, ANY, first, last);
-      if (ANY && (first || last)) dy.ends(st);
+      const Extent dy(static_cast<const T*>(a.dy) + row * a.lddy, row_bytes, ANY, all_dy);
+      if (ANY && dy.cut()) dy.ends(st);
       if constexpr (CKPT) {
-        const Extent scales(a.scales + row * a.spitch, uint32_t(a.spitch), true, first, last);
-        if (first || last) scales.ends(st + room + a.pitch);
+        const Extent scales(a.scales + row * a.spitch, uint32_t(a.spitch), true, all_x);
+        if (scales.cut()) scales.ends(st + room + a.pitch);
         mbar_arrive_expect_tx(bar, dy.bytes() + uint32_t(a.pitch) + scales.bytes());
         bulk_g2s(st + room, a.codes + row * a.pitch, uint32_t(a.pitch), bar);
-        scales.copy(st + room + a.pitch, bar);
+        copy_row(scales, st + room + a.pitch, bar);
       } else {
-        const Extent x(static_cast<const T*>(a.x) + row * a.ldx, row_bytes, ANY, first, last);
-        if (ANY && (first || last)) x.ends(st + room);
+        const Extent x(static_cast<const T*>(a.x) + row * a.ldx, row_bytes, ANY, all_x);
+        if (ANY && x.cut()) x.ends(st + room);
         mbar_arrive_expect_tx(bar, dy.bytes() + x.bytes());
-        x.copy(st + room, bar);
+        copy_row(x, st + room, bar);
       }
-      dy.copy(st, bar);
+      copy_row(dy, st, bar);
     });
     // the barriers of the others' sums
     if (sums_wanted) {
