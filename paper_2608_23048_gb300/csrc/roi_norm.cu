@@ -229,8 +229,9 @@ __device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
   __syncthreads();
 }
 // A warp that fills rings, a lane a team: `copy(team, stage, row, barrier)` sends a row's copies off.  It
-// gives up when no stage has become free for `lim`; what was sent off lands before it leaves.  (A
-// copy takes a warp some 70 cycles to send off, so the many teams of narrow rows have several.)
+// gives up when no stage has become free for `lim`; what was sent off lands before it leaves, and
+// before what comes after the rings takes their place.  (A copy takes a warp some 70 cycles to send
+// off, so the many teams of narrow rows have several.)
 template <class Copy>
 __device__ __forceinline__ void fill_rings(TeamState& ts, const Shape& s, int64_t rows, uint64_t lim, unsigned int* status, Copy copy) {
   const int team = int(threadIdx.x & 31) * s.fillers + (int(threadIdx.x) - s.teams * s.nt) / 32;
@@ -255,12 +256,11 @@ __device__ __forceinline__ void fill_rings(TeamState& ts, const Shape& s, int64_
       break;
     }
   }
-  const bool gave_up = __any_sync(0xffffffffu, row < rows);
-  if (gave_up || (team < s.teams && ts.gave_up[team] != 0)) {
-    // (a stage's phases end one after another, so the last rows of the ring stand for all)
-    for (int q = k > s.depth ? k - s.depth : 0; q < k; ++q) mbar_wait_bounded(&ts.full[team][q % s.depth], uint32_t(q / s.depth) & 1u);
-  }
-  if (gave_up && (threadIdx.x & 31) == 0) atomicOr(status, kStatusTimeout);
+  if (__any_sync(0xffffffffu, row < rows) && (threadIdx.x & 31) == 0) atomicOr(status, kStatusTimeout);
+  // What was sent off lands, whether or not a team gives up on it, now or later (a stage's phases end one after
+  // another, so the last rows of the ring stand for all).
+  for (int q = k > s.depth ? k - s.depth : 0; q < k; ++q) mbar_wait_bounded(&ts.full[team][q % s.depth], uint32_t(q / s.depth) & 1u);
+  __syncwarp();
 }
 
 // RUN pieces a lane.

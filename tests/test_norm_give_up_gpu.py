@@ -1,0 +1,72 @@
+"""Norms whose bounded waits run out, with more than one row a team.  Every copy is valid and every wait
+bounded: a call that gives up says so in the device status, leaves when its copies have landed, and what
+comes after it is right."""
+import pytest
+
+from test_checkpoint_gpu import roi, values  # noqa: F401  (roi: the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+class Calls:
+    def __init__(self, roi, rows, cols, kind, dtype="bfloat16", gap=0):  # noqa: F811
+        import torch
+        t = getattr(torch, dtype)
+        g = torch.Generator("cuda").manual_seed(rows + cols)
+        new = lambda: torch.randn(rows, cols + gap, device="cuda", generator=g).to(t)[:, :cols]  # noqa: E731
+        self.roi, self.kind, self.x, self.dy = roi, kind, new(), new()
+        self.gamma = (1 + 0.1 * torch.randn(cols, device="cuda", generator=g)).to(t)
+        self.q = roi.new_checkpoint(rows, cols)
+        self.y, self.dx = torch.empty(rows, cols, dtype=t, device="cuda"), torch.empty(rows, cols, dtype=t, device="cuda")
+        self.mean = torch.empty(rows, device="cuda") if kind == "layer" else None
+        self.rstd, self.dg = torch.empty(rows, device="cuda"), torch.empty(cols, device="cuda")
+        self.ws = torch.empty(roi.roi_norm_bwd_workspace_size(rows, cols), dtype=torch.uint8, device="cuda")
+        roi.roi_checkpoint_save(self.x, *self.q)
+        self.calls = [self.fwd, lambda: self.bwd(self.x), lambda: self.bwd(self.q)]
+        self.fwd()
+        # (of the backward: the statistics as they are now)
+        self.stats = None if self.mean is None else self.mean.clone(), self.rstd.clone()
+
+    def fwd(self):
+        self.roi.roi_norm_fwd(self.x, self.kind, self.gamma, None, 1e-5, self.y, self.mean, self.rstd)
+        return self.y, self.rstd
+
+    def bwd(self, x):
+        self.roi.roi_norm_bwd(self.dy, x, self.kind, self.gamma, *self.stats, self.dx, self.dg, None, self.ws)
+        return self.dx, self.dg
+
+
+def same(a, b):
+    import torch
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def others(m):
+    """Work of other kernels that lives in shared memory."""
+    import torch
+    return torch.softmax(m, 1), m @ m.T, m.cumsum(1), m.sort(1).values
+
+
+# 2 to 5 rows a team, all of which fit its ring
+@pytest.mark.parametrize("rows,cols,kind,gap", [(760, 8192, "rms", 0), (760, 8192, "layer", 0), (600, 8001, "rms", 3), (450, 6000, "layer", 0)])
+def test_copies_land_before_the_next_kernel(roi, rows, cols, kind, gap):  # noqa: F811
+    import torch
+    c = Calls(roi, rows, cols, kind, gap=gap)
+    m = torch.randn(1024, 1500, device="cuda")
+    for call in c.calls:
+        want, beside = [t.clone() for t in call()], others(m)
+        roi.roi_device_status()
+        got = []
+        roi.roi_set_ring_wait_limit_ns(0)
+        try:
+            for _ in range(20):
+                call()
+                got.append(others(m))
+            with pytest.raises(roi.RoiError) as err:
+                roi.roi_device_status()
+            assert err.value.status == 8
+        finally:
+            roi.roi_set_ring_wait_limit_ns(roi.ROI_DEFAULT_RING_WAIT_NS)
+        assert all(same(beside, g) for g in got)
+        assert same(want, call())
+        roi.roi_device_status()
