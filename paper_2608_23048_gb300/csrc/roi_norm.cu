@@ -228,6 +228,10 @@ __device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
   fence_mbar_init();
   __syncthreads();
 }
+// Whether a row has landed, one answer for the warp.
+__device__ __forceinline__ bool row_landed(uint64_t* full, uint32_t parity, uint64_t lim) {
+  return __all_sync(0xffffffffu, mbar_wait_ring(full, parity, lim));
+}
 // A warp that fills rings, a lane a team: `copy(team, stage, row, barrier)` sends a row's copies off.  It
 // gives up when no stage has become free for `lim`; what was sent off lands before it leaves, and
 // before what comes after the rings takes their place.  (A copy takes a warp some 70 cycles to send
@@ -310,7 +314,8 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
     return v;
   };
   for (int64_t row = row0; row < a.rows; row += all) {
-    if (!mbar_wait_ring(&ts.full[team][at], pass, lim)) ts.gave_up[team] = 1;
+    const bool landed = row_landed(&ts.full[team][at], pass, lim);
+    if (!landed) ts.gave_up[team] = 1;
     const uint8_t* st = ring + at * a.shape.stage;
     const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.x) + row * a.ldx);
     RowWords<E, 8> x[RUN];
@@ -325,8 +330,9 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
         sum = sum + ((v.v[0] + v.v[1]) + (v.v[2] + v.v[3]));
       }
     }
+    // (the stage of a row that did not land stays taken: its copy may still be on its way)
     __syncwarp();
-    if (lane == 0) mbar_arrive(&ts.empty[team][at]);
+    if (landed && lane == 0) mbar_arrive(&ts.empty[team][at]);
     float mean = 0.0f;
     if constexpr (LAYER) mean = meet(total(sum)) * inv_cols;
     const F2 minus = f2(-mean);
@@ -480,7 +486,8 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       next_rstd = __ldg(a.rstd + after);
       if constexpr (LAYER) next_mean = __ldg(a.mean + after);
     }
-    if (!mbar_wait_ring(&ts.full[team][at], pass, lim)) ts.gave_up[team] = 1;
+    const bool landed = row_landed(&ts.full[team][at], pass, lim);
+    if (!landed) ts.gave_up[team] = 1;
     const uint8_t* st = ring + at * a.shape.stage;
     const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.dy) + row * a.lddy);
     const uint32_t ms = CKPT ? row_shift<true>(a.scales + row * a.spitch) : 0u;
@@ -535,8 +542,9 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       if constexpr (KEEP) raw[i] = words;
       else w[i] = p;
     }
+    // (the stage of a row that did not land stays taken: its copy may still be on its way)
     __syncwarp();
-    if (lane == 0) mbar_arrive(&ts.empty[team][at]);
+    if (landed && lane == 0) mbar_arrive(&ts.empty[team][at]);
     float c1 = warp_sum(total(s1)), c2 = LAYER ? warp_sum(total(s2)) : 0.0f;
     if (nt > 32 && lane == 0) {
       ts.slots[turn][warp0 + warp][0] = c1;

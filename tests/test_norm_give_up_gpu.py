@@ -70,3 +70,25 @@ def test_copies_land_before_the_next_kernel(roi, rows, cols, kind, gap):  # noqa
         assert all(same(beside, g) for g in got)
         assert same(want, call())
         roi.roi_device_status()
+
+
+# teams with many more rows than their rings are deep; every warp gives up at its first row
+@pytest.mark.parametrize("rows,cols,kind,gap,dtype", [(8000, 8192, "rms", 0, "bfloat16"), (8000, 8192, "layer", 0, "bfloat16"),
+                                                      (9000, 4100, "rms", 3, "float16"), (4000, 4096, "layer", 0, "float32"),
+                                                      (90000, 256, "layer", 0, "bfloat16"), (60000, 1001, "rms", 0, "float32")])
+def test_long_rings(roi, rows, cols, kind, gap, dtype):  # noqa: F811
+    c = Calls(roi, rows, cols, kind, dtype, gap)
+    for call in c.calls:
+        want = [t.clone() for t in call()]
+        roi.roi_device_status()
+        roi.roi_set_ring_wait_limit_ns(0)
+        try:
+            for _ in range(5):
+                call()
+            with pytest.raises(roi.RoiError) as err:
+                roi.roi_device_status()
+            assert err.value.status == 8
+        finally:
+            roi.roi_set_ring_wait_limit_ns(roi.ROI_DEFAULT_RING_WAIT_NS)
+        assert same(want, call())
+        roi.roi_device_status()
