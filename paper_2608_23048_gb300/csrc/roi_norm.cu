@@ -211,12 +211,15 @@ constexpr int kRun = E == Elem::kFp32 ? 2 : 4;
 template <bool LAYER, bool ANY>
 constexpr int kFwdThreads = LAYER && ANY ? 640 : 768;
 constexpr int kThreads = 1024, kMostTeams = 32, kMostNamed = 15, kMostDepth = 8;
-// Barriers, slots and flags of the teams.
+// Barriers, slots and lost rows of the teams.
 struct TeamState {
   uint64_t full[kMostTeams][kMostDepth];   // the row has landed
   uint64_t empty[kMostTeams][kMostDepth];  // every warp has read it
   float slots[3][kThreads / 32][2];  // a set is written again two meetings later
-  int gave_up[kMostTeams];
+  // Whether the row of a turn did not land for a warp of the team, written before the row's meeting and read
+  // after it, so that the team breaks off together.  (A warp that has gone on to its next row may write while the others
+  // still read for this one; with one flag for all rows they would part, and one part would wait for ever.)
+  int lost[3][kMostTeams];
 };
 // The barriers of the rings (the whole CTA).
 __device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
@@ -224,7 +227,7 @@ __device__ __forceinline__ void init_teams(TeamState& ts, const Shape& s) {
     mbar_init(&ts.full[i / s.depth][i % s.depth], 1);
     mbar_init(&ts.empty[i / s.depth][i % s.depth], s.nt / 32);
   }
-  if (threadIdx.x < kMostTeams) ts.gave_up[threadIdx.x] = 0;
+  for (int i = threadIdx.x; i < 3 * kMostTeams; i += blockDim.x) ts.lost[i / kMostTeams][i % kMostTeams] = 0;
   fence_mbar_init();
   __syncthreads();
 }
@@ -315,7 +318,8 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
   };
   for (int64_t row = row0; row < a.rows; row += all) {
     const bool landed = row_landed(&ts.full[team][at], pass, lim);
-    if (!landed) ts.gave_up[team] = 1;
+    const int of = turn;
+    if (!landed) ts.lost[of][team] = 1;
     const uint8_t* st = ring + at * a.shape.stage;
     const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.x) + row * a.ldx);
     RowWords<E, 8> x[RUN];
@@ -357,7 +361,10 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
       for (int k = 0; k < 4; ++k) squares = vfma(v.v[k], v.v[k], squares);
     }
     const float rstd = 1.0f / sqrtf(meet(total(squares)) * inv_cols + a.eps);
-    if (ts.gave_up[team]) break;  // (the whole team)
+    if (ts.lost[of][team] != 0) {  // (the whole team)
+      if (t == 0) atomicOr(a.status, kStatusTimeout);
+      break;
+    }
     if (t == 0) {
       if (LAYER && a.mean != nullptr) a.mean[row] = mean;
       if (a.rstd != nullptr) a.rstd[row] = rstd;
@@ -403,7 +410,6 @@ __global__ void __launch_bounds__(RUN == 1 ? kThreads : kFwdThreads<LAYER, ANY>)
     }
     if (++at == depth) at = 0, pass ^= 1u;
   }
-  if (ts.gave_up[team] && t == 0) atomicOr(a.status, kStatusTimeout);
 }
 
 // First column of run i of a team's thread t, with NP runs a thread.
@@ -487,7 +493,7 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       if constexpr (LAYER) next_mean = __ldg(a.mean + after);
     }
     const bool landed = row_landed(&ts.full[team][at], pass, lim);
-    if (!landed) ts.gave_up[team] = 1;
+    if (!landed) ts.lost[turn][team] = 1;
     const uint8_t* st = ring + at * a.shape.stage;
     const uint32_t m = row_shift<ANY>(static_cast<const T*>(a.dy) + row * a.lddy);
     const uint32_t ms = CKPT ? row_shift<true>(a.scales + row * a.spitch) : 0u;
@@ -551,12 +557,15 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
       if constexpr (LAYER) ts.slots[turn][warp0 + warp][1] = c2;
     }
     team_sync(team, nt);
-    if (ts.gave_up[team]) break;  // (the whole team)
+    if (ts.lost[turn][team] != 0) {  // (the whole team)
+      if (t == 0) atomicOr(a.status, kStatusTimeout);
+      break;
+    }
     if (nt > 32) {
       c1 = warp_sum(lane < warps ? ts.slots[turn][warp0 + lane][0] : 0.0f);
       if constexpr (LAYER) c2 = warp_sum(lane < warps ? ts.slots[turn][warp0 + lane][1] : 0.0f);
-      turn = turn == 2 ? 0 : turn + 1;
     }
+    turn = turn == 2 ? 0 : turn + 1;
     // dx = rstd a - rstd mean(a) - xh (rstd mean(a xh))
     const F2 k1 = f2(-(c1 * inv_cols) * rstd), k2 = f2(-(c2 * inv_cols) * rstd);
     RowWords<E, 8> before;
@@ -588,7 +597,6 @@ __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
     to += all * a.lddx;
     if (++at == depth) at = 0, pass ^= 1u;
   }
-  if (ts.gave_up[team] && t == 0) atomicOr(a.status, kStatusTimeout);
   if (!sums_wanted) return;
   __syncthreads();  // the rings are done with
   // the teams' sums in their order, then this CTA's to its place among the partial sums (the outputs

@@ -92,3 +92,32 @@ def test_long_rings(roi, rows, cols, kind, gap, dtype):  # noqa: F811
             roi.roi_set_ring_wait_limit_ns(roi.ROI_DEFAULT_RING_WAIT_NS)
         assert same(want, call())
         roi.roi_device_status()
+
+
+# teams of one, two and many warps
+@pytest.mark.parametrize("rows,cols,kind,gap,dtype", [(8000, 8192, "layer", 0, "bfloat16"), (9000, 4100, "rms", 3, "float16"),
+                                                      (3000, 9000, "layer", 0, "bfloat16"), (90000, 256, "rms", 0, "bfloat16"),
+                                                      (60000, 1001, "layer", 0, "float32"), (300, 3584, "layer", 0, "bfloat16")])
+def test_small_limits(roi, rows, cols, kind, gap, dtype):  # noqa: F811
+    """Limits around the time that a copy takes, so that some waits of a team run out and some do not, at any
+    row: every call returns, and either says that it gave up or is right.  (Which of the two is the clock's
+    affair.)"""
+    c = Calls(roi, rows, cols, kind, dtype, gap)
+    for call in c.calls:
+        want = [t.clone() for t in call()]
+        roi.roi_device_status()
+        try:
+            for ns in (1, 50, 200, 500, 1000, 2000, 3000, 5000, 10000, 30000, 100000):
+                roi.roi_set_ring_wait_limit_ns(ns)
+                for _ in range(10):
+                    got = call()
+                    try:
+                        roi.roi_device_status()
+                    except roi.RoiError as err:
+                        assert err.status == 8
+                    else:
+                        assert same(want, got), ns
+        finally:
+            roi.roi_set_ring_wait_limit_ns(roi.ROI_DEFAULT_RING_WAIT_NS)
+        assert same(want, call())
+        roi.roi_device_status()
