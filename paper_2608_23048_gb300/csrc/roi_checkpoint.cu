@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_rows_kernel(Save
   const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
   const int64_t stride = int64_t(gridDim.x) * (kThreads / 32) * kUnits;
   for (int64_t t = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits; t < tasks; t += stride) {
-    Window<E, 16, false> x[kUnits];
+    Window<E, 16> x[kUnits];
     int64_t row[kUnits], j[kUnits];
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {

@@ -115,18 +115,17 @@ __device__ __forceinline__ void block8_codes(const RowWords<E, N>& r, uint32_t t
   }
 }
 
-// N elements from column c of a row on, on their way: ALIGNED (rows start on 16-byte boundaries) as
-// they are, else the granules around them.
-template <Elem E, int N, bool ALIGNED>
+// N elements from column c of a row on, on their way: the granules around them.
+template <Elem E, int N>
 struct Window {
   using R = RowWords<E, N>;
   static constexpr int kWords = R::kWords;
-  uint32_t w[ALIGNED ? kWords : kWords + 4];
-  uint32_t m;  // (not ALIGNED)
+  uint32_t w[kWords + 4];
+  uint32_t m;
 
   __device__ __forceinline__ void zero() {
 #pragma unroll
-    for (int i = 0; i < (ALIGNED ? kWords : kWords + 4); ++i) w[i] = 0;
+    for (int i = 0; i < kWords + 4; ++i) w[i] = 0;
     m = 0;
   }
   __device__ __forceinline__ void load(const typename ElemType<E>::T* row, int64_t c, int64_t cols) {
@@ -136,13 +135,12 @@ struct Window {
       return;
     }
     const typename ElemType<E>::T* p = row + c;
-    m = ALIGNED ? 0u : uint32_t(reinterpret_cast<uintptr_t>(p) & 15u);
+    m = uint32_t(reinterpret_cast<uintptr_t>(p) & 15u);
     // whole granules inside the row
-    const bool inside = ALIGNED ? left >= N : c * elem_bytes<E>() >= m && left * elem_bytes<E>() + m >= kWords * 4 + 16;
-    if (inside) {
+    if (c * elem_bytes<E>() >= m && left * elem_bytes<E>() + m >= kWords * 4 + 16) {
       const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) - m);
 #pragma unroll
-      for (int i = 0; i < (ALIGNED ? kWords / 4 : kWords / 4 + 1); ++i) {
+      for (int i = 0; i < kWords / 4 + 1; ++i) {
         const uint4 v = __ldg(q + i);
         w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
       }
@@ -154,14 +152,7 @@ struct Window {
       for (int i = 0; i < kWords; ++i) w[i] = r.u[i];
     }
   }
-  __device__ __forceinline__ void get(R& r) const {
-    if constexpr (ALIGNED) {
-#pragma unroll
-      for (int i = 0; i < kWords; ++i) r.u[i] = w[i];
-    } else {
-      shift_words<kWords>(w, m, r.u);
-    }
-  }
+  __device__ __forceinline__ void get(R& r) const { shift_words<kWords>(w, m, r.u); }
 };
 
 // All lanes of a warp, in groups of `width` (a power of two) with a row each: lane l of a group

@@ -684,7 +684,7 @@ __global__ void __launch_bounds__(256) roi_wgrad_align_kernel(const uint16_t* sr
   for (int64_t t = int64_t(blockIdx.x) * per + threadIdx.x / width; t < T; t += int64_t(gridDim.x) * per) {
 #pragma unroll 2
     for (int64_t c = 8 * j; c < cols; c += 8 * width) {
-      Window<Elem::kBf16, 8, false> x;
+      Window<Elem::kBf16, 8> x;
       x.load(reinterpret_cast<const E*>(src) + t * ld, c, cols);
       RowWords<Elem::kBf16, 8> r;
       x.get(r);
