@@ -328,6 +328,8 @@ roi_status roi_hard_mask_export(const float* logits, int N, int M, int64_t rows,
  * Matrices of these calls (x, y, dy, dx, dY) are row-major with a row stride ld in
  * elements, ld >= cols, and need only the alignment of their elements, except dY;
  * base pointers and strides that are multiples of 16 bytes take the fast paths.
+ * gamma, beta, out_dWm, acc and workspaces are 16-byte aligned; mean, rstd, out_dgamma
+ * and out_dbeta need 4 bytes.
  * Outputs may lie between the rows of inputs, but not on them.
  *
  * A checkpoint is a pair of arrays.  Blocks of 32 consecutive columns of a row share

@@ -7,9 +7,9 @@
 // all rows follow one another and every access is whole sectors; elsewhere a warp, or a part of
 // one, has a row of its own and goes by granules (roi_rows.cuh).
 //
-// Measured, 8192 x 18944 (of 6.79 TB/s copied): bf16 save 82 us (5.75 TB/s), load 77 to 83; fp32 save 115 (6.79),
-// load 125 to 128 (6.1 to 6.3; stores alone run at 3.9 TB/s here).  A save in bf16 issues in 60 % of the cycles, a load waits
-// for memory.  Rows that start anywhere, 8192 x 18943 bf16: 93 and 117 us.  The same aligned matrices through the kernels
+// Measured, 8192 x 18944 (of 6.79 TB/s copied): bf16 save 82 us (5.75 TB/s), load 77 to 84; fp32 save 115 (6.79),
+// load 121 to 128 (6.1 to 6.4; stores alone run at 3.9 TB/s here).  A save in bf16 issues in 60 % of the cycles, a load waits
+// for memory.  Rows that start anywhere, 8192 x 18943 bf16: 93 and 131 us.  The same aligned matrices through the kernels
 // of rows that start anywhere: bf16 91 and 102 us, fp32 125 and 156.
 #include "roi_block8.cuh"
 #include "roi_launch.h"

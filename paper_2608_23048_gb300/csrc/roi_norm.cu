@@ -23,13 +23,15 @@
 // ends byte by byte) and shifted as they are read; they are written as roi_rows.cuh does.  Rows so wide that
 // two of them do not fit go to kernels that read them again for each step.
 //
-// Measured, 8192 x 3584 bf16 (of 6.79 TB/s copied): RMS norm forward 22.7 us (5.2 TB/s), with y's checkpoint
-// 35.8, layer norm 33; RMS norm backward 41.5 us from x (4.2 TB/s), 41.6 from its checkpoint, 7 of which are the
-// sums' (their places in memory and the second launch), layer norm 45.7 and 47.4.  With rows loaded
-// by the threads that use them: RMS norm forward 48 us, layer norm 46, RMS norm backward from the checkpoint 52.  What is
-// left is instructions: the forward with y's checkpoint issues in 56 % of the cycles, the backward in 47 %, with 15 to 22
-// warps an SM.  Rows that start anywhere (8192
-// x 3583) take 1.5 to 1.7 times as long, for the shifts.
+// Measured, 8192 x 3584 bf16 (of 6.79 TB/s copied): RMS norm forward 22.8 us (5.2 TB/s), with y's checkpoint
+// 35.8, layer norm 31.4; RMS norm backward 39.4 us from x (4.5 TB/s), 42.0 from its checkpoint, 7 of which are the
+// sums' (their places in memory and the second launch), layer norm 45.2 and 49.0.  fp32: RMS norm 44.3 (5.3 TB/s) forward,
+// 67.4 and 55.8 backward; layer norm 51.9, 68.0 and 59.4.  With rows loaded
+// by the threads that use them: RMS norm forward 48 us, layer norm 46, RMS norm backward from the checkpoint 52.
+// The forward with y's checkpoint issues in 57 % of the cycles and the backward in 59 %, with 20 to 22 warps an SM, which
+// wait for instructions before (`wait`), shared memory and their teams' meetings.  Rows that start anywhere (8192
+// x 3583) take 1.5 to 1.8 times as long, for the shifts and, in the backward, for registers (roi_norm_bwd_kernel).
+// Rows too wide for a ring, 2048 x 16384: backward 186 to 243 us, 6 to 10 times its floor, three passes over everything.
 #include <atomic>
 
 #include "roi_block8.cuh"
@@ -417,14 +419,17 @@ template <int NP>
 __device__ __forceinline__ int column(int i, int t) { return ((t >> 5) * NP + i) * 256 + (t & 31) * 8; }
 
 // What a thread keeps of dy until dx is written: dy as it was read where that is half the registers (16
-// bits) and they are short, else its product with gamma.  bf16, x from memory: RMS norm 8192 x 3584 41.6 us
+// bits) and they are short, else its product with gamma.  bf16, x from memory: RMS norm 8192 x 3584 39.4 us
 // with dy in 768 threads (46 in 640) and 50 with the product in 640; layer norm 8192 x 8192 98 us with dy
 // and 130 with the product in 640; 8192 x 3584 46 us with the product and 53 with dy, both in 512.
 template <Elem E, bool LAYER, int THREADS>
 constexpr bool kKeepDy = E != Elem::kFp32 && (!LAYER || THREADS > 512);
 
-// THREADS: what leaves two pieces a thread their registers; 1024 for one piece, and for rows too wide for
-// these.
+// THREADS: 1024 for one piece; for two pieces what leaves them their registers where rows are whole granules (spills of 0
+// to 28 bytes).  These numbers were chosen by such rows; rows that start anywhere have the same and spill 20 to 300 bytes (RMS
+// norm in 16 bits 116, layer norm in 640 threads 140 to 172), and so does one piece, up to 124.  Rows too wide for
+// these take two pieces in 1024 threads (RMS norm in 16 bits from 11777 columns on, layer norm and fp32 from 9729) and spill
+// 152 to 584 bytes: RMS norm 4096 x 12288 bf16 94 us from x, layer norm 152, against 83 and 99 at 8192 x 8192.
 template <Elem E, bool LAYER, bool CKPT, bool ANY, int NP, int THREADS>
 __global__ void __launch_bounds__(THREADS) roi_norm_bwd_kernel(BwdArgs a) {
   using T = typename ElemType<E>::T;
@@ -921,8 +926,8 @@ int bwd(const NormBwdCall& c, BwdArgs& a) {
   // (the teams' sums take the place of the rings)
   const size_t least = size_t(kinds) * 8 * size_t((pieces + np - 1) / np * np) * 32 * 4;
   const int64_t nt = (pieces + np - 1) / np * 32;
-  // (layer norm, 8192 rows, from the checkpoint, 512 threads against 640: 3584 columns 47 and 66 us, 2048 columns
-  // 31 and 34; the sums of dbeta take registers, and 512 hold no two teams of more than 240 threads)
+  // (layer norm, 8192 rows, from the checkpoint, 512 threads against 640: 3584 columns 49 and 54 us, 2048 columns
+  // 31.5 and 31.7, from x 45 and 52, 28 and 31; the sums of dbeta take registers, and 512 hold no two teams of more than 240 threads)
   constexpr int kFew = E != Elem::kFp32 && !LAYER ? 768 : 640;
   const int threads = np == 1 || nt > kFew - 32 ? 1024 : LAYER && nt <= 240 ? 512 : kFew;
   a.shape = shape_of(a.rows, a.cols, pieces, np, threads, stage, params, least);

@@ -23,7 +23,8 @@
 // chunk 1888 us; without that release 982; two sets of converting warps and the scales staged apart
 // 867; even bytes converted where they are 727; rings of their own and loops of whole warps
 // around the MMAs, so that descriptors stay in uniform registers, 631; whole sectors out 583 to 600,
-// which is 1860 to 1910 TFLOP/s.  Under a long load the clock falls with the power (681 us).
+// which is 1860 to 1910 TFLOP/s; waits that a whole warp answers as one 605.  Under a long load the clock falls with the
+// power (697 us).
 // Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
 //
 // Tiles go to the pairs in rounds.  In the last, partial round the tokens of
@@ -78,7 +79,7 @@ constexpr int kMinRange = 8, kSplitCost = 8;
 // The most chunks that TMEM sums unbroken for acc.  The tensor cores drop the bits below their sum's last
 // instead of rounding, all towards zero, which grows with the tokens: 4.3e-7 of the sum's norm at 2000
 // tokens, 1.1e-6 at 4000, 6.8e-6 at 16000, where an fp32 product has 5e-7.  So longer sums are added to
-// acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 841 us with acc, in three pieces, and 590
+// acc in pieces, rounded in fp32: at most 6.3e-7.  8192 tokens, 18944 x 3584: 846 us with acc, in three pieces, and 605
 // without, where the result is rounded to bf16, 4000 times as coarse.
 constexpr int kMostChunks = 44;
 // The same for a bf16 result alone.  Unbroken, its error against the nearest bf16 number's (1.66e-3 of the norm) is
