@@ -61,7 +61,7 @@ typedef enum {
     ROI_ERR_CUDA = 7,      /* launch failed (cudaGetLastError after the launch)          */
     ROI_ERR_TIMEOUT = 8,   /* a kernel gave up waiting on its own copies (see below)     */
     ROI_ERR_OPT = 9,       /* bad optimizer settings (roi_mask_bwd_adamw)                */
-    ROI_ERR_TYPE = 10      /* unknown element type or norm kind, or eps not finite >= 0  */
+    ROI_ERR_TYPE = 10      /* unknown element type, format or norm kind, or eps not finite >= 0 */
 } roi_status;
 
 /* Element types of the calls that take more than one. */
@@ -428,6 +428,52 @@ size_t roi_masked_linear_wgrad_workspace_size(int64_t T, int64_t rows, int64_t c
 roi_status roi_masked_linear_wgrad(const roi_bf16* dY, int64_t lddy, const int8_t* codes, const uint8_t* scales,
                                    int64_t T, int64_t rows, int64_t cols, roi_bf16* out_dWm, float* acc,
                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The masked layers' other two products, in 8-bit floating point.  A copy is a pair of arrays: codes in e4m3 or e5m2
+ * (largest numbers 448 and 57344) and, for every block, a scale byte s that multiplies them by 2^(s - 127).
+ *   of an activation x [rows, cols]: blocks of 128 consecutive columns of a row
+ *     codes [rows, roi_fp8_pitch(cols)]: cols rounded up to 128; scales [rows, roi_fp8_scale_pitch(cols)]: 16 for
+ *     every 2048 columns begun
+ *   of a weight [rows, cols]: e4m3, blocks of 128 x 128; codes the same, scales [ceil(rows / 128),
+ *     roi_fp8_scale_pitch(cols)].  One copy serves both products.
+ * s - 127 is the least exponent e >= -126 with the block's largest magnitude <= 448 * 2^e (57344 * 2^e); a code is
+ * x * 2^(127 - s) rounded to the format, ties to even.  A block with an infinity or a NaN has s = 255 and codes 0
+ * and makes every sum NaN that it is part of.  Padding codes are 0, padding scales 1.  Both arrays are
+ * contiguous and 16-byte aligned, as every row of theirs is: an activation's copy may be saved and used in slices of rows,
+ * a weight's in slices of 128.
+ */
+typedef enum {
+    ROI_E4M3 = 0,
+    ROI_E5M2 = 1
+} roi_fp8_format;
+int64_t roi_fp8_pitch(int64_t cols);
+int64_t roi_fp8_scale_pitch(int64_t cols);
+
+/* Copies x [rows, cols] of type dtype (roi_dtype), row stride ldx, aligned to its elements; rows and cols at most 2^30.
+ *  format: roi_fp8_format (e4m3 for activations; e5m2, a longer range and one bit less, for gradients)          */
+roi_status roi_fp8_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int format,
+                        uint8_t* out_codes, uint8_t* out_scales, void* stream);
+
+/* Copies a weight [rows, cols] (the mask forward's out_Wm; contiguous, 16-byte aligned). */
+roi_status roi_fp8_save_weight(const roi_bf16* W, int64_t rows, int64_t cols, uint8_t* out_codes, uint8_t* out_scales,
+                               void* stream);
+
+/* The layer's forward, Y[t, r] = sum_c x^[t, c] w^[r, c], and the gradient of its input,
+ * dX[t, c] = sum_r dy^[t, r] w^[r, c], x^, w^, dy^ the values that the copies stand for.  Products are exact,
+ * sums in fp32 on the tensor cores' block-scaled instructions, rounded once to dtype.
+ *  x_codes, x_scales, format    the copy of x [T, cols]
+ *  dy_codes, dy_scales, format  the copy of dy [T, rows]
+ *  w_codes, w_scales            the copy of the weight [rows, cols]
+ *  out_y [T, rows], out_dx [T, cols]  of type dtype, row stride ldy, lddx, aligned to their elements
+ * T, rows and cols at most 2^30.  Sums are taken in an order that depends on sizes and GPU, not on timing.  A
+ * gradient over no outputs (rows == 0) is 0.  roi_device_status reports a kernel that gave up waiting on its copies.    */
+roi_status roi_fp8_linear_fwd(const uint8_t* x_codes, const uint8_t* x_scales, int format, const uint8_t* w_codes,
+                              const uint8_t* w_scales, int64_t T, int64_t rows, int64_t cols, void* out_y, int dtype,
+                              int64_t ldy, void* stream);
+roi_status roi_fp8_linear_dgrad(const uint8_t* dy_codes, const uint8_t* dy_scales, int format, const uint8_t* w_codes,
+                                const uint8_t* w_scales, int64_t T, int64_t rows, int64_t cols, void* out_dx, int dtype,
+                                int64_t lddx, void* stream);
 
 /* The noise of a call, materialised (for inspecting or reproducing a sample; the
  * mask calls never store it).  st->lambda is ignored; st->row_offset applies.

@@ -21,6 +21,8 @@ __all__ = [
     "roi_checkpoint_pitch", "roi_checkpoint_scale_pitch", "roi_checkpoint_save", "roi_checkpoint_load",
     "new_checkpoint", "roi_norm_fwd", "roi_norm_bwd", "roi_norm_bwd_workspace_size",
     "roi_masked_linear_wgrad", "roi_masked_linear_wgrad_workspace_size",
+    "roi_fp8_pitch", "roi_fp8_scale_pitch", "new_fp8", "new_fp8_weight", "roi_fp8_save", "roi_fp8_save_weight",
+    "roi_fp8_linear_fwd", "roi_fp8_linear_dgrad",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -129,6 +131,14 @@ def lib() -> ctypes.CDLL:
     L.roi_masked_linear_wgrad.argtypes = [_P, i64, _P, _P, i64, i64, i64, _P, _P, _P, ctypes.c_size_t, _P]
     L.roi_masked_linear_wgrad_workspace_size.argtypes = [i64, i64, i64, i64]
     L.roi_masked_linear_wgrad_workspace_size.restype = ctypes.c_size_t
+    L.roi_fp8_pitch.argtypes = [i64]
+    L.roi_fp8_pitch.restype = i64
+    L.roi_fp8_scale_pitch.argtypes = [i64]
+    L.roi_fp8_scale_pitch.restype = i64
+    L.roi_fp8_save.argtypes = [_P, i32, i64, i64, i64, i32, _P, _P, _P]
+    L.roi_fp8_save_weight.argtypes = [_P, i64, i64, _P, _P, _P]
+    for name in ("roi_fp8_linear_fwd", "roi_fp8_linear_dgrad"):
+        getattr(L, name).argtypes = [_P, _P, i32, _P, _P, i64, i64, i64, _P, i32, i64, _P]
     L.roi_device_status.argtypes = [_P]
     L.roi_set_ring_wait_limit_ns.argtypes = [u64]
     L.roi_noise_words.argtypes = [ctypes.POINTER(NoiseState), i64, i64, _P, _P]
@@ -143,7 +153,8 @@ def lib() -> ctypes.CDLL:
                  "roi_masked_linear_fwd_noalloc", "roi_mask_fwd_batch", "roi_mask_bwd_batch",
                  "roi_mask_bwd_adamw_batch", "roi_mask_fwd_st_batch", "roi_mask_bwd_st_batch",
                  "roi_set_ring_wait_limit_ns", "roi_checkpoint_save", "roi_checkpoint_load", "roi_norm_fwd",
-                 "roi_norm_bwd", "roi_masked_linear_wgrad"):
+                 "roi_norm_bwd", "roi_masked_linear_wgrad", "roi_fp8_save", "roi_fp8_save_weight", "roi_fp8_linear_fwd",
+                 "roi_fp8_linear_dgrad"):
         getattr(L, name).restype = i32
     _LIB = L
     return L
@@ -677,6 +688,94 @@ def roi_masked_linear_wgrad(dY, x_checkpoint, out_dWm=None, acc=None, workspace=
     s = lib().roi_masked_linear_wgrad(dY.data_ptr(), lddy, codes, scales, T, rows, cols, _ptr(out_dWm), _ptr(acc), ws,
                                       ws_bytes, _stream(stream))
     _raise(s, "roi_masked_linear_wgrad")
+
+
+# ---------------------------------------------------------------------------
+# the masked layers' products in 8-bit floating point
+# ---------------------------------------------------------------------------
+FP8_FORMATS = {"e4m3": 0, "e5m2": 1}
+
+
+def _format(format):
+    code = FP8_FORMATS.get(format)
+    if code is None:
+        raise ValueError(f"format: expected one of {sorted(FP8_FORMATS)}, got {format!r}")
+    return code
+
+
+def roi_fp8_pitch(cols) -> int:
+    """Codes in a row of a copy of `cols` columns."""
+    return int(lib().roi_fp8_pitch(int(cols)))
+
+
+def roi_fp8_scale_pitch(cols) -> int:
+    """Scale bytes in a row of a copy of `cols` columns."""
+    return int(lib().roi_fp8_scale_pitch(int(cols)))
+
+
+def new_fp8(rows, cols, device="cuda"):
+    """Uninitialised (codes, scales) for the copy of an activation [rows, cols]."""
+    import torch
+    return (torch.empty(rows, roi_fp8_pitch(cols), dtype=torch.uint8, device=device),
+            torch.empty(rows, roi_fp8_scale_pitch(cols), dtype=torch.uint8, device=device))
+
+
+def new_fp8_weight(rows, cols, device="cuda"):
+    """Uninitialised (codes, scales) for the copy of a weight [rows, cols]."""
+    import torch
+    return (torch.empty(rows, roi_fp8_pitch(cols), dtype=torch.uint8, device=device),
+            torch.empty((rows + 127) // 128, roi_fp8_scale_pitch(cols), dtype=torch.uint8, device=device))
+
+
+def _fp8(pair, name, rows, cols, weight=False):
+    """Addresses of a copy's codes and scales (of a matrix [rows, cols])."""
+    import torch
+    codes, scales = pair
+    _check_tensor(codes, f"{name} codes", torch.uint8, (rows, (cols + 127) // 128 * 128))
+    _check_tensor(scales, f"{name} scales", torch.uint8, ((rows + 127) // 128 if weight else rows, (cols + 2047) // 2048 * 16))
+    return codes.data_ptr(), scales.data_ptr()
+
+
+def roi_fp8_save(x, format, out_codes, out_scales, stream=None):
+    """Copies x [rows, cols] (bfloat16, float16 or float32; rows may be apart) in 8-bit floating point
+    ("e4m3" or "e5m2") with a power of two for every 128 columns of a row."""
+    ld = _stride(x, "x")
+    rows, cols = x.shape
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols)
+    s = lib().roi_fp8_save(x.data_ptr(), _type(x, "x"), rows, cols, ld, _format(format), codes, scales, _stream(stream))
+    _raise(s, "roi_fp8_save")
+
+
+def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
+    """Copies a weight [rows, cols] (bfloat16) in e4m3 with a power of two for every block of 128 x 128."""
+    import torch
+    rows, cols = W.shape
+    _check_tensor(W, "W", torch.bfloat16)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, True)
+    s = lib().roi_fp8_save_weight(W.data_ptr(), rows, cols, codes, scales, _stream(stream))
+    _raise(s, "roi_fp8_save_weight")
+
+
+def _fp8_linear(name, dgrad, x8, format, w8, out, stream):
+    ld = _stride(out, "out")
+    T, outs = out.shape
+    rows = w8[0].shape[0]
+    # the columns of the sum, or of the weight: padding is zeros, so a whole number of blocks stands for them
+    cols = outs if dgrad else w8[0].shape[1]
+    xq, xs = _fp8(x8, "x8", T, rows if dgrad else cols)
+    wq, ws = _fp8(w8, "w8", rows if dgrad else outs, cols, True)
+    s = getattr(lib(), name)(xq, xs, _format(format), wq, ws, T, rows, cols, out.data_ptr(), _type(out, "out"), ld, _stream(stream))
+    _raise(s, name)
+
+
+def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
+    """out_y[T, rows] = x w^T from the (codes, scales) pairs of an activation (`format`) and of a weight."""
+    _fp8_linear("roi_fp8_linear_fwd", False, x8, format, w8, out_y, stream)
+
+
+def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
+    """out_dx[T, cols] = dy w, from the (codes, scales) pairs of dy [T, rows] (`format`) and of the weight [rows, cols]."""
+    _fp8_linear("roi_fp8_linear_dgrad", True, dy8, format, w8, out_dx, stream)
 
 
 def roi_noise_words(state: NoiseState, rows, cols, out_words, stream=None):

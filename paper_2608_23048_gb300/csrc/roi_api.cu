@@ -910,6 +910,99 @@ roi_status roi_masked_linear_wgrad(const roi_bf16* dY, int64_t lddy, const int8_
   return finish(launch_wgrad(c));
 }
 
+int64_t roi_fp8_pitch(int64_t cols) { return cols <= 0 || cols > INT64_MAX / 1024 ? 0 : fp8_pitch(cols); }
+int64_t roi_fp8_scale_pitch(int64_t cols) { return cols <= 0 || cols > INT64_MAX / 1024 ? 0 : fp8_scale_pitch(cols); }
+
+static bool known_format(int format) { return format == ROI_E4M3 || format == ROI_E5M2; }
+// Tensor-map coordinates and tile numbers are 32-bit.
+static constexpr int64_t kFp8Most = int64_t(1) << 30;
+
+static roi_status fp8_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ld, int format, bool weight,
+                           uint8_t* codes, uint8_t* scales, void* stream) {
+  if (!known_type(dtype) || !known_format(format)) return ROI_ERR_TYPE;
+  if (!good_shape(rows, cols, ld) || rows > kFp8Most || cols > kFp8Most) return ROI_ERR_SHAPE;
+  if (rows == 0) return ROI_OK;
+  if (x == nullptr || codes == nullptr || scales == nullptr) return ROI_ERR_NULL;
+  const int b = type_bytes(dtype);
+  if (!aligned_to(x, weight ? 16 : b) || !aligned16(codes) || !aligned16(scales)) return ROI_ERR_ALIGN;
+  const Strided m[1] = {matrix(x, rows, cols, ld, b)};
+  const Strided out[2] = {flat(codes, uint64_t(rows) * uint64_t(fp8_pitch(cols))),
+                          flat(scales, uint64_t(weight ? (rows + 127) / 128 : rows) * uint64_t(fp8_scale_pitch(cols)))};
+  if (any_alias(m, out)) return ROI_ERR_ALIAS;
+  Fp8SaveCall c;
+  c.x = x;
+  c.codes = codes;
+  c.scales = scales;
+  c.dtype = static_cast<Elem>(dtype);
+  c.format = static_cast<Fp8>(format);
+  c.rows = rows;
+  c.cols = cols;
+  c.ld = ld;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(weight ? launch_fp8_save_weight(c) : launch_fp8_save(c));
+}
+
+roi_status roi_fp8_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int format, uint8_t* out_codes,
+                        uint8_t* out_scales, void* stream) {
+  return fp8_save(x, dtype, rows, cols, ldx, format, false, out_codes, out_scales, stream);
+}
+
+roi_status roi_fp8_save_weight(const roi_bf16* W, int64_t rows, int64_t cols, uint8_t* out_codes, uint8_t* out_scales, void* stream) {
+  return fp8_save(W, ROI_BF16, rows, cols, cols, ROI_E4M3, true, out_codes, out_scales, stream);
+}
+
+static roi_status fp8_linear(bool dgrad, const uint8_t* x_codes, const uint8_t* x_scales, int format, const uint8_t* w_codes,
+                             const uint8_t* w_scales, int64_t T, int64_t rows, int64_t cols, void* out, int dtype, int64_t ldo,
+                             void* stream) {
+  if (!known_type(dtype) || !known_format(format)) return ROI_ERR_TYPE;
+  const int64_t outs = dgrad ? cols : rows, width = dgrad ? rows : cols;
+  if (T < 0 || rows < 0 || cols <= 0 || T > kFp8Most || rows > kFp8Most || cols > kFp8Most) return ROI_ERR_SHAPE;
+  if (T == 0 || outs == 0) return ROI_OK;
+  if (!good_shape(T, outs, ldo) || ((outs + 127) / 128) * ((T + 255) / 256) > kFp8Most) return ROI_ERR_SHAPE;
+  const int b = type_bytes(dtype);
+  if (out == nullptr || (width > 0 && (x_codes == nullptr || x_scales == nullptr || w_codes == nullptr || w_scales == nullptr)))
+    return ROI_ERR_NULL;
+  if (!aligned_to(out, b) || !aligned16(x_codes) || !aligned16(x_scales) || !aligned16(w_codes) || !aligned16(w_scales))
+    return ROI_ERR_ALIGN;
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (width == 0)  // empty sums
+    return cudaMemset2DAsync(out, size_t(ldo) * b, 0, size_t(outs) * b, size_t(T), st) == cudaSuccess ? ROI_OK : ROI_ERR_CUDA;
+  const Strided in[4] = {flat(x_codes, uint64_t(T) * uint64_t(fp8_pitch(width))), flat(x_scales, uint64_t(T) * uint64_t(fp8_scale_pitch(width))),
+                         flat(w_codes, uint64_t(rows) * uint64_t(fp8_pitch(cols))),
+                         flat(w_scales, uint64_t((rows + 127) / 128) * uint64_t(fp8_scale_pitch(cols)))};
+  const Strided o[1] = {matrix(out, T, outs, ldo, b)};
+  if (any_alias(in, o)) return ROI_ERR_ALIAS;
+  Fp8LinearCall c;
+  c.x_codes = x_codes;
+  c.x_scales = x_scales;
+  c.w_codes = w_codes;
+  c.w_scales = w_scales;
+  c.out = out;
+  c.format = static_cast<Fp8>(format);
+  c.dtype = static_cast<Elem>(dtype);
+  c.dgrad = dgrad;
+  c.T = T;
+  c.rows = rows;
+  c.cols = cols;
+  c.ldo = ldo;
+  c.status = status_word();
+  if (c.status == nullptr) return ROI_ERR_CUDA;
+  c.stream = st;
+  return finish(launch_fp8_linear(c));
+}
+
+roi_status roi_fp8_linear_fwd(const uint8_t* x_codes, const uint8_t* x_scales, int format, const uint8_t* w_codes,
+                              const uint8_t* w_scales, int64_t T, int64_t rows, int64_t cols, void* out_y, int dtype, int64_t ldy,
+                              void* stream) {
+  return fp8_linear(false, x_codes, x_scales, format, w_codes, w_scales, T, rows, cols, out_y, dtype, ldy, stream);
+}
+
+roi_status roi_fp8_linear_dgrad(const uint8_t* dy_codes, const uint8_t* dy_scales, int format, const uint8_t* w_codes,
+                                const uint8_t* w_scales, int64_t T, int64_t rows, int64_t cols, void* out_dx, int dtype, int64_t lddx,
+                                void* stream) {
+  return fp8_linear(true, dy_codes, dy_scales, format, w_codes, w_scales, T, rows, cols, out_dx, dtype, lddx, stream);
+}
+
 static roi_status noise_call(const roi_noise_state* st, int64_t rows, int64_t cols, uint32_t* words, float* g,
                              void* stream) {
   if (st == nullptr) return ROI_ERR_NULL;

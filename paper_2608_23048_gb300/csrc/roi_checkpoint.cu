@@ -43,23 +43,6 @@ struct LoadArgs {
   bool wait;
 };
 
-// Row and place in the row of the `i`-th item of a row-major walk over rows of `per_row`
-// items, from the row and the place of the walk's start (one division of 64 bits a tile).
-__device__ __forceinline__ void walk(int64_t row0, int64_t rem0, uint32_t i, int64_t per_row, int64_t& row, int64_t& j) {
-  j = rem0 + i;
-  row = row0;
-  if (j >= per_row) {
-    if (per_row <= 0x3fffffff) {
-      const uint32_t q = uint32_t(j) / uint32_t(per_row);
-      row += q;
-      j -= int64_t(q) * per_row;
-    } else {
-      ++row;
-      j -= per_row;
-    }
-  }
-}
-
 // Codes and scale of a piece (all lanes of the warp); `q` is its place in the row.
 template <Elem E>
 __device__ __forceinline__ void save_piece(const SaveArgs& a, const RowWords<E, 16>& r, int64_t row, int64_t q) {
@@ -161,18 +144,6 @@ __global__ void __launch_bounds__(kThreads) roi_checkpoint_load_kernel(LoadArgs 
   }
 }
 
-// Rows anywhere.  A warp's task: 32 / width rows, or one segment of a row.
-__device__ __forceinline__ void row_task(int64_t task, int width, int segments, int64_t& row, int64_t& piece) {
-  const int lane = threadIdx.x & 31;
-  if (segments > 1) {
-    row = task / segments;
-    piece = (task - row * segments) * 32 + lane;
-  } else {
-    row = task * (32 / width) + lane / width;
-    piece = lane & (width - 1);
-  }
-}
-
 template <Elem E>
 __global__ void __launch_bounds__(kThreads) roi_checkpoint_save_rows_kernel(SaveArgs a) {
   using T = typename ElemType<E>::T;
@@ -231,21 +202,6 @@ int launch(void (*kern)(Args), const Args& a, int64_t total, int tile, cudaStrea
   const int64_t cap = int64_t(sm_count()) * 8;  // what an SM holds at once
   if (grid > cap) grid = cap;
   return launch_maybe_pdl(kern, int(grid), kThreads, 0, stream, a.wait, a);
-}
-
-// Rows that are whole 32-byte sectors apart.
-bool in_sectors(const void* p, int64_t ld, int64_t rows, int bytes) {
-  return (reinterpret_cast<uintptr_t>(p) & 31u) == 0 && (rows <= 1 || ld * bytes % 32 == 0);
-}
-// Rows anywhere: the lanes of a row, a power of two that holds its pieces, or a whole warp that
-// goes over it in segments.  Returns the tiles of the launch.
-template <class Args>
-int64_t by_rows(Args& a) {
-  a.width = 8;
-  while (a.width < 32 && a.width < a.pieces) a.width *= 2;
-  a.segments = int((a.pieces + 31) / 32);
-  const int64_t per = 32 / a.width;
-  return (a.rows + per - 1) / per * a.segments;
 }
 
 template <Elem E>

@@ -1,0 +1,193 @@
+// Copies in 8-bit floating point (the layout is in roi_fp8.cuh) of activations and of weights.
+//
+// Bound by memory: b bytes an element are read and 129/128 written.  A thread takes 16 consecutive columns (one 16-byte
+// store of codes), so eight neighbouring lanes hold a block of a row and its largest magnitude takes three shuffles.  A
+// weight's block of 128 x 128 is a CTA's, four such pieces a thread, and its largest magnitude goes through shared memory.
+#include "roi_fp8.cuh"
+#include "roi_launch.h"
+
+namespace roi {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kUnits = 2;  // pieces of 16 columns a thread has in flight
+
+struct SaveArgs {
+  const void* x;
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t rows, cols, ld;
+  int64_t pitch, spitch;
+  int64_t pieces;       // of 16 columns in a row, whole blocks of them
+  int width, segments;  // rows anywhere: lanes of a row, and how often they go over it
+  bool wait;
+};
+
+// Codes and scale of a piece, the q-th of its row (all lanes of the warp; eight of them hold a block).
+template <Fp8 F, Elem E>
+__device__ __forceinline__ void save_piece(const SaveArgs& a, const RowWords<E, 16>& r, int64_t row, int64_t q) {
+  uint32_t top = max_bits(r);
+#pragma unroll
+  for (int m = 1; m < 8; m *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+  const uint32_t s = fp8_scale<F>(top);
+  const uint4 w = fp8_codes16<F>(r, s);
+  if (row < a.rows && q < a.pieces) {
+    *reinterpret_cast<uint4*>(a.codes + row * a.pitch + 16 * q) = w;
+    if ((q & 7) == 0) {
+      uint8_t* to = a.scales + row * a.spitch;
+      to[q >> 3] = uint8_t(s);
+      if (q + 8 == a.pieces)
+        for (int64_t b = a.pieces >> 3; b < a.spitch; ++b) to[b] = 1;
+    }
+  }
+}
+
+template <Fp8 F, Elem E>
+__global__ void __launch_bounds__(kThreads) roi_fp8_save_kernel(SaveArgs a) {
+  using T = typename ElemType<E>::T;
+  constexpr int kWords = RowWords<E, 16>::kWords;
+  pdl_begin(a.wait);
+  const T* x = static_cast<const T*>(a.x);
+  const int64_t total = a.rows * a.pieces;
+  constexpr int kTile = kThreads * kUnits;
+  for (int64_t base = int64_t(blockIdx.x) * kTile; base < total; base += int64_t(gridDim.x) * kTile) {
+    const int64_t row0 = base / a.pieces, rem0 = base - row0 * a.pieces;
+    RowWords<E, 16> r[kUnits];
+    int64_t row[kUnits], j[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      walk(row0, rem0, uint32_t(u * kThreads) + threadIdx.x, a.pieces, row[u], j[u]);
+      const T* p = x + row[u] * a.ld + 16 * j[u];
+      if (row[u] < a.rows && a.cols - 16 * j[u] >= 16) {
+#pragma unroll
+        for (int i = 0; i < kWords / 8; ++i) load32(reinterpret_cast<const uint4*>(p) + 2 * i, r[u].u + 8 * i);
+      } else if (row[u] < a.rows) {
+        r[u].load_elements(x + row[u] * a.ld, 16 * j[u], a.cols);
+      } else {
+        r[u].zero();
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) save_piece<F, E>(a, r[u], row[u], j[u]);
+  }
+}
+
+template <Fp8 F, Elem E>
+__global__ void __launch_bounds__(kThreads) roi_fp8_save_rows_kernel(SaveArgs a) {
+  using T = typename ElemType<E>::T;
+  pdl_begin(a.wait);
+  const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
+  const int64_t stride = int64_t(gridDim.x) * (kThreads / 32) * kUnits;
+  for (int64_t t = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits; t < tasks; t += stride) {
+    Window<E, 16> x[kUnits];
+    int64_t row[kUnits], j[kUnits];
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      row_task(t + u, a.width, a.segments, row[u], j[u]);
+      x[u].load(static_cast<const T*>(a.x) + row[u] * a.ld, 16 * j[u], row[u] < a.rows ? a.cols : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      RowWords<E, 16> r;
+      x[u].get(r);
+      save_piece<F, E>(a, r, row[u], j[u]);
+    }
+  }
+}
+
+struct WeightArgs {
+  const uint16_t* W;
+  uint8_t* codes;
+  uint8_t* scales;
+  int64_t rows, cols, pitch, spitch;
+  int64_t blocks_n, blocks;
+  bool wait;
+};
+
+// ANYWHERE: rows that are not whole sectors apart.
+template <bool ANYWHERE>
+__global__ void __launch_bounds__(kThreads) roi_fp8_save_weight_kernel(WeightArgs a) {
+  constexpr int kPieces = 4;
+  __shared__ uint32_t tops[2][kThreads / 32];
+  pdl_begin(a.wait);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int turn = 0;
+  for (int64_t b = blockIdx.x; b < a.blocks; b += gridDim.x, turn ^= 1) {
+    const int64_t bm = b / a.blocks_n, bn = b - bm * a.blocks_n;
+    const int64_t r0 = bm * 128 + (threadIdx.x >> 3), c = bn * 128 + 16 * (threadIdx.x & 7);
+    RowWords<Elem::kBf16, 16> r[kPieces];
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int64_t row = r0 + 32 * i;
+      if constexpr (ANYWHERE) {
+        Window<Elem::kBf16, 16> w;
+        w.load(a.W + row * a.cols, c, row < a.rows ? a.cols : 0);
+        w.get(r[i]);
+      } else if (row < a.rows && c + 16 <= a.cols) {
+        load32(a.W + row * a.cols + c, r[i].u);
+      } else {
+        r[i].zero();  // (columns come in sixteens)
+      }
+    }
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) top = max(top, max_bits(r[i]));
+    top = __reduce_max_sync(0xffffffffu, top);
+    if (lane == 0) tops[turn][warp] = top;
+    __syncthreads();  // (the next block's tops lie apart)
+    top = __reduce_max_sync(0xffffffffu, tops[turn][lane & (kThreads / 32 - 1)]);
+    const uint32_t s = fp8_scale<Fp8::kE4M3>(top);
+#pragma unroll
+    for (int i = 0; i < kPieces; ++i) {
+      const int64_t row = r0 + 32 * i;
+      if (row < a.rows) *reinterpret_cast<uint4*>(a.codes + row * a.pitch + c) = fp8_codes16<Fp8::kE4M3>(r[i], s);
+    }
+    if (threadIdx.x == 0) {
+      uint8_t* to = a.scales + bm * a.spitch;
+      to[bn] = uint8_t(s);
+      if (bn == a.blocks_n - 1)
+        for (int64_t k = a.blocks_n; k < a.spitch; ++k) to[k] = 1;
+    }
+  }
+}
+
+template <class Args>
+int launch(void (*kern)(Args), const Args& a, int64_t grid, cudaStream_t stream) {
+  const int64_t cap = int64_t(sm_count()) * 8;  // what an SM holds at once
+  return launch_maybe_pdl(kern, int(grid < cap ? grid : cap), kThreads, 0, stream, a.wait, a);
+}
+
+template <Fp8 F, Elem E>
+int save(const Fp8SaveCall& c) {
+  SaveArgs a{c.x,  c.codes, c.scales, c.rows, c.cols, c.ld, fp8_pitch(c.cols), fp8_scale_pitch(c.cols), fp8_pitch(c.cols) / 16, 0, 0,
+             lone_pdl(c.stream)};
+  if (!in_sectors(c.x, c.ld, c.rows, elem_bytes<E>())) {
+    const int64_t tasks = by_rows(a);
+    return launch(roi_fp8_save_rows_kernel<F, E>, a, (tasks + kThreads / 32 * kUnits - 1) / (kThreads / 32 * kUnits), c.stream);
+  }
+  const int64_t total = a.rows * a.pieces;
+  return launch(roi_fp8_save_kernel<F, E>, a, (total + kThreads * kUnits - 1) / (kThreads * kUnits), c.stream);
+}
+
+template <Fp8 F>
+int save_of(const Fp8SaveCall& c) {
+  switch (c.dtype) {
+    case Elem::kBf16: return save<F, Elem::kBf16>(c);
+    case Elem::kFp16: return save<F, Elem::kFp16>(c);
+    default: return save<F, Elem::kFp32>(c);
+  }
+}
+
+}  // namespace
+
+int launch_fp8_save(const Fp8SaveCall& c) { return c.format == Fp8::kE4M3 ? save_of<Fp8::kE4M3>(c) : save_of<Fp8::kE5M2>(c); }
+
+int launch_fp8_save_weight(const Fp8SaveCall& c) {
+  WeightArgs a{static_cast<const uint16_t*>(c.x), c.codes, c.scales, c.rows, c.cols, fp8_pitch(c.cols), fp8_scale_pitch(c.cols),
+               (c.cols + 127) / 128, 0, lone_pdl(c.stream)};
+  a.blocks = a.blocks_n * ((c.rows + 127) / 128);
+  if (in_sectors(c.x, c.cols, 2, 2)) return launch(roi_fp8_save_weight_kernel<false>, a, a.blocks, c.stream);
+  return launch(roi_fp8_save_weight_kernel<true>, a, a.blocks, c.stream);
+}
+
+}  // namespace roi

@@ -7,6 +7,7 @@
 
 #include "roi_block8.cuh"
 #include "roi_common.cuh"
+#include "roi_fp8.cuh"
 
 namespace roi {
 
@@ -186,6 +187,32 @@ struct WgradCall {
   cudaStream_t stream;
 };
 
+// A copy in 8-bit floating point: of an activation (x of type dtype, rows ld apart) or of a weight (bf16, rows whole).
+struct Fp8SaveCall {
+  const void* x;
+  uint8_t* codes;
+  uint8_t* scales;
+  Elem dtype;
+  Fp8 format;
+  int64_t rows, cols, ld;
+  cudaStream_t stream;
+};
+
+// out[T, rows] = x^ w^^T, x^ [T, cols]; or, dgrad, out[T, cols] = x^ w^, x^ [T, rows].
+struct Fp8LinearCall {
+  const uint8_t* x_codes;
+  const uint8_t* x_scales;
+  const uint8_t* w_codes;  // [rows, cols]
+  const uint8_t* w_scales;
+  void* out;
+  Fp8 format;              // of x
+  Elem dtype;              // of out
+  bool dgrad;
+  int64_t T, rows, cols, ldo;
+  unsigned int* status;
+  cudaStream_t stream;
+};
+
 // Each returns the number of kernels launched (>= 0) or -1 after a CUDA error.
 int launch_checkpoint_save(const CheckpointCall& c);
 int launch_checkpoint_load(const CheckpointCall& c);
@@ -197,6 +224,9 @@ size_t norm_bwd_workspace_bytes(int64_t rows, int64_t cols);
 size_t wgrad_workspace_bytes(int64_t T, int64_t rows, int64_t cols, int64_t lddy);
 size_t wgrad_copy_bytes(int64_t T, int64_t rows, int64_t lddy);
 int launch_wgrad(const WgradCall& c);
+int launch_fp8_save(const Fp8SaveCall& c);
+int launch_fp8_save_weight(const Fp8SaveCall& c);
+int launch_fp8_linear(const Fp8LinearCall& c);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);
 // Many independent tensors on one stream: one launch per tensor, or per run of

@@ -224,4 +224,45 @@ __device__ __forceinline__ bool mbar_wait_ring_cluster(uint64_t* bar, uint32_t p
   }
 }
 
+// ---------------------------------------------------------------------------
+// block-scaled products of 8-bit floating point (kind::mxf8f6f4)
+// ---------------------------------------------------------------------------
+// K-major operand with 128-byte swizzle: rows of 128 bytes along K, atoms of 8 rows (1024 bytes) one after
+// another, as a TMA box of 128 bytes leaves them.  1024-byte aligned; 32 bytes on for the next 32 of K.
+__device__ __forceinline__ uint64_t tc_smem_desc_k128(uint32_t saddr) {
+  uint64_t d = uint64_t((saddr >> 4) & 0x3FFFu);
+  d |= uint64_t(1) << 16;
+  d |= uint64_t(1024 >> 4) << 32;
+  d |= uint64_t(1) << 46;
+  d |= uint64_t(2) << 61;  // 128-byte swizzle
+  return d;
+}
+// Instruction descriptor: A and B formats at bits 7-9 and 10-12 (0 e4m3, 1 e5m2), MN-major A and B at
+// bits 15 and 16, N >> 3 at 17-22, scales in powers of two at 23, M >> 4 at 24-28.  Which byte of the words of
+// scales goes with a step is at bits 4-5 (B) and 29-30 (A).
+__host__ __device__ constexpr uint32_t tc_idesc_mxf8(int m, int n, int a_format, int b_format, bool a_mn, bool b_mn) {
+  return (uint32_t(a_format) << 7) | (uint32_t(b_format) << 10) | (uint32_t(a_mn) << 15) | (uint32_t(b_mn) << 16) |
+         (uint32_t(n >> 3) << 17) | (1u << 23) | (uint32_t(m >> 4) << 24);
+}
+__device__ __forceinline__ uint32_t tc_idesc_scale_byte(uint32_t idesc, uint32_t byte) {
+  return idesc | (byte << 4) | (byte << 29);
+}
+// D[tmem] (+)= (A 2^(sa - 127)) * (B 2^(sb - 127))^T for one M x N x 32 step: a scale a row of A and of B.
+// Scales lie in TMEM in words of four steps: row r's in lane r % 32 (the same in all four quarters of the lanes)
+// of column r / 32.
+__device__ __forceinline__ void tc_mma_mxf8(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
+                                            uint32_t sb_tmem, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(uint32_t(accumulate))
+      : "memory");
+}
+// 32 rows of 16 bytes (512 bytes one after another) from shared memory to four columns of TMEM, the same in
+// all four quarters of the lanes.  In order with the MMAs of the thread that issues it.
+__device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint32_t saddr) {
+  const uint64_t desc = tc_smem_desc(saddr, 128, 128);
+  asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 }  // namespace roi
