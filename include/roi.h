@@ -194,7 +194,7 @@ typedef struct {
  *  out_dlogits  nullable: the gradient g as well
  *  out_dW       nullable: bf16_rne(float(dWm) * S), as roi_mask_bwd
  * The step needs the gradient of this mask op alone (one use of phi per step;
- * a data-parallel run reduces gradients first and uses roi_mask_bwd instead).
+ * a data-parallel run reduces roi_mask_bwd's gradients first and then takes roi_adamw_step).
  * ROI_ERR_OPT for settings outside the ranges above. */
 roi_status roi_mask_bwd_adamw(float* logits, const roi_bf16* W, const roi_noise_state* st, int N, int M,
                               const roi_bf16* dWm, float tau, int64_t rows, int64_t cols,
@@ -219,6 +219,72 @@ typedef struct {
 } roi_adamw_item;
 roi_status roi_mask_bwd_adamw_batch(const roi_adamw_item* items, int count, int N, int M, float tau,
                                     const roi_adamw* opt, void* stream);
+
+/* The same step on gradients that are there already, for many tensors of any size in one call: the logits after a
+ * data-parallel reduction of roi_mask_bwd's gradients, and norm weights.
+ *  param      [n] float32, read and written
+ *  grad       [n] of type grad_dtype (roi_dtype)
+ *  m, v       [n] float32, read and written; zeros before the first step
+ *  out_copy   nullable: the new parameters, rounded to copy_dtype (ROI_BF16 or ROI_FP16)
+ *  n          0: the item is skipped, its pointers may be NULL
+ *  grad_scale nullable: one float32 on the device (4-byte aligned), by which every gradient is multiplied
+ *             first (a clipping factor, the reduction's 1 / ranks)
+ * Per element, with g = grad * grad_scale, the same operations as roi_mask_bwd_adamw: the same bits.  No output
+ * may overlap any other range of any item (ROI_ERR_ALIAS).  `items` is host memory, read during the call.
+ * ROI_ERR_TYPE for unknown types, ROI_ERR_OPT as above.  */
+typedef struct {
+    float* param;
+    const void* grad;
+    float* m;
+    float* v;
+    void* out_copy;
+    int64_t n;
+    int grad_dtype;
+    int copy_dtype;
+} roi_adamw_step_item;
+roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi_adamw* opt, const float* grad_scale,
+                          void* stream);
+
+/* roi_adamw_step with the moments in 8 bits: 2 bytes an element and 2 for every 128.  Blocks of 128
+ * consecutive elements hold m in e4m3 (largest code 448) and u = sqrt(v) without a sign, four bits of exponent and four of
+ * mantissa with the same bias 7 (largest code 480, 0xff a NaN), each with a power of two of their own, 2^(s - 127),
+ * s - 127 >= -126 the least exponent that keeps the block's largest finite magnitude within the largest code.
+ *  m_codes, u_codes  [n rounded up to 128] uint8, 16-byte aligned, read and written; padding is written as 0
+ *  scales            [blocks][2] uint8, m's and u's; 2-byte aligned
+ * All of them zero before the first step.  A step forms m and v = u * u in float32, updates them and the parameters
+ * as roi_adamw_step does, from the unrounded moments, and rounds m and sqrt(v) up with the probability of what their
+ * codes would drop (to the nearest, u could not follow a beta2 of 0.95 down): code = floor(|x| / step + r / 65536), r the low
+ * (m) or high (u) half of the element's Philox word for (seed, opt->t, tensor_id), counters as for the mask's noise.
+ * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.
+ * Results are a pure function of the arguments: they do not depend on how elements are divided among calls' items,
+ * except that blocks start with each item. */
+typedef struct {
+    float* param;
+    const void* grad;
+    uint8_t* m_codes;
+    uint8_t* u_codes;
+    uint8_t* scales;
+    void* out_copy;
+    int64_t n;
+    int grad_dtype;
+    int copy_dtype;
+    uint32_t tensor_id;
+} roi_adamw_step8_item;
+roi_status roi_adamw_step8(const roi_adamw_step8_item* items, int count, const roi_adamw* opt, uint64_t seed,
+                           const float* grad_scale, void* stream);
+
+/* The m and u that states in 8 bits stand for, in dtype (at least one of the two; bf16 holds both exactly where
+ * s >= 4, fp16 ends before their range does). */
+typedef struct {
+    const uint8_t* m_codes;
+    const uint8_t* u_codes;
+    const uint8_t* scales;
+    void* out_m;
+    void* out_u;
+    int64_t n;
+    int dtype;
+} roi_adamw_state8_item;
+roi_status roi_adamw_state8_load(const roi_adamw_state8_item* items, int count, void* stream);
 
 /* Exponential annealing of tau and lambda (Sec. 4.2.3, Eq. 13), on the host:
  *     x_t = max(x_end, x_init (x_end / x_init)^(t / T_anneal))

@@ -23,6 +23,8 @@ __all__ = [
     "roi_masked_linear_wgrad", "roi_masked_linear_wgrad_workspace_size",
     "roi_fp8_pitch", "roi_fp8_scale_pitch", "new_fp8", "new_fp8_weight", "roi_fp8_save", "roi_fp8_save_weight",
     "roi_fp8_linear_fwd", "roi_fp8_linear_dgrad",
+    "make_adamw_step_items", "make_adamw_step8_items", "make_adamw_state8_items", "new_adamw_state8",
+    "roi_adamw_step", "roi_adamw_step8", "roi_adamw_state8_load",
 ]
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -79,6 +81,27 @@ class BwdStItem(ctypes.Structure):
     _fields_ = [("logits", ctypes.c_void_p), ("W", ctypes.c_void_p), ("dWm", ctypes.c_void_p),
                 ("hard", ctypes.c_void_p), ("out_dlogits", ctypes.c_void_p), ("out_dW", ctypes.c_void_p),
                 ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("st", NoiseState)]
+
+
+class AdamWStepItem(ctypes.Structure):
+    """roi_adamw_step_item: one tensor of roi_adamw_step."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("out_copy", ctypes.c_void_p), ("n", ctypes.c_int64), ("grad_dtype", ctypes.c_int),
+                ("copy_dtype", ctypes.c_int)]
+
+
+class AdamWStep8Item(ctypes.Structure):
+    """roi_adamw_step8_item: one tensor of roi_adamw_step8."""
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m_codes", ctypes.c_void_p),
+                ("u_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("out_copy", ctypes.c_void_p),
+                ("n", ctypes.c_int64), ("grad_dtype", ctypes.c_int), ("copy_dtype", ctypes.c_int),
+                ("tensor_id", ctypes.c_uint32)]
+
+
+class AdamWState8Item(ctypes.Structure):
+    """roi_adamw_state8_item: one tensor of roi_adamw_state8_load."""
+    _fields_ = [("m_codes", ctypes.c_void_p), ("u_codes", ctypes.c_void_p), ("scales", ctypes.c_void_p),
+                ("out_m", ctypes.c_void_p), ("out_u", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int)]
 
 
 _LIB = None
@@ -139,6 +162,9 @@ def lib() -> ctypes.CDLL:
     L.roi_fp8_save_weight.argtypes = [_P, i64, i64, _P, _P, _P]
     for name in ("roi_fp8_linear_fwd", "roi_fp8_linear_dgrad"):
         getattr(L, name).argtypes = [_P, _P, i32, _P, _P, i64, i64, i64, _P, i32, i64, _P]
+    L.roi_adamw_step.argtypes = [ctypes.POINTER(AdamWStepItem), i32, ctypes.POINTER(AdamW), _P, _P]
+    L.roi_adamw_step8.argtypes = [ctypes.POINTER(AdamWStep8Item), i32, ctypes.POINTER(AdamW), u64, _P, _P]
+    L.roi_adamw_state8_load.argtypes = [ctypes.POINTER(AdamWState8Item), i32, _P]
     L.roi_device_status.argtypes = [_P]
     L.roi_set_ring_wait_limit_ns.argtypes = [u64]
     L.roi_noise_words.argtypes = [ctypes.POINTER(NoiseState), i64, i64, _P, _P]
@@ -154,7 +180,7 @@ def lib() -> ctypes.CDLL:
                  "roi_mask_bwd_adamw_batch", "roi_mask_fwd_st_batch", "roi_mask_bwd_st_batch",
                  "roi_set_ring_wait_limit_ns", "roi_checkpoint_save", "roi_checkpoint_load", "roi_norm_fwd",
                  "roi_norm_bwd", "roi_masked_linear_wgrad", "roi_fp8_save", "roi_fp8_save_weight", "roi_fp8_linear_fwd",
-                 "roi_fp8_linear_dgrad"):
+                 "roi_fp8_linear_dgrad", "roi_adamw_step", "roi_adamw_step8", "roi_adamw_state8_load"):
         getattr(L, name).restype = i32
     _LIB = L
     return L
@@ -776,6 +802,136 @@ def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
 def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
     """out_dx[T, cols] = dy w, from the (codes, scales) pairs of dy [T, rows] (`format`) and of the weight [rows, cols]."""
     _fp8_linear("roi_fp8_linear_dgrad", True, dy8, format, w8, out_dx, stream)
+
+
+# ---------------------------------------------------------------------------
+# the AdamW step over many tensors
+# ---------------------------------------------------------------------------
+def _half(t, name, shape):
+    """Type code of a copy in 16 bits (None: none)."""
+    if t is None:
+        return 0
+    code = _type(t, name)
+    if code == 2:
+        raise TypeError(f"{name}: expected bfloat16 or float16, got {t.dtype}")
+    _check_tensor(t, name, t.dtype, shape)
+    return code
+
+
+def _same_size(t, name, dtype, n):
+    _check_tensor(t, name, dtype)
+    if t.numel() != n:
+        raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
+
+
+def _device(tensors, name):
+    """One device for all of an item's tensors."""
+    first = None
+    for t in tensors:
+        if t is not None:
+            first = t.device if first is None else first
+            if t.device != first:
+                raise ValueError(f"{name}: tensors on {first} and on {t.device}")
+
+
+def make_adamw_step_items(items):
+    """ctypes array of AdamWStepItem from (param, grad, m, v, copy) tuples: tensors of any shape, copy (bfloat16 or
+    float16) or None."""
+    import torch
+    arr = (AdamWStepItem * len(items))()
+    for k, (param, grad, m, v, copy) in enumerate(items):
+        shape = param.shape
+        _check_tensor(param, "param", torch.float32)
+        code = _type(grad, "grad")
+        _check_tensor(grad, "grad", grad.dtype, shape)
+        _check_tensor(m, "m", torch.float32, shape)
+        _check_tensor(v, "v", torch.float32, shape)
+        half = _half(copy, "copy", shape)
+        _device((param, grad, m, v, copy), f"item {k}")
+        arr[k] = AdamWStepItem(_addr(param), _addr(grad), _addr(m), _addr(v), _addr(copy), param.numel(), code, half)
+    return arr
+
+
+def new_adamw_state8(n, device="cuda"):
+    """State in 8 bits before the first step of a tensor of n elements: (codes of m, codes of sqrt(v), scales)."""
+    import torch
+    blocks = (int(n) + 127) // 128
+    return tuple(torch.zeros(s, dtype=torch.uint8, device=device) for s in ((blocks * 128,), (blocks * 128,), (blocks, 2)))
+
+
+def _state8(state, n):
+    import torch
+    m, u, s = state
+    blocks = (n + 127) // 128
+    _check_tensor(m, "state's m", torch.uint8, (blocks * 128,))
+    _check_tensor(u, "state's u", torch.uint8, (blocks * 128,))
+    _check_tensor(s, "state's scales", torch.uint8, (blocks, 2))
+    return m.data_ptr(), u.data_ptr(), s.data_ptr()
+
+
+def make_adamw_step8_items(items):
+    """ctypes array of AdamWStep8Item from (param, grad, state, copy, tensor_id) tuples, state as from new_adamw_state8."""
+    import torch
+    arr = (AdamWStep8Item * len(items))()
+    for k, (param, grad, state, copy, tensor_id) in enumerate(items):
+        shape = param.shape
+        _check_tensor(param, "param", torch.float32)
+        code = _type(grad, "grad")
+        _check_tensor(grad, "grad", grad.dtype, shape)
+        half = _half(copy, "copy", shape)
+        n = param.numel()
+        at = _state8(state, n)
+        _device((param, grad, *state, copy), f"item {k}")
+        arr[k] = AdamWStep8Item(_addr(param), _addr(grad), *at, _addr(copy), n, code, half, int(tensor_id))
+    return arr
+
+
+def make_adamw_state8_items(items):
+    """ctypes array of AdamWState8Item from (state, out_m, out_u) tuples: tensors of one type, one of them or None."""
+    arr = (AdamWState8Item * len(items))()
+    for k, (state, out_m, out_u) in enumerate(items):
+        like = out_m if out_m is not None else out_u
+        if like is None:
+            raise ValueError("out_m or out_u: a tensor is required")
+        code, n = _type(like, "out_m"), like.numel()
+        for t, name in ((out_m, "out_m"), (out_u, "out_u")):
+            if t is not None:
+                _same_size(t, name, like.dtype, n)
+        at = _state8(state, n)
+        _device((*state, out_m, out_u), f"item {k}")
+        arr[k] = AdamWState8Item(*at, _addr(out_m), _addr(out_u), n, code)
+    return arr
+
+
+def _grad_scale(t):
+    import torch
+    if t is None:
+        return None
+    _same_size(t, "grad_scale", torch.float32, 1)
+    return t.data_ptr()
+
+
+def roi_adamw_step(items, opt: AdamW, grad_scale=None, stream=None):
+    """One AdamW step of many tensors in place (an AdamWStepItem array from make_adamw_step_items, reusable while its
+    tensors live, or a list of (param, grad, m, v, copy) tuples).  grad_scale: float32 [1] on the device, or None."""
+    arr = items if isinstance(items, ctypes.Array) else make_adamw_step_items(items)
+    s = lib().roi_adamw_step(arr, len(arr), ctypes.byref(opt), _grad_scale(grad_scale), _stream(stream))
+    _raise(s, "roi_adamw_step")
+
+
+def roi_adamw_step8(items, opt: AdamW, seed, grad_scale=None, stream=None):
+    """roi_adamw_step with states in 8 bits, rounded by the noise of (seed, opt.t, tensor_id) (an AdamWStep8Item array
+    from make_adamw_step8_items, or a list of (param, grad, state, copy, tensor_id) tuples)."""
+    arr = items if isinstance(items, ctypes.Array) else make_adamw_step8_items(items)
+    s = lib().roi_adamw_step8(arr, len(arr), ctypes.byref(opt), int(seed), _grad_scale(grad_scale), _stream(stream))
+    _raise(s, "roi_adamw_step8")
+
+
+def roi_adamw_state8_load(items, stream=None):
+    """m and sqrt(v) of states in 8 bits (an AdamWState8Item array from make_adamw_state8_items, or a list of
+    (state, out_m, out_u) tuples)."""
+    arr = items if isinstance(items, ctypes.Array) else make_adamw_state8_items(items)
+    _raise(lib().roi_adamw_state8_load(arr, len(arr), _stream(stream)), "roi_adamw_state8_load")
 
 
 def roi_noise_words(state: NoiseState, rows, cols, out_words, stream=None):

@@ -1003,6 +1003,117 @@ roi_status roi_fp8_linear_dgrad(const uint8_t* dy_codes, const uint8_t* dy_scale
   return fp8_linear(true, dy_codes, dy_scales, format, w_codes, w_scales, T, rows, cols, out_dx, dtype, lddx, stream);
 }
 
+// Elements of a tensor whose byte counts fit.
+static bool good_count(int64_t n) { return n >= 0 && n <= INT64_MAX / 64; }
+static uint64_t whole_blocks(int64_t n) { return (uint64_t(n) + 127) / 128 * 128; }
+
+roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi_adamw* opt, const float* grad_scale, void* stream) {
+  if (count < 0) return ROI_ERR_SHAPE;
+  if (count > 0 && items == nullptr) return ROI_ERR_NULL;
+  OptimCall c{};
+  const roi_status s = adamw_constants(opt, &c.opt);
+  if (s != ROI_OK) return s;
+  std::vector<Tagged> ranges;
+  std::vector<OptimItem> to;
+  ranges.reserve(size_t(count) * 5 + 1);
+  to.reserve(size_t(count));
+  if (!aligned_to(grad_scale, 4)) return ROI_ERR_ALIGN;
+  add_range(ranges, grad_scale, 4, false);
+  for (int i = 0; i < count; ++i) {
+    const roi_adamw_step_item& x = items[i];
+    if (!known_type(x.grad_dtype) || (x.out_copy != nullptr && x.copy_dtype != ROI_BF16 && x.copy_dtype != ROI_FP16)) return ROI_ERR_TYPE;
+    if (!good_count(x.n)) return ROI_ERR_SHAPE;
+    if (x.n == 0) continue;
+    if (x.param == nullptr || x.grad == nullptr || x.m == nullptr || x.v == nullptr) return ROI_ERR_NULL;
+    if (!aligned16(x.param) || !aligned16(x.grad) || !aligned16(x.m) || !aligned16(x.v) || !aligned16(x.out_copy)) return ROI_ERR_ALIGN;
+    const uint64_t n = uint64_t(x.n);
+    add_range(ranges, x.grad, n * uint64_t(type_bytes(x.grad_dtype)), false);
+    add_range(ranges, x.param, n * 4, true);
+    add_range(ranges, x.m, n * 4, true);
+    add_range(ranges, x.v, n * 4, true);
+    add_range(ranges, x.out_copy, n * 2, true);
+    to.push_back({x.param, x.grad, x.m, x.v, nullptr, x.out_copy, x.n, 0u, static_cast<Elem>(x.grad_dtype),
+                  x.out_copy != nullptr ? static_cast<Elem>(x.copy_dtype) : Elem::kBf16});
+  }
+  if (batch_alias(ranges)) return ROI_ERR_ALIAS;
+  c.kind = OptimKind::kStep;
+  c.scale = grad_scale;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(launch_optim(c, to.data(), int(to.size())));
+}
+
+roi_status roi_adamw_step8(const roi_adamw_step8_item* items, int count, const roi_adamw* opt, uint64_t seed, const float* grad_scale,
+                           void* stream) {
+  if (count < 0) return ROI_ERR_SHAPE;
+  if (count > 0 && items == nullptr) return ROI_ERR_NULL;
+  OptimCall c{};
+  const roi_status s = adamw_constants(opt, &c.opt);
+  if (s != ROI_OK) return s;
+  std::vector<Tagged> ranges;
+  std::vector<OptimItem> to;
+  ranges.reserve(size_t(count) * 6 + 1);
+  to.reserve(size_t(count));
+  if (!aligned_to(grad_scale, 4)) return ROI_ERR_ALIGN;
+  add_range(ranges, grad_scale, 4, false);
+  for (int i = 0; i < count; ++i) {
+    const roi_adamw_step8_item& x = items[i];
+    if (!known_type(x.grad_dtype) || (x.out_copy != nullptr && x.copy_dtype != ROI_BF16 && x.copy_dtype != ROI_FP16)) return ROI_ERR_TYPE;
+    if (!good_count(x.n)) return ROI_ERR_SHAPE;
+    if (x.n == 0) continue;
+    if (x.param == nullptr || x.grad == nullptr || x.m_codes == nullptr || x.u_codes == nullptr || x.scales == nullptr) return ROI_ERR_NULL;
+    if (!aligned16(x.param) || !aligned16(x.grad) || !aligned16(x.m_codes) || !aligned16(x.u_codes) || !aligned_to(x.scales, 2) ||
+        !aligned16(x.out_copy))
+      return ROI_ERR_ALIGN;
+    const uint64_t n = uint64_t(x.n), codes = whole_blocks(x.n);
+    add_range(ranges, x.grad, n * uint64_t(type_bytes(x.grad_dtype)), false);
+    add_range(ranges, x.param, n * 4, true);
+    add_range(ranges, x.m_codes, codes, true);
+    add_range(ranges, x.u_codes, codes, true);
+    add_range(ranges, x.scales, codes / 64, true);
+    add_range(ranges, x.out_copy, n * 2, true);
+    to.push_back({x.param, x.grad, x.m_codes, x.u_codes, x.scales, x.out_copy, x.n, x.tensor_id, static_cast<Elem>(x.grad_dtype),
+                  x.out_copy != nullptr ? static_cast<Elem>(x.copy_dtype) : Elem::kBf16});
+  }
+  if (batch_alias(ranges)) return ROI_ERR_ALIAS;
+  c.kind = OptimKind::kStep8;
+  c.seed = seed;
+  c.step = opt->t;
+  c.scale = grad_scale;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(launch_optim(c, to.data(), int(to.size())));
+}
+
+roi_status roi_adamw_state8_load(const roi_adamw_state8_item* items, int count, void* stream) {
+  if (count < 0) return ROI_ERR_SHAPE;
+  if (count > 0 && items == nullptr) return ROI_ERR_NULL;
+  OptimCall c{};
+  std::vector<Tagged> ranges;
+  std::vector<OptimItem> to;
+  ranges.reserve(size_t(count) * 5);
+  to.reserve(size_t(count));
+  for (int i = 0; i < count; ++i) {
+    const roi_adamw_state8_item& x = items[i];
+    if (!known_type(x.dtype)) return ROI_ERR_TYPE;
+    if (!good_count(x.n)) return ROI_ERR_SHAPE;
+    if (x.n == 0) continue;
+    if (x.m_codes == nullptr || x.u_codes == nullptr || x.scales == nullptr || (x.out_m == nullptr && x.out_u == nullptr)) return ROI_ERR_NULL;
+    if (!aligned16(x.m_codes) || !aligned16(x.u_codes) || !aligned_to(x.scales, 2) || !aligned16(x.out_m) || !aligned16(x.out_u))
+      return ROI_ERR_ALIGN;
+    const uint64_t bytes = uint64_t(x.n) * uint64_t(type_bytes(x.dtype)), codes = whole_blocks(x.n);
+    add_range(ranges, x.m_codes, codes, false);
+    add_range(ranges, x.u_codes, codes, false);
+    add_range(ranges, x.scales, codes / 64, false);
+    add_range(ranges, x.out_m, bytes, true);
+    add_range(ranges, x.out_u, bytes, true);
+    to.push_back({static_cast<float*>(x.out_m), nullptr, const_cast<uint8_t*>(x.m_codes), const_cast<uint8_t*>(x.u_codes),
+                  const_cast<uint8_t*>(x.scales), x.out_u, x.n, 0u, static_cast<Elem>(x.dtype), Elem::kBf16});
+  }
+  if (batch_alias(ranges)) return ROI_ERR_ALIAS;
+  c.kind = OptimKind::kLoad8;
+  c.stream = static_cast<cudaStream_t>(stream);
+  return finish(launch_optim(c, to.data(), int(to.size())));
+}
+
 static roi_status noise_call(const roi_noise_state* st, int64_t rows, int64_t cols, uint32_t* words, float* g,
                              void* stream) {
   if (st == nullptr) return ROI_ERR_NULL;

@@ -213,6 +213,28 @@ struct Fp8LinearCall {
   cudaStream_t stream;
 };
 
+// AdamW over many tensors; what the pointers mean is in roi_optim.cu.
+enum class OptimKind { kStep, kStep8, kLoad8 };
+struct OptimItem {
+  float* p;
+  const void* g;
+  void* a;
+  void* b;
+  uint8_t* scales;
+  void* copy;
+  int64_t n;
+  uint32_t id;
+  Elem grad, copied;
+};
+struct OptimCall {
+  OptimKind kind;
+  AdamW opt;
+  uint64_t seed;
+  uint32_t step;
+  const float* scale;  // nullable
+  cudaStream_t stream;
+};
+
 // Each returns the number of kernels launched (>= 0) or -1 after a CUDA error.
 int launch_checkpoint_save(const CheckpointCall& c);
 int launch_checkpoint_load(const CheckpointCall& c);
@@ -227,6 +249,7 @@ int launch_wgrad(const WgradCall& c);
 int launch_fp8_save(const Fp8SaveCall& c);
 int launch_fp8_save_weight(const Fp8SaveCall& c);
 int launch_fp8_linear(const Fp8LinearCall& c);
+int launch_optim(const OptimCall& c, const OptimItem* items, int count);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);
 // Many independent tensors on one stream: one launch per tensor, or per run of
