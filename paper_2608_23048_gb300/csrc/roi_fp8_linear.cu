@@ -292,6 +292,8 @@ int launch_of(Elem e, const CUtensorMap& tm_w, const CUtensorMap& tm_x, const Li
 int launch_fp8_linear(const Fp8LinearCall& c) {
   LinearArgs a;
   const int64_t outs = c.dgrad ? c.cols : c.rows, width = c.dgrad ? c.rows : c.cols;
+  // tiles of a pair of CTAs where there are enough for half of the pairs
+  if (((c.T + 255) / 256) * ((outs + 223) / 224) >= sm_count() / 4 && c.T > 128) return launch_fp8_pair(c);
   a.w_scales = c.w_scales;
   a.x_scales = c.x_scales;
   a.out = c.out;

@@ -265,4 +265,42 @@ __device__ __forceinline__ void tc_copy_scales(uint32_t taddr, uint32_t saddr) {
   asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
 }
 
+// The same of a pair of CTAs, issued by one thread of the even CTA: M and N over the pair, each CTA with the scales of its
+// half of A's rows and of all of B's; a copy of scales takes each CTA's from its own shared memory to its own TMEM.
+__device__ __forceinline__ void tc_mma_mxf8_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa_tmem,
+                                                 uint32_t sb_tmem, bool accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa_tmem), "r"(sb_tmem), "r"(uint32_t(accumulate))
+      : "memory");
+}
+__device__ __forceinline__ void tc_copy_scales_pair(uint32_t taddr, uint32_t saddr) {
+  const uint64_t desc = tc_smem_desc(saddr, 128, 128);
+  asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+// The place of `p` in the shared memory of CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
+  uint32_t a;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+  return a;
+}
+// tma_load_2d into this CTA's shared memory that completes on a barrier of its pair (a cluster address).
+__device__ __forceinline__ void tma_load_2d_pair(void* dst_smem, const void* tmap, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          smem_addr(dst_smem)),
+      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+// A place in a ring of N, and the parity of the pass over it.
+template <int N>
+struct TcRing {
+  int at = 0;
+  uint32_t pass = 0;
+  __device__ __forceinline__ void next() {
+    if (++at == N) at = 0, pass ^= 1u;
+  }
+};
+
 }  // namespace roi

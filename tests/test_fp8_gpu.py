@@ -110,7 +110,8 @@ def product(roi, way, x, fmt, W, dtype, gap=0):  # noqa: F811
 # (tokens, outputs, width of the sum): one tile and parts of tiles, ranges of the sum in a cluster of every size, several
 # tiles of tokens, sums that end inside a block, more blocks than one word of scales
 SIZES = [(1, 1, 1), (1, 128, 128), (16, 128, 512), (17, 130, 640), (37, 128, 896), (100, 257, 1000), (256, 384, 1152), (257, 100, 300),
-         (300, 640, 130), (1, 2000, 2560), (64, 33, 5000), (600, 1000, 777), (130, 19500, 257)]
+         (300, 640, 130), (1, 2000, 2560), (64, 33, 5000), (600, 1000, 777), (130, 19500, 257), (700, 3000, 900), (2050, 1121, 400),
+         (300, 5000, 2500), (10000, 100, 130), (1537, 2001, 4200)]
 
 
 @pytest.mark.parametrize("way", ["fwd", "dgrad"])
