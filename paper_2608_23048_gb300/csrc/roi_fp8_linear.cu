@@ -8,8 +8,8 @@
 // The weight is the product's A (128 outputs of the tile in the lanes of TMEM), the tokens are B, so that few tokens
 // make narrow tiles.  A's tile is K-major in the forward and MN-major in the input gradient (one copy of the weight serves
 // both); tokens are K-major.  A CTA has one tile of 128 outputs by `n` tokens, or, where the tiles are
-// fewer than the SMs, a range of its sum: the CTAs of a tile are a cluster, put their sums into one another's shared memory and
-// add them in the order of the ranges, each for some of the tokens.
+// fewer than the SMs, a range of its sum: the CTAs of a tile are a cluster, copy their sums into one another's shared memory and
+// add them in the order of the ranges, each for some of the tokens.  Many tokens go to roi_fp8_pair.cu.
 #include <atomic>
 
 #include "roi_fp8.cuh"
@@ -28,7 +28,7 @@ constexpr int kMaxStages = 11;                  // 16 tokens
 constexpr int kScaleSlots = 4;                  // of four blocks' scales: 128 outputs, 256 tokens
 constexpr uint32_t kScaleBytes = 512 + 1024;
 constexpr uint32_t kOffScales = kRingBytes, kOffBars = kOffScales + kScaleSlots * kScaleBytes;
-constexpr int kBars = 2 * kMaxStages + 2 * kScaleSlots + 1;
+constexpr int kBars = 2 * kMaxStages + 2 * kScaleSlots + 2;
 constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 8;
 static_assert(kSmem + 1024 <= 232448, "shared memory");
 
@@ -43,18 +43,14 @@ struct LinearArgs {
   int tiles_o;
   int splits;     // ranges of a tile's sum: CTAs of a cluster
   int blocks;     // of the sum
+  int unbroken;   // the most blocks of a sum in TMEM: the next ones have columns of their own
   int stages;
   uint32_t idesc, tmem_cols;
   unsigned int* status;
   bool wait;
 };
 
-// Stores a float into the shared memory of CTA `rank` of the cluster at this CTA's `place`.
-__device__ __forceinline__ void store_cluster(uint32_t place, uint32_t rank, float v) {
-  asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\tst.shared::cluster.f32 [ra], %2;\n\t}" ::"r"(place),
-               "r"(rank), "f"(v)
-               : "memory");
-}
+constexpr uint32_t kGroupBytes = 16 * 128 * 4;  // the sums of 16 tokens
 
 template <bool DGRAD, Elem E>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -64,7 +60,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
   uint64_t *full = bars, *empty = full + kMaxStages, *scale_full = empty + kMaxStages, *scale_empty = scale_full + kScaleSlots;
-  uint64_t* done = scale_empty + kScaleSlots;
+  uint64_t *done = scale_empty + kScaleSlots, *joined = done + 1;
   uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = a.splits > 1 ? int(cluster_rank()) : 0;
@@ -83,6 +79,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(scale_empty + s, 1);
     }
     mbar_init(done, 1);
+    mbar_init(joined, 1);
     misc[1] = 1u;
     fence_mbar_init();
   }
@@ -90,7 +87,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = misc[0], scales_at = tmem + uint32_t((a.n + 31) / 32 * 32);
+  const uint32_t tmem = misc[0], scales_at = tmem + a.tmem_cols - 32;
   pdl_begin(a.wait);
 
   const uint64_t lim = ring_wait_limit(a.status);
@@ -117,7 +114,11 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else if (warp == 1) {
     int slot = 0, chunk = 0;
     uint32_t slot_pass = 0;
+    int piece_end = k0 + a.unbroken;
+    uint32_t d = tmem;
+    bool first = true;
     for (int k = k0; k < k1; ++k, ++committed) {
+      if (k == piece_end) piece_end += a.unbroken, d += uint32_t(a.n), first = true;
       const bool fresh = k == k0 || (k & 3) == 0, last = (k & 3) == 3 || k == k1 - 1;
       if (fresh) ok = agreed(mbar_wait_ring(scale_full + slot, slot_pass, lim));
       if (ok) ok = agreed(mbar_wait_ring(full + stage, pass, lim));
@@ -137,23 +138,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
 #pragma unroll
         for (int s = 0; s < kStep / 32; ++s)
-          tc_mma_mxf8(tmem, w + s * (DGRAD ? 4096 / 16 : 32 / 16), x + s * (32 / 16), idesc, sa, sb, s > 0 || k > k0);
+          tc_mma_mxf8(d, w + s * (DGRAD ? 4096 / 16 : 32 / 16), x + s * (32 / 16), idesc, sa, sb, s > 0 || !first);
         tc_commit(empty + stage);
         if (last) tc_commit(scale_empty + slot);
         if (k == k1 - 1) tc_commit(done);
       }
       __syncwarp();
+      first = false;
       if (++stage == a.stages) stage = 0, pass ^= 1u;
       if (last) {
         ++chunk;
         if (++slot == kScaleSlots) slot = 0, slot_pass ^= 1u;
       }
     }
-  } else if (warp == 2) {
-    // words of four blocks' scales: the weight's, the same for the tile's 128 outputs, and each token's
-    int slot = 0;
+  } else {
+    // two warps, every other chunk each: words of four blocks' scales, the weight's, the same for the tile's 128 outputs,
+    // and each token's
+    int slot = warp & 1;
     uint32_t slot_pass = 0;
-    for (int k = k0 & ~3; k < k1; k += 4) {
+    for (int k = (k0 & ~3) + 4 * slot; k < k1; k += 8) {
       uint32_t w = 0x7f7f7f7fu;
       if constexpr (DGRAD) {
         uint32_t byte = 0x7fu;
@@ -178,7 +181,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(scale_full + slot);
-      if (++slot == kScaleSlots) slot = 0, slot_pass ^= 1u;
+      if ((slot += 2) >= kScaleSlots) slot -= kScaleSlots, slot_pass ^= 1u;
     }
   }
   if (ok) ok = agreed(mbar_wait_ring(done, 0, lim));
@@ -198,51 +201,82 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   // a lane's output, and the tokens of the tile sixteen at a time
   const int64_t o = o0 + 32 * warp + lane;
-  T* out = static_cast<T*>(a.out) + o;
+  T* out = static_cast<T*>(a.out) + t0 * a.ldo + o;
   const uint32_t sums = tmem + (uint32_t(warp * 32) << 16);
-  const int groups = a.n / 16;
+  const int groups = a.n / 16, pieces = (k1 - k0 + a.unbroken - 1) / a.unbroken;
+  const int64_t left = o < a.outs ? a.T - t0 : 0;  // tokens, of which this lane writes
+  auto read = [&](int g, float (&v)[16]) {
+    uint32_t u[16];
+    tc_ld16(sums + 16 * g, u);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(u[e]);
+    for (int p = 1; p < pieces; ++p) {
+      tc_ld16(sums + p * a.n + 16 * g, u);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] += __uint_as_float(u[e]);
+    }
+  };
+  auto write = [&](int g, const float (&v)[16]) {
+    T* to = out + int64_t(16 * g) * a.ldo;
+#pragma unroll
+    for (int e = 0; e < 16; ++e, to += a.ldo)
+      if (16 * g + e < left) *to = from_f32<E>(v[e]);
+  };
   if (a.splits == 1) {
     for (int g = 0; whole && g < groups; ++g) {
-      uint32_t u[16];
-      tc_ld16(sums + 16 * g, u);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t t = t0 + 16 * g + e;
-        if (o < a.outs && t < a.T) out[t * a.ldo] = from_f32<E>(__uint_as_float(u[e]));
-      }
+      float v[16];
+      read(g, v);
+      write(g, v);
     }
   } else {
-    // Group g of tokens is added by CTA g % splits, where every CTA's sums lie one after another:
-    // [CTA][g / splits][16 tokens][128 outputs].
-    const int each = (groups + a.splits - 1) / a.splits;
-    cluster_sync();  // every CTA is done with its stages
+    // Group g of sixteen tokens is added by CTA g % splits.  A CTA's sums lie at the start, group after group ([16 tokens][128
+    // outputs]), then the other CTAs' of its groups: [CTA, itself left out][g / splits].
+    const int each = (groups + a.splits - 1) / a.splits, mine = (groups - rank + a.splits - 1) / a.splits;
+    float* own = reinterpret_cast<float*>(smem);
+    const int place = 32 * warp + lane;
+    bool all = whole;
     for (int g = 0; whole && g < groups; ++g) {
-      uint32_t u[16];
-      tc_ld16(sums + 16 * g, u);
-      const uint32_t place = smem_addr(smem) + uint32_t(((rank * each + g / a.splits) * 16) * 128 + 32 * warp + lane) * 4;
+      float v[16];
+      read(g, v);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) store_cluster(place + e * 512, uint32_t(g % a.splits), __uint_as_float(u[e]));
+      for (int e = 0; e < 16; ++e) own[(g * 16 + e) * 128 + place] = v[e];
     }
-    cluster_sync();
-    const float* from = reinterpret_cast<const float*>(smem) + 32 * warp + lane;
-    for (int g = rank; whole && g < groups; g += a.splits) {
-#pragma unroll 4
-      for (int e = 0; e < 16; ++e) {
-        const int64_t t = t0 + 16 * g + e;
-        if (o >= a.outs || t >= a.T) continue;
-        float v = 0.0f;
-        for (int r = 0; r < a.splits; ++r) v += from[((r * each + g / a.splits) * 16 + e) * 128];
-        out[t * a.ldo] = from_f32<E>(v);
+    fence_proxy_async_smem();
+    if (tid == 0) mbar_arrive_expect_tx(joined, uint32_t((a.splits - 1) * mine) * kGroupBytes);
+    cluster_sync();  // every CTA is done with its stages, and its sums lie there
+    if (warp == 0 && whole) {
+      for (int g = lane; g < groups; g += 32) {
+        const int to = g % a.splits;
+        if (to == rank) continue;
+        const uint32_t at = uint32_t(groups + (rank - (rank > to ? 1 : 0)) * each + g / a.splits) * kGroupBytes;
+        bulk_s2s(cluster_addr(smem + at, uint32_t(to)), smem + uint32_t(g) * kGroupBytes, kGroupBytes, cluster_addr(joined, uint32_t(to)));
       }
     }
+    if (all) all = agreed(mbar_wait_ring_cluster(joined, 0, lim));
+    if (!all && whole && lane == 0) atomicOr(a.status, kStatusTimeout);
+    for (int g = rank; all && g < groups; g += a.splits) {
+      float v[16];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = 0.0f;
+      for (int r = 0; r < a.splits; ++r) {
+        const int at = r == rank ? g : groups + (r - (r > rank ? 1 : 0)) * each + g / a.splits;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] += own[(at * 16 + e) * 128 + place];
+      }
+      write(g, v);
+    }
+    cluster_sync();  // what this CTA copied to the others has been read
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 0) tc_dealloc(tmem, a.tmem_cols);
 }
 
-// Bytes in which a CTA of a split tile takes its group's sums.
-uint32_t join_bytes(int n, int splits) { return uint32_t(splits) * uint32_t((n / 16 + splits - 1) / splits) * 16 * 128 * 4; }
+// Bytes in which a CTA of a split tile has its own sums and takes the others'.
+uint32_t join_bytes(int n, int splits) {
+  const int groups = n / 16, each = (groups + splits - 1) / splits;
+  return uint32_t(groups + (splits - 1) * each) * kGroupBytes;
+}
 
 template <bool DGRAD, Elem E>
 int launch(const CUtensorMap& tm_w, const CUtensorMap& tm_x, const LinearArgs& a, int64_t grid, cudaStream_t stream) {
@@ -287,13 +321,77 @@ int launch_of(Elem e, const CUtensorMap& tm_w, const CUtensorMap& tm_x, const Li
   }
 }
 
+// The most blocks of an unbroken sum for fp32 results, where TMEM has the columns (roi_fp8_pair.cu says why).
+constexpr int kMostBlocks = 16;
+
+// Clusters of `size` CTAs of this kernel that the device holds at once: a cluster lies within one of its GPCs, so that
+// they do not use every SM (7 CTAs to a cluster, 21 clusters, 147 CTAs on 152 SMs: two waves).
+int clusters_at_once(int size) {
+  if (size == 1) return sm_count();
+  static std::atomic<int> known[64][9];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
+  int n = known[dev][size].load(std::memory_order_acquire);
+  if (n == 0) {
+    auto kern = roi_fp8_linear_kernel<false, Elem::kBf16>;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(size);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(unsigned(size));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmem + 1024;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kSmem + 1024)) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) {
+      cudaGetLastError();
+      n = 1;
+    }
+    known[dev][size].store(n, std::memory_order_release);
+  }
+  return n;
+}
+
+// Tokens of a tile, ranges of its sum and their pieces, for the least time; returns that in cycles.  An SM takes in 64 bytes
+// a cycle: 2 (128 + n) cycles a block.  Filling the ring and writing the tile come once a tile, joining ranges once a range.
+constexpr int kTileCycles = 2000, kTokenCycles = 12, kJoinCycles = 2000;
+int64_t plan(int64_t T, int64_t tiles_o, int blocks, bool fp32, LinearArgs& a, int64_t& tiles_t) {
+  int64_t least = INT64_MAX;
+  int64_t last = 0;
+  for (int64_t t = (T + 255) / 256, tries = 0; tries < 16; ++t, ++tries) {
+    const int64_t n = ((T + t - 1) / t + 15) / 16 * 16;
+    if (n == last) continue;
+    last = n;
+    for (int s = 1; s <= 8 && s <= blocks; ++s) {
+      const int64_t once = clusters_at_once(s);
+      if (s > 1 && (tiles_o * t > once || join_bytes(int(n), s) > kRingBytes)) break;
+      const int range = (blocks + s - 1) / s;
+      int pieces = fp32 ? (range + kMostBlocks - 1) / kMostBlocks : 1;
+      const int room = int(480 / n);
+      if (pieces > room) pieces = room;
+      const int64_t rounds = (tiles_o * t + once - 1) / once;
+      const int64_t time = rounds * (range * 2 * (128 + n) + kTileCycles + kTokenCycles * n + (s > 1 ? kJoinCycles + kTokenCycles * n : 0));
+      if (time >= least) continue;
+      least = time;
+      tiles_t = (T + n - 1) / n;
+      a.n = int(n);
+      a.splits = s;
+      a.unbroken = (range + pieces - 1) / pieces;
+      a.tmem_cols = 64;
+      while (int(a.tmem_cols) < (int(n) * pieces + 31) / 32 * 32 + 32) a.tmem_cols *= 2;
+    }
+    if (t >= T) break;
+  }
+  return least;
+}
+
 }  // namespace
 
 int launch_fp8_linear(const Fp8LinearCall& c) {
   LinearArgs a;
   const int64_t outs = c.dgrad ? c.cols : c.rows, width = c.dgrad ? c.rows : c.cols;
-  // tiles of a pair of CTAs where there are enough for half of the pairs
-  if (((c.T + 255) / 256) * ((outs + 223) / 224) >= sm_count() / 4 && c.T > 128) return launch_fp8_pair(c);
   a.w_scales = c.w_scales;
   a.x_scales = c.x_scales;
   a.out = c.out;
@@ -305,17 +403,11 @@ int launch_fp8_linear(const Fp8LinearCall& c) {
   a.w_blocks = int((c.rows + 127) / 128);
   a.blocks = int((width + kStep - 1) / kStep);
   a.tiles_o = int((outs + 127) / 128);
-  const int64_t tiles_t = (c.T + 255) / 256;
-  a.n = int(((c.T + tiles_t - 1) / tiles_t + 15) / 16 * 16);
-  const int64_t tiles = a.tiles_o * tiles_t;
+  int64_t tiles_t;
+  if (plan(c.T, a.tiles_o, a.blocks, c.dtype == Elem::kFp32, a, tiles_t) > fp8_pair_cycles(c.T, outs, width)) return launch_fp8_pair(c);
   a.stages = int(kRingBytes / (kABytes + uint32_t(a.n) * kStep));
   if (a.stages > kMaxStages) a.stages = kMaxStages;
-  a.splits = 1;
-  while (a.splits < 8 && a.splits < a.blocks && tiles * (a.splits + 1) <= sm_count() && join_bytes(a.n, a.splits + 1) <= kRingBytes)
-    ++a.splits;
   a.idesc = tc_idesc_mxf8(128, a.n, int(Fp8::kE4M3), int(c.format), c.dgrad, false);
-  a.tmem_cols = 64;
-  while (int(a.tmem_cols) < (a.n + 31) / 32 * 32 + 32) a.tmem_cols *= 2;
   a.status = c.status;
   a.wait = lone_pdl(c.stream);
   CUtensorMap tm_w, tm_x;
@@ -325,7 +417,7 @@ int launch_fp8_linear(const Fp8LinearCall& c) {
       !make_tensor_map(&tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.x_codes, uint64_t(x_pitch), uint64_t(c.T), uint64_t(x_pitch), kStep,
                        uint32_t(a.n), CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
     return -1;
-  const int64_t grid = tiles * a.splits;
+  const int64_t grid = a.tiles_o * tiles_t * a.splits;
   return c.dgrad ? launch_of<true>(c.dtype, tm_w, tm_x, a, grid, c.stream) : launch_of<false>(c.dtype, tm_w, tm_x, a, grid, c.stream);
 }
 

@@ -1,15 +1,18 @@
-// The products of roi_fp8_linear.cu for many tokens: a pair of CTAs shares its MMAs (cta_group::2) and owns a tile of 256 tokens
-// by n outputs, n a multiple of 32 up to 224; each CTA holds 128 tokens, half of the outputs, and in TMEM the
-// sums of its 128 tokens.  The sums are double: 2 x 224 columns, and the scales of four chunks of four blocks take the other 64.
+// The products of roi_fp8_linear.cu for many tokens: a pair of CTAs shares its MMAs (cta_group::2) and owns a tile of 256 by n, n
+// a multiple of 32 up to 224.  Either tokens or outputs are the 256, A's rows: each CTA holds 128 of them and half of B's
+// n, and in TMEM the sums of its 128 rows.  The sums are double, 2 x 224 columns, and the scales of four chunks of four blocks
+// take the other 64.
 //
-// Roles of the 8 warps of a CTA, each a loop over the same list of tiles and blocks of 128:
-//   warp 0      stages tokens and weight by TMA; both CTAs' copies end on the even CTA's barrier
-//   warp 1      of the even CTA: copies of scales to TMEM, and four MMAs a block, for both; commits them to `empty`
-//               and, after the last block, to `sum`
-//   warp 2      stages scales: words of four blocks, of the CTA's 128 tokens and of the tile's outputs
-//   warps 4 - 7 read the sums from TMEM and write them out, `free`, while the next tile's MMAs go to the other half
+// Roles of the 12 warps of a CTA, each a loop over the same list of tiles and blocks of 128:
+//   warp 0       stages tokens and weight by TMA; both CTAs' copies end on the even CTA's barrier
+//   warp 1       of the even CTA: copies of scales to TMEM, and four MMAs a block, for both; commits them to `empty`
+//                and, after the last block, to `sum`
+//   warps 2, 3   stage scales, every other chunk each: words of four blocks, of the CTA's 128 rows of A and of all n of B
+//   warps 4 - 11 read the sums from TMEM and write them out, `free`, while the next tile's MMAs go to the other half; two
+//                warps share 32 rows
 // Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
 #include <atomic>
+#include <type_traits>
 
 #include "roi_fp8.cuh"
 #include "roi_launch.h"
@@ -19,17 +22,15 @@
 namespace roi {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kSide = 256;                 // tokens of a tile
+constexpr int kThreads = 384;
+constexpr int kSide = 256;                 // rows of A of a tile
 constexpr int kStep = 128;                 // of the sum a stage holds: a block
 constexpr int kMaxN = 224;
 constexpr int kStages = 6;
 constexpr uint32_t kABytes = 128 * kStep, kStageBytes = 2 * kABytes;
-constexpr int kScaleSlots = 4;             // of four blocks' scales: 128 tokens, up to 256 outputs
+constexpr int kScaleSlots = 4;             // of four blocks' scales: 128 rows of A, up to 256 of B
 constexpr uint32_t kScaleBytes = 512 + 1024;
-constexpr uint32_t kOffScales = kStages * kStageBytes, kOffBlocks = kOffScales + kScaleSlots * kScaleBytes;
-constexpr int kBlockPitch = 33;            // 32 rows of 32 sums for each of the warps that write, where rows are not whole sectors
-constexpr uint32_t kOffBars = kOffBlocks + 4 * 32 * kBlockPitch * 4;
+constexpr uint32_t kOffScales = kStages * kStageBytes, kOffBars = kOffScales + kScaleSlots * kScaleBytes;
 constexpr int kBars = 2 * kStages + 2 * kScaleSlots + 4;
 constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 8;
 static_assert(kSmem + 1024 <= 232448, "shared memory");
@@ -42,22 +43,22 @@ struct PairArgs {
   int64_t T, outs, ldo;
   int64_t w_spitch, x_spitch;
   int w_blocks;    // rows of the weight's scales
-  int n;           // outputs of a tile
+  int n;           // rows of B of a tile
   int tiles_m, tiles;
   int groups;      // pairs of CTAs
   int blocks;      // of the sum
-  int pieces;      // of the sum, added in out
+  int pieces;      // of the sum, added by the warps that write
+  int unbroken;    // blocks of a piece, whole chunks
   uint32_t idesc;
-  bool sectors;    // rows of out are whole sectors apart
   unsigned int* status;
   bool wait;
 };
 
-// A sum in TMEM: blocks k0 .. k1 of a tile; pieces after the first are added to out.
+// A sum in TMEM: blocks k0 .. k1 of a tile.
 struct Work {
   int64_t m0, n0;
   int k0, k1;
-  bool first;
+  bool first, last;  // of a tile's pieces
 };
 __device__ __forceinline__ bool work_of(const PairArgs& a, int g, int i, Work& w) {
   const int round = i / a.pieces, piece = i - round * a.pieces;
@@ -66,79 +67,70 @@ __device__ __forceinline__ bool work_of(const PairArgs& a, int g, int i, Work& w
   const int n = tile / a.tiles_m;
   w.m0 = int64_t(tile - n * a.tiles_m) * kSide;
   w.n0 = int64_t(n) * a.n;
-  w.k0 = int(int64_t(a.blocks) * piece / a.pieces);
-  w.k1 = int(int64_t(a.blocks) * (piece + 1) / a.pieces);
+  w.k0 = a.unbroken * piece;
+  w.k1 = piece == a.pieces - 1 ? a.blocks : w.k0 + a.unbroken;
   w.first = piece == 0;
+  w.last = piece == a.pieces - 1;
   return true;
 }
 
-// 32 columns of a row of the sums from column n on, where rows are whole sectors (the last may end inside one).
+// 16 columns of sums, from column c of the tile on, as the warps that write have them: lanes are A's rows, columns B's.
+// Tokens in the lanes: a lane writes its token's outputs, whole sectors (rows of out are whole sectors apart; the last of
+// a row may end inside one).
 template <Elem E>
-__device__ __forceinline__ void store_sectors(const PairArgs& a, bool first, int64_t m, int64_t n, const float (&v)[32], int width) {
+struct TokenLanes {
   using T = typename ElemType<E>::T;
-  constexpr int kPer = 32 / int(sizeof(T));  // columns of a sector
-  T* out = static_cast<T*>(a.out) + m * a.ldo + n;
+  T* out;      // the lane's row of out at the tile's first column
+  bool there;  // whether it has one
+  int width;   // columns of the tile
+  __device__ __forceinline__ TokenLanes(const PairArgs& a, const Work& w, int row) {
+    const int64_t t = w.m0 + row, left = a.outs - w.n0;
+    out = static_cast<T*>(a.out) + t * a.ldo + w.n0;
+    there = t < a.T;
+    width = left < a.n ? int(left) : a.n;
+  }
+  __device__ __forceinline__ void store(int c, const RowWords<E, 16>& r) const {
+    if (!there) return;
+    T* p = out + c;
+    if (c + 16 <= width) {
 #pragma unroll
-  for (int q = 0; q < 32 / kPer; ++q) {
-    if (kPer * q + kPer <= width) {
-      uint32_t w[8];
-      if constexpr (E == Elem::kFp32) {
-        if (!first) {
-          asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                       : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                       : "l"(out + 8 * q)
-                       : "memory");
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) + v[8 * q + e]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(v[8 * q + e]);
-        }
-      } else {
-        RowWords<E, 16> r;
-        float x[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = v[16 * q + e];
-        r.set(x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = r.u[e];
-      }
-      store32(out + kPer * q, w);
+      for (int q = 0; q < RowWords<E, 16>::kWords / 8; ++q) store32(reinterpret_cast<uint32_t*>(p) + 8 * q, r.u + 8 * q);
     } else {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) {
-        if (kPer * q + e >= width) break;
-        float x = v[kPer * q + e];
-        if (E == Elem::kFp32 && !first) x += to_f32<E>(out[kPer * q + e]);
-        out[kPer * q + e] = from_f32<E>(x);
-      }
+      for (int e = 0; e < 16; ++e)
+        if (c + e < width) p[e] = r.at(e);
     }
   }
-}
-// Any other rows (the whole warp, rows m0 on): through shared memory, so that a warp writes consecutive columns of a row.
+};
+// Outputs in the lanes: a warp writes 32 outputs of a token side by side, wherever rows start.
 template <Elem E>
-__device__ __forceinline__ void store_block(const PairArgs& a, bool first, float* block, int64_t m0, int64_t n, const float (&v)[32],
-                                            int width) {
+struct OutputLanes {
   using T = typename ElemType<E>::T;
-  const int lane = threadIdx.x & 31;
-  __syncwarp();
-#pragma unroll
-  for (int e = 0; e < 32; ++e) block[lane * kBlockPitch + e] = v[e];
-  __syncwarp();
-  const int64_t below = a.T - m0;
-  const int rows = lane >= width || below <= 0 ? 0 : below > 32 ? 32 : int(below);
-  T* out = static_cast<T*>(a.out) + m0 * a.ldo + n + lane;
-#pragma unroll 8
-  for (int r = 0; r < rows; ++r, out += a.ldo) {
-    float x = block[r * kBlockPitch + lane];
-    if (E == Elem::kFp32 && !first) x += to_f32<E>(*out);
-    *out = from_f32<E>(x);
+  T* out;  // the lane's output of the tile's first token
+  bool there;
+  int width;
+  int64_t ldo;
+  __device__ __forceinline__ OutputLanes(const PairArgs& a, const Work& w, int row) {
+    const int64_t o = w.m0 + row, left = a.T - w.n0;
+    out = static_cast<T*>(a.out) + w.n0 * a.ldo + o;
+    there = o < a.outs;
+    width = left < a.n ? int(left) : a.n;
+    ldo = a.ldo;
   }
-}
+  __device__ __forceinline__ void store(int c, const RowWords<E, 16>& r) const {
+    if (!there) return;
+    T* p = out + c * ldo;
+#pragma unroll
+    for (int e = 0; e < 16; ++e, p += ldo)
+      if (c + e < width) *p = r.at(e);
+  }
+};
 
-template <bool DGRAD, Elem E>
+// OUTPUTS: A is the weight (MN-major in the input gradient), B the tokens; else A is the tokens (forward only).
+template <bool DGRAD, bool OUTPUTS, Elem E>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    roi_fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w, PairArgs a) {
+    roi_fp8_pair_kernel(const __grid_constant__ CUtensorMap tm_a, const __grid_constant__ CUtensorMap tm_b, PairArgs a) {
+  static_assert(OUTPUTS || !DGRAD, "the weight is A where it is MN-major: whole tiles of 128 columns are aligned");
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
@@ -161,7 +153,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(sum + b, 1);
-      mbar_init(free + b, 4 * 2);
+      mbar_init(free + b, 8 * 2);
     }
     misc[1] = 1u;
     fence_mbar_init();
@@ -184,7 +176,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   auto agreed = [](bool mine) { return __all_sync(0xffffffffu, mine) != 0; };
   const int half = a.n / 2;
   if (warp == 0) {
-    const uint32_t b_bytes = DGRAD ? kABytes : uint32_t(half) * kStep;
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       const int m = int(w.m0) + int(rank) * 128, n = int(w.n0) + int(rank) * half;
       for (int k = w.k0; k < w.k1; ++k, ++issued, ring.next()) {
@@ -192,31 +183,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         if (!ok) break;
         uint8_t* st = smem + ring.at * kStageBytes;
         if (elect_one()) {
-          if (rank == 0) mbar_arrive_expect_tx(full + ring.at, 2 * (kABytes + b_bytes));
+          if (rank == 0) mbar_arrive_expect_tx(full + ring.at, 2 * (kABytes + uint32_t(half) * kStep));
           const uint32_t bar = cluster_addr(full + ring.at, 0);
-          tma_load_2d_pair(st, &tm_x, k * kStep, m, bar);
-          if constexpr (DGRAD) tma_load_2d_pair(st + kABytes, &tm_w, n, k * kStep, bar);
-          else tma_load_2d_pair(st + kABytes, &tm_w, k * kStep, n, bar);
+          if constexpr (DGRAD) tma_load_2d_pair(st, &tm_a, m, k * kStep, bar);
+          else tma_load_2d_pair(st, &tm_a, k * kStep, m, bar);
+          tma_load_2d_pair(st + kABytes, &tm_b, k * kStep, n, bar);
         }
         __syncwarp();
       }
     }
   } else if (warp == 1) {
     if (rank == 0) {
-      const uint64_t x0 = tc_smem_desc_k128(smem_addr(smem));
-      const uint64_t w0 = DGRAD ? tc_smem_desc_mn128(smem_addr(smem + kABytes), kABytes) : tc_smem_desc_k128(smem_addr(smem + kABytes));
+      const uint64_t a0 = DGRAD ? tc_smem_desc_mn128(smem_addr(smem), kABytes) : tc_smem_desc_k128(smem_addr(smem));
+      const uint64_t b0 = tc_smem_desc_k128(smem_addr(smem + kABytes));
       const uint32_t scales0 = smem_addr(smem + kOffScales);
       for (int i = 0; ok && work_of(a, g, i, w); ++i) {
         const int b = i & 1;
         ok = agreed(mbar_wait_ring_cluster(free + b, (uint32_t(i >> 1) & 1u) ^ 1u, lim));
         const uint32_t d = tmem + uint32_t(b) * kMaxN;
         for (int k = w.k0; ok && k < w.k1; ++k, ++committed, ring.next()) {
-          const bool fresh = k == w.k0 || (k & 3) == 0, last = (k & 3) == 3 || k == w.k1 - 1;
+          const bool fresh = (k & 3) == 0, last = (k & 3) == 3 || k == w.k1 - 1;
           if (fresh) ok = agreed(mbar_wait_ring_cluster(scale_full + slot.at, slot.pass, lim));
           if (ok) ok = agreed(mbar_wait_ring_cluster(full + ring.at, ring.pass, lim));
           if (!ok) break;
           tc_fence_after();
-          const uint64_t x = x0 + uint32_t(ring.at) * (kStageBytes / 16), v = w0 + uint32_t(ring.at) * (kStageBytes / 16);
+          const uint64_t ad = a0 + uint32_t(ring.at) * (kStageBytes / 16), bd = b0 + uint32_t(ring.at) * (kStageBytes / 16);
           const uint32_t idesc = tc_idesc_scale_byte(a.idesc, uint32_t(k) & 3u);
           const uint32_t sa = tmem + kTmemScales + uint32_t(slot.at) * 16, sb = sa + 4;
           if (elect_one()) {
@@ -228,7 +219,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
             }
 #pragma unroll
             for (int s = 0; s < kStep / 32; ++s)
-              tc_mma_mxf8_pair(d, x + s * (32 / 16), v + s * (DGRAD ? 4096 / 16 : 32 / 16), idesc, sa, sb, s > 0 || k > w.k0);
+              tc_mma_mxf8_pair(d, ad + s * (DGRAD ? 4096 / 16 : 32 / 16), bd + s * (32 / 16), idesc, sa, sb, s > 0 || k > w.k0);
             tc_commit_pair(empty + ring.at);
             if (last) tc_commit_pair(scale_empty + slot.at);
             if (k == w.k1 - 1) tc_commit_pair(sum + b);
@@ -238,73 +229,93 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
         }
       }
     }
-  } else if (warp == 2) {
+  } else if (warp < 4) {
+    uint32_t chunk = 0;  // of all
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
-      const int64_t t = w.m0 + int64_t(rank) * 128 + lane, b0 = w.n0 / 128;
-      for (int k = w.k0 & ~3; k < w.k1; k += 4, slot.next()) {
-        uint32_t x[4], word[3] = {0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu};
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          x[q] = t + 32 * q < a.T ? *reinterpret_cast<const uint32_t*>(a.x_scales + (t + 32 * q) * a.x_spitch + k) : 0x7f7f7f7fu;
-        // the tile's outputs lie in three blocks of 128 at most
+      const int64_t row = w.m0 + int64_t(rank) * 128;  // A's first here
+      // the weight's blocks of 128 outputs: A's one here, or the three at most that B's n lie in
+      constexpr int kWords = OUTPUTS ? 1 : 3;
+      const int64_t block = (OUTPUTS ? row : w.n0) / 128, t0 = OUTPUTS ? w.n0 : row;
+      for (int k = w.k0; k < w.k1; k += 4, slot.next(), ++chunk) {
+        if ((chunk & 1u) != uint32_t(warp & 1)) continue;
+        uint32_t word[kWords];
         if constexpr (DGRAD) {
-          const int block = lane >> 2, row = k + (lane & 3);
+          // (a block of the sum is a row of scales)
           uint32_t byte = 0x7fu;
-          if (block < 3 && b0 + block < a.w_spitch && row < a.w_blocks) byte = a.w_scales[int64_t(row) * a.w_spitch + b0 + block];
+          if (lane < 4 && k + lane < a.w_blocks && block < a.w_spitch) byte = a.w_scales[int64_t(k + lane) * a.w_spitch + block];
           byte <<= 8 * (lane & 3);
           byte |= __shfl_xor_sync(0xffffffffu, byte, 1);
           byte |= __shfl_xor_sync(0xffffffffu, byte, 2);
-#pragma unroll
-          for (int j = 0; j < 3; ++j) word[j] = __shfl_sync(0xffffffffu, byte, 4 * j);
+          word[0] = __shfl_sync(0xffffffffu, byte, 0);
         } else {
 #pragma unroll
-          for (int j = 0; j < 3; ++j)
-            if (b0 + j < a.w_blocks) word[j] = *reinterpret_cast<const uint32_t*>(a.w_scales + (b0 + j) * a.w_spitch + k);
+          for (int j = 0; j < kWords; ++j)
+            word[j] = block + j < a.w_blocks ? *reinterpret_cast<const uint32_t*>(a.w_scales + (block + j) * a.w_spitch + k) : 0x7f7f7f7fu;
         }
-        uint32_t o[8];
+        uint32_t x[8], o[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int64_t j = (w.n0 + 32 * q + lane) / 128 - b0;
-          o[q] = j == 0 ? word[0] : j == 1 ? word[1] : word[2];
+        for (int q = 0; q < (OUTPUTS ? 8 : 4); ++q) {
+          const int64_t t = t0 + 32 * q + lane;
+          x[q] = t < a.T && (!OUTPUTS || 32 * q < a.n) ? *reinterpret_cast<const uint32_t*>(a.x_scales + t * a.x_spitch + k) : 0x7f7f7f7fu;
+        }
+#pragma unroll
+        for (int q = 0; q < (OUTPUTS ? 4 : 8); ++q) {
+          if constexpr (OUTPUTS) {
+            o[q] = word[0];
+          } else {
+            const int64_t j = (w.n0 + 32 * q + lane) / 128 - block;
+            o[q] = j == 0 ? word[0] : j == 1 ? word[1] : word[2];
+          }
         }
         ok = agreed(mbar_wait_ring_cluster(scale_empty + slot.at, slot.pass ^ 1u, lim));
         if (!ok) break;
         uint8_t* to = smem + kOffScales + slot.at * kScaleBytes + 16 * lane;
-        *reinterpret_cast<uint4*>(to) = make_uint4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<uint4*>(to + 512) = make_uint4(o[0], o[1], o[2], o[3]);
-        *reinterpret_cast<uint4*>(to + 1024) = make_uint4(o[4], o[5], o[6], o[7]);
+        const uint32_t(&ra)[8] = OUTPUTS ? o : x, (&rb)[8] = OUTPUTS ? x : o;
+        *reinterpret_cast<uint4*>(to) = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+        *reinterpret_cast<uint4*>(to + 512) = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+        *reinterpret_cast<uint4*>(to + 1024) = make_uint4(rb[4], rb[5], rb[6], rb[7]);
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive_cluster(scale_full + slot.at, 0);
       }
     }
   } else if (warp >= 4) {
-    const int quarter = warp & 3;
-    float* block = reinterpret_cast<float*>(smem + kOffBlocks) + quarter * 32 * kBlockPitch;
+    using Lanes = std::conditional_t<OUTPUTS, OutputLanes<E>, TokenLanes<E>>;
+    const int quarter = warp & 3, part = (warp - 4) >> 2;  // 32 rows, and every other 16 columns
+    constexpr int kChunks = kMaxN / 32;
+    // They leave TMEM before any is written: in 16 bits, or, fp32, added to what earlier pieces left.
+    RowWords<E, 16> kept[kChunks];
     for (int i = 0; ok && work_of(a, g, i, w); ++i) {
       const int b = i & 1;
-      const int64_t m = w.m0 + int64_t(rank) * 128 + quarter * 32 + lane;
+      const Lanes out(a, w, int(rank) * 128 + quarter * 32 + lane);
       ok = agreed(mbar_wait_ring_cluster(sum + b, uint32_t(i >> 1) & 1u, lim));
       if (!ok) break;
       tc_fence_after();
-      const int64_t left = a.outs - w.n0;
-      const int width = left < a.n ? int(left) : a.n;
-      for (int c = 0; c < width; c += 32) {
-        uint32_t u[32];
-        tc_ld32(tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * kMaxN + c), u);
-        float v[32];
+      const uint32_t from = tmem + (uint32_t(quarter * 32) << 16) + uint32_t(b * kMaxN + 16 * part);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] = __uint_as_float(u[e]);
-        const int cols = width - c < 32 ? width - c : 32;
-        if (a.sectors) {
-          if (m < a.T) store_sectors<E>(a, w.first, m, w.n0 + c, v, cols);
+      for (int q = 0; q < kChunks; ++q) {
+        // (columns past the tile's are read, and not written)
+        uint32_t u[16];
+        tc_ld16(from + 32 * q, u);
+        if constexpr (E == Elem::kFp32) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) kept[q].u[e] = __float_as_uint(__uint_as_float(w.first ? 0u : kept[q].u[e]) + __uint_as_float(u[e]));
         } else {
-          store_block<E>(a, w.first, block, m - lane, w.n0 + c, v, cols);
+          float v[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = __uint_as_float(u[e]);
+          kept[q].set(v);
         }
       }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(free + b, 0);
+      if (!w.last) continue;
+#pragma unroll
+      for (int q = 0; q < kChunks; ++q) {
+        const int c = 16 * (2 * q + part);
+        if (c < out.width) out.store(c, kept[q]);
+      }
     }
   }
   if (!ok) misc[1] = 0u;
@@ -325,9 +336,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 0) tc_dealloc_pair(tmem, kTmemCols);
 }
 
-template <bool DGRAD, Elem E>
-int launch(const CUtensorMap& tm_x, const CUtensorMap& tm_w, const PairArgs& a, int grid, cudaStream_t stream) {
-  auto kern = roi_fp8_pair_kernel<DGRAD, E>;
+template <bool DGRAD, bool OUTPUTS, Elem E>
+int launch(const CUtensorMap& tm_a, const CUtensorMap& tm_b, const PairArgs& a, int grid, cudaStream_t stream) {
+  auto kern = roi_fp8_pair_kernel<DGRAD, OUTPUTS, E>;
   constexpr size_t smem = kSmem + 1024;
   static std::atomic<bool> set[64];
   int dev = 0;
@@ -336,34 +347,46 @@ int launch(const CUtensorMap& tm_x, const CUtensorMap& tm_w, const PairArgs& a, 
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return -1;
     set[dev].store(true, std::memory_order_release);
   }
-  return launch_maybe_pdl(kern, grid, kThreads, smem, stream, a.wait, tm_x, tm_w, a);
+  return launch_maybe_pdl(kern, grid, kThreads, smem, stream, a.wait, tm_a, tm_b, a);
 }
 
-template <bool DGRAD>
-int launch_of(Elem e, const CUtensorMap& tm_x, const CUtensorMap& tm_w, const PairArgs& a, int grid, cudaStream_t stream) {
+template <bool DGRAD, bool OUTPUTS>
+int launch_of(Elem e, const CUtensorMap& tm_a, const CUtensorMap& tm_b, const PairArgs& a, int grid, cudaStream_t stream) {
   switch (e) {
-    case Elem::kBf16: return launch<DGRAD, Elem::kBf16>(tm_x, tm_w, a, grid, stream);
-    case Elem::kFp16: return launch<DGRAD, Elem::kFp16>(tm_x, tm_w, a, grid, stream);
-    default: return launch<DGRAD, Elem::kFp32>(tm_x, tm_w, a, grid, stream);
+    case Elem::kBf16: return launch<DGRAD, OUTPUTS, Elem::kBf16>(tm_a, tm_b, a, grid, stream);
+    case Elem::kFp16: return launch<DGRAD, OUTPUTS, Elem::kFp16>(tm_a, tm_b, a, grid, stream);
+    default: return launch<DGRAD, OUTPUTS, Elem::kFp32>(tm_a, tm_b, a, grid, stream);
   }
 }
 
-// The fewest rounds of tiles over the pairs, each as long as its outputs (and what a tile costs besides, in outputs).
-constexpr int kTileCost = 16;
-int outputs_of(int64_t tiles_m, int64_t outs, int groups) {
-  int best = kMaxN;
+// A block's stage brings an SM 128 rows of A and n / 2 of B, 64 bytes a cycle: 256 + n cycles, where its MMAs take 2 n.  Measured
+// a round of tiles (8192 tokens, 3584 x 18944), n = 128, 160, 192, 224: 40.1, 42.2, 46.1, 48.9 us, 0.10 us per 256 + n.
+// What a tile, and the launch, cost besides is from a sweep over 1 to 4096 tokens of seven layers.
+constexpr int kTileCycles = 2000, kLaunchCycles = 4000;
+// Finds the n of the least time for tiles of `m` by n outputs; returns that time in cycles.
+int64_t rows_of_b(int64_t m, int64_t n, int blocks, int groups, int& best) {
   int64_t least = INT64_MAX;
-  for (int n = kMaxN; n >= 64; n -= 32) {
-    const int64_t tiles = tiles_m * ((outs + n - 1) / n), rounds = (tiles + groups - 1) / groups;
-    if (rounds * (n + kTileCost) < least) least = rounds * (n + kTileCost), best = n;
+  for (int b = kMaxN; b >= 64; b -= 32) {
+    const int64_t tiles = ((m + kSide - 1) / kSide) * ((n + b - 1) / b);
+    const int64_t time = (tiles + groups - 1) / groups * (int64_t(256 + b) * blocks + kTileCycles) + kLaunchCycles;
+    if (time < least) least = time, best = b;
   }
-  return best;
+  return least;
 }
 
-// The most blocks of an unbroken sum for fp32 results (the tensor cores drop what is below a sum's last bit).
+// The most blocks of an unbroken sum for fp32 results.  The tensor cores drop the bits below their sum's last instead of
+// rounding, an error that grows with the sum: 1.4e-6 of the result's norm over 18944, where an fp32 product has 2.1e-7.
+// Pieces of 64, 32, 16 blocks: 3.5e-7, 2.0e-7, 1.2e-7.
 constexpr int kMostBlocks = 16;
 
 }  // namespace
+
+int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width) {
+  const int groups = sm_count() / 2, blocks = int((width + kStep - 1) / kStep);
+  int n;
+  const int64_t a = rows_of_b(T, outs, blocks, groups, n), b = rows_of_b(outs, T, blocks, groups, n);
+  return a < b ? a : b;
+}
 
 int launch_fp8_pair(const Fp8LinearCall& c) {
   PairArgs a;
@@ -378,25 +401,37 @@ int launch_fp8_pair(const Fp8LinearCall& c) {
   a.x_spitch = fp8_scale_pitch(width);
   a.w_blocks = int((c.rows + 127) / 128);
   a.blocks = int((width + kStep - 1) / kStep);
-  a.pieces = c.dtype == Elem::kFp32 ? (a.blocks + kMostBlocks - 1) / kMostBlocks : 1;
+  a.unbroken = c.dtype == Elem::kFp32 ? kMostBlocks : (a.blocks + 3) / 4 * 4;
+  a.pieces = (a.blocks + a.unbroken - 1) / a.unbroken;
   a.groups = sm_count() / 2;
-  a.tiles_m = int((c.T + kSide - 1) / kSide);
-  a.n = outputs_of(a.tiles_m, outs, a.groups);
-  a.tiles = int(a.tiles_m * ((outs + a.n - 1) / a.n));
-  a.idesc = tc_idesc_mxf8(kSide, a.n, int(c.format), int(Fp8::kE4M3), false, c.dgrad);
+  // Tokens in the lanes need whole sectors of out and K-major weights; with both ways open, the one of fewer rounds.
   const int b = c.dtype == Elem::kFp32 ? 4 : 2;
-  a.sectors = (reinterpret_cast<uintptr_t>(c.out) & 31u) == 0 && c.ldo * b % 32 == 0;
+  bool outputs = c.dgrad || (reinterpret_cast<uintptr_t>(c.out) & 31u) != 0 || c.ldo * b % 32 != 0;
+  const int64_t by_outputs = rows_of_b(outs, c.T, a.blocks, a.groups, a.n);
+  if (!outputs) {
+    int n;
+    if (rows_of_b(c.T, outs, a.blocks, a.groups, n) <= by_outputs) a.n = n;
+    else outputs = true;
+  }
+  const int64_t m = outputs ? outs : c.T, n = outputs ? c.T : outs;
+  a.tiles_m = int((m + kSide - 1) / kSide);
+  a.tiles = int(a.tiles_m * ((n + a.n - 1) / a.n));
+  a.idesc = outputs ? tc_idesc_mxf8(kSide, a.n, int(Fp8::kE4M3), int(c.format), c.dgrad, false)
+                    : tc_idesc_mxf8(kSide, a.n, int(c.format), int(Fp8::kE4M3), false, false);
   a.status = c.status;
   a.wait = lone_pdl(c.stream);
-  CUtensorMap tm_w, tm_x;
   const int64_t w_pitch = fp8_pitch(c.cols), x_pitch = fp8_pitch(width);
-  if (!make_tensor_map(&tm_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.w_codes, uint64_t(w_pitch), uint64_t(c.rows), uint64_t(w_pitch), 128,
-                       c.dgrad ? kStep : uint32_t(a.n) / 2, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B) ||
-      !make_tensor_map(&tm_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.x_codes, uint64_t(x_pitch), uint64_t(c.T), uint64_t(x_pitch), kStep, 128,
-                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B))
+  auto map = [](CUtensorMap* t, const uint8_t* codes, int64_t pitch, int64_t rows, int box) {
+    return make_tensor_map(t, CU_TENSOR_MAP_DATA_TYPE_UINT8, codes, uint64_t(pitch), uint64_t(rows), uint64_t(pitch), 128, uint32_t(box),
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+  };
+  CUtensorMap tm_w, tm_x;
+  if (!map(&tm_w, c.w_codes, w_pitch, c.rows, outputs ? 128 : a.n / 2) || !map(&tm_x, c.x_codes, x_pitch, c.T, outputs ? a.n / 2 : 128))
     return -1;
   const int grid = 2 * (a.tiles < a.groups ? a.tiles : a.groups);
-  return c.dgrad ? launch_of<true>(c.dtype, tm_x, tm_w, a, grid, c.stream) : launch_of<false>(c.dtype, tm_x, tm_w, a, grid, c.stream);
+  if (c.dgrad) return launch_of<true, true>(c.dtype, tm_w, tm_x, a, grid, c.stream);
+  return outputs ? launch_of<false, true>(c.dtype, tm_w, tm_x, a, grid, c.stream)
+                 : launch_of<false, false>(c.dtype, tm_x, tm_w, a, grid, c.stream);
 }
 
 }  // namespace roi

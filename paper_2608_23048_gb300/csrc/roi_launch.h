@@ -249,7 +249,9 @@ int launch_wgrad(const WgradCall& c);
 int launch_fp8_save(const Fp8SaveCall& c);
 int launch_fp8_save_weight(const Fp8SaveCall& c);
 int launch_fp8_linear(const Fp8LinearCall& c);
-int launch_fp8_pair(const Fp8LinearCall& c);  // (many tokens)
+// (many tokens; and the time it would take, in cycles)
+int launch_fp8_pair(const Fp8LinearCall& c);
+int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width);
 int launch_optim(const OptimCall& c, const OptimItem* items, int count);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);

@@ -293,6 +293,13 @@ __device__ __forceinline__ void tma_load_2d_pair(void* dst_smem, const void* tma
       "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(bar)
       : "memory");
 }
+// Bytes (a multiple of 16) from this CTA's shared memory to another's of its cluster (cluster addresses), completing on a
+// barrier there.
+__device__ __forceinline__ void bulk_s2s(uint32_t dst, const void* src_smem, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+               "r"(smem_addr(src_smem)), "r"(bytes), "r"(bar)
+               : "memory");
+}
 // A place in a ring of N, and the parity of the pass over it.
 template <int N>
 struct TcRing {
