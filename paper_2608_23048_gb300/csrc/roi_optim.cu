@@ -9,17 +9,19 @@
 // The probability is compared in 16 bits, m's in the low and u's in the high half of the element's Philox word (counter
 // as the mask's noise: element / 4, step, tensor).  The parameters take the step from the moments before they are rounded.
 //
-// Bound by memory in 32 bits (28 bytes an element, fp32 gradients); in 8 (16 bytes) near the rate of its instructions.
+// Bound by memory in 32 bits (28 bytes an element, fp32 gradients); in 8 (16 bytes) near the rate of its instructions too.
 //
-// Tensors are cut into tiles of 1024 elements that follow one another over all tensors; a CTA has a range of them.  A
-// thread has four elements of a tile, so in 8 bits a warp has a block.
+// Tensors are cut into tiles that follow one another over all tensors; a CTA has a range of them.  A thread has 8
+// consecutive elements of a tile, or 16 where the moments are in 8 bits: whole sectors of each array, and a block in eight
+// neighbouring lanes.
 #include "roi_launch.h"
+#include "roi_rows.cuh"
 
 namespace roi {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTile = 4 * kThreads;
+constexpr int kThreads = 128;
+constexpr int kEach32 = 8, kEach8 = 16;
 
 struct Item {
   float* p;
@@ -32,117 +34,196 @@ struct Item {
   int64_t tile0;    // its first tile among all
   uint32_t id;
   uint8_t grad, copied;  // roi_dtype
+  bool sectors;          // every array starts on a sector
 };
 constexpr int kMost = 400;  // items a launch
 struct Args {
   int count;
   bool wait;
   AdamW opt;
-  uint32_t k0, k1, step;
+  uint32_t keys[2][10];  // of Philox's rounds
+  uint32_t step;
   const float* scale;  // nullable: a factor of the gradients
   int64_t tiles;
   Item it[kMost];
 };
 static_assert(sizeof(Args) <= 32764, "kernel parameter block");
 
-__device__ __forceinline__ float element(uint32_t word, int half, bool fp16) {
-  const uint16_t h = uint16_t(half ? word >> 16 : word);
-  return fp16 ? to_f32<Elem::kFp16>(h) : to_f32<Elem::kBf16>(h);
-}
-// Four gradients from element e on (a multiple of 4), zeros past the last.
-__device__ __forceinline__ void load_grad(const Item& it, int64_t e, float (&g)[4]) {
-  const bool whole = e + 4 <= it.n;
-  if (it.grad == uint8_t(Elem::kFp32)) {
-    const float* p = static_cast<const float*>(it.g) + e;
-    if (whole) {
-      const float4 x = __ldcs(reinterpret_cast<const float4*>(p));
-      g[0] = x.x, g[1] = x.y, g[2] = x.z, g[3] = x.w;
-    } else {
+// N elements from the `left` of a row that are left (zeros past them), and back.
+template <Elem E, int N>
+__device__ __forceinline__ void load_words(const void* p, int64_t left, bool sectors, RowWords<E, N>& r) {
+  using T = typename ElemType<E>::T;
+  constexpr int W = RowWords<E, N>::kWords;
+  if (left >= N && W % 8 == 0 && sectors) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) g[i] = e + i < it.n ? p[i] : 0.0f;
+    for (int i = 0; i < W / 8; ++i)
+      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(r.u[8 * i]), "=r"(r.u[8 * i + 1]), "=r"(r.u[8 * i + 2]), "=r"(r.u[8 * i + 3]), "=r"(r.u[8 * i + 4]),
+                     "=r"(r.u[8 * i + 5]), "=r"(r.u[8 * i + 6]), "=r"(r.u[8 * i + 7])
+                   : "l"(static_cast<const uint32_t*>(p) + 8 * i)
+                   : "memory");
+  } else if (left >= N) {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i) {
+      const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+      r.u[4 * i] = v.x, r.u[4 * i + 1] = v.y, r.u[4 * i + 2] = v.z, r.u[4 * i + 3] = v.w;
     }
   } else {
-    const uint16_t* p = static_cast<const uint16_t*>(it.g) + e;
-    const bool fp16 = it.grad == uint8_t(Elem::kFp16);
-    uint2 x = make_uint2(0u, 0u);
-    if (whole) {
-      x = __ldcs(reinterpret_cast<const uint2*>(p));
-    } else {
-      if (e < it.n) x.x = p[0];
-      if (e + 1 < it.n) x.x |= uint32_t(p[1]) << 16;
-      if (e + 2 < it.n) x.y = p[2];
+    r.zero();
+    const T* q = static_cast<const T*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (i < left) {
+        if constexpr (E == Elem::kFp32) r.u[i] = __float_as_uint(q[i]);
+        else r.u[i / 2] |= uint32_t(q[i]) << (16 * (i % 2));
+      }
     }
-    g[0] = element(x.x, 0, fp16), g[1] = element(x.x, 1, fp16), g[2] = element(x.y, 0, fp16), g[3] = element(x.y, 1, fp16);
   }
 }
-__device__ __forceinline__ void load4(const float* p, int64_t e, int64_t n, float (&v)[4]) {
-  if (e + 4 <= n) {
-    const float4 x = *reinterpret_cast<const float4*>(p + e);
-    v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w;
-  } else {
+template <Elem E, int N>
+__device__ __forceinline__ void store_words(void* p, int64_t left, bool sectors, const RowWords<E, N>& r) {
+  using T = typename ElemType<E>::T;
+  constexpr int W = RowWords<E, N>::kWords;
+  if (left >= N && W % 8 == 0 && sectors) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = e + i < n ? p[e + i] : 0.0f;
+    for (int i = 0; i < W / 8; ++i) store32(static_cast<uint32_t*>(p) + 8 * i, r.u + 8 * i);
+  } else if (left >= N) {
+#pragma unroll
+    for (int i = 0; i < W / 4; ++i)
+      reinterpret_cast<uint4*>(p)[i] = make_uint4(r.u[4 * i], r.u[4 * i + 1], r.u[4 * i + 2], r.u[4 * i + 3]);
+  } else {
+    T* q = static_cast<T*>(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < left) q[i] = r.at(i);
   }
 }
-__device__ __forceinline__ void store4(float* p, int64_t e, int64_t n, const float (&v)[4]) {
-  if (e + 4 <= n) {
-    *reinterpret_cast<float4*>(p + e) = make_float4(v[0], v[1], v[2], v[3]);
+template <int N>
+__device__ __forceinline__ void load_floats(const void* p, int64_t left, bool sectors, float (&v)[N]) {
+  RowWords<Elem::kFp32, N> r;
+  load_words(p, left, sectors, r);
+  r.get(v);
+}
+template <int N>
+__device__ __forceinline__ void store_floats(void* p, int64_t left, bool sectors, const float (&v)[N]) {
+  RowWords<Elem::kFp32, N> r;
+  r.set(v);
+  store_words(p, left, sectors, r);
+}
+// In 16 bits or 32.
+template <int N>
+__device__ __forceinline__ void load_any(const void* p, uint8_t type, int64_t e, int64_t left, bool sectors, float (&v)[N]) {
+  if (type == uint8_t(Elem::kFp32)) {
+    load_floats(static_cast<const float*>(p) + e, left, sectors, v);
+    return;
+  }
+  RowWords<Elem::kBf16, N> r;
+  load_words(static_cast<const uint16_t*>(p) + e, left, sectors, r);
+  if (type == uint8_t(Elem::kBf16)) {
+    r.get(v);
   } else {
+    RowWords<Elem::kFp16, N> h;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e + i < n) p[e + i] = v[i];
+    for (int i = 0; i < N / 2; ++i) h.u[i] = r.u[i];
+    h.get(v);
   }
 }
-// Rounded to bf16 or fp16.
-__device__ __forceinline__ void store_half4(void* to, bool fp16, int64_t e, int64_t n, const float (&v)[4]) {
-  uint16_t h[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = fp16 ? from_f32<Elem::kFp16>(v[i]) : from_f32<Elem::kBf16>(v[i]);
-  uint16_t* p = static_cast<uint16_t*>(to) + e;
-  if (e + 4 <= n) {
-    *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | uint32_t(h[1]) << 16, h[2] | uint32_t(h[3]) << 16);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (e + i < n) p[i] = h[i];
+template <int N>
+__device__ __forceinline__ void store_any(void* p, uint8_t type, int64_t e, int64_t left, bool sectors, const float (&v)[N]) {
+  if (type == uint8_t(Elem::kFp32)) {
+    store_floats(static_cast<float*>(p) + e, left, sectors, v);
+    return;
   }
+  RowWords<Elem::kBf16, N> r;
+  if (type == uint8_t(Elem::kBf16)) {
+    r.set(v);
+  } else {
+    RowWords<Elem::kFp16, N> h;
+    h.set(v);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) r.u[i] = h.u[i];
+  }
+  store_words(static_cast<uint16_t*>(p) + e, left, sectors, r);
 }
 
 // ---------------------------------------------------------------------------
 // moments in 8 bits
 // ---------------------------------------------------------------------------
-// A code's bits at the place of a float's are the code's value times 2^-120, subnormals among them.
 constexpr int kMBits = 3, kUBits = 4;
-template <int BITS>
-__device__ __forceinline__ float decode(uint32_t code, float step) {
-  constexpr uint32_t kNaN = BITS == kMBits ? 0x7fu : 0xffu;
-  const uint32_t c = BITS == kMBits ? code & 0x7fu : code;
-  float v = __uint_as_float(c << (23 - BITS)) * __uint_as_float((120u + 127u) << 23) * step;
-  if (c == kNaN) v = __uint_as_float(0x7fc00000u);
-  return BITS == kMBits && (code & 0x80u) != 0u ? -v : v;
+// Scale bytes that no step writes stand for the nearest that one does.
+__device__ __forceinline__ uint32_t state_byte(uint32_t s) { return min(max(s, 1u), 247u); }
+__device__ __forceinline__ float power(uint32_t biased) { return __uint_as_float(biased << 23); }
+// Up to here 2^(s - 7) and 2^(7 - s) are float32 numbers; above, factors come in two.
+constexpr uint32_t kScaleDirect = 133;
+
+// Four codes of m: the instruction gives them in fp16, which holds them, and NaN with them.
+__device__ __forceinline__ void decode_m4(uint32_t w, float step, float* v) {
+  uint32_t a, b;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
+      : "=r"(a), "=r"(b)
+      : "r"(w));
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
+  v[0] = x.x * step, v[1] = x.y * step, v[2] = y.x * step, v[3] = y.y * step;
 }
-// 2^(s - 127), and 2^(127 - s); scale bytes that no step writes stand for the nearest that one does.
-__device__ __forceinline__ float scale_step(uint32_t s) { return __uint_as_float(min(max(s, 1u), 247u) << 23); }
-__device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - s) << 23); }
+// Whether a byte of w is zero.
+__device__ __forceinline__ bool zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
+// Four codes of u: a code's bits at the place of a float's are its value times 2^-120, subnormals among them.
+__device__ __forceinline__ void decode_u4(uint32_t w, uint32_t s, float* v) {
+  constexpr uint32_t kMask = 0xffu << 19;
+  const float k = power(s <= kScaleDirect ? s + 120u : 247u);
+  v[0] = __uint_as_float((w << 19) & kMask) * k;
+  v[1] = __uint_as_float((w << 11) & kMask) * k;
+  v[2] = __uint_as_float((w << 3) & kMask) * k;
+  v[3] = __uint_as_float((w >> 5) & kMask) * k;
+  if (s > kScaleDirect) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] *= power(s);
+  }
+  if (zero_byte(~w)) {  // the last code, a NaN
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (((w >> (8 * i)) & 0xffu) == 0xffu) v[i] = __uint_as_float(0x7fc00000u);
+  }
+}
 // The scale byte from the bits of the largest finite magnitude (largest codes 1.75 2^8 and 1.875 2^8).
 template <int BITS>
 __device__ __forceinline__ uint32_t state_scale(uint32_t top_bits) {
   constexpr uint32_t kAbove = BITS == kMBits ? 0x1fffffu : 0x0fffffu;
   return uint32_t(max(int((top_bits + kAbove) >> 23) - 8, 1));
 }
-// The code of a magnitude: what is below its last bit decides with 16 random bits whether it is rounded up.
+// The code of a magnitude, in bits 16 on: x 2^(127 - s) 2^-120 has the code at the head of a float's bits (products towards
+// zero: what is under 2^-149 is dropped), and the 16 bits behind it decide with 16 random ones whether it is rounded up.
 template <int BITS>
-__device__ __forceinline__ uint32_t encode(float x, float inverse, uint32_t random) {
-  constexpr int kDrop = 23 - BITS;
-  const uint32_t bits = abs_bits(x);
-  // (towards zero: what is under 2^-149 is dropped)
-  const uint32_t t = __float_as_uint(__fmul_rz(__uint_as_float(bits) * inverse, __uint_as_float((127u - 120u) << 23)));
-  const uint32_t code = (t + (random << (kDrop - 16))) >> kDrop;
-  return bits >= kInfBits ? (BITS == kMBits ? 0x7fu : 0xffu) : code;
+__device__ __forceinline__ uint32_t encode(float x, float k, uint32_t random) {
+  return (__float_as_uint(__fmul_rz(fabsf(x), k)) >> (7 - BITS)) + random;
+}
+// Any scale, and what is not finite.
+template <int BITS>
+__device__ __forceinline__ uint32_t encode_any(float x, uint32_t s, uint32_t random) {
+  if (abs_bits(x) >= kInfBits) return (BITS == kMBits ? 0x7fu : 0xffu) << 16;
+  // (2^-100 first: of what that rounds, nothing reaches a code of a block whose largest is over 2^14)
+  return s <= kScaleDirect ? encode<BITS>(x, power(134u - s), random) : encode<BITS>(x * power(27u), __uint_as_float(s <= 233u ? (234u - s) << 23 : 1u << (256u - s)), random);
 }
 __device__ __forceinline__ uint32_t finite_bits(float x) {
   const uint32_t b = abs_bits(x);
   return b >= kInfBits ? 0u : b;
+}
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Of the eight lanes of a block.
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+#pragma unroll
+  for (int m = 1; m < 8; m *= 2) v = max(v, __shfl_xor_sync(0xffffffffu, v, m));
+  return v;
+}
+// Byte k of each of four words.
+template <int K>
+__device__ __forceinline__ uint32_t pack_byte(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  constexpr uint32_t kPick = K | (K + 4) << 4;
+  return __byte_perm(__byte_perm(a, b, kPick), __byte_perm(c, d, kPick), 0x5410);
 }
 
 // One element's step; u is the root of the new v.  (adamw_elem, operation for operation.)
@@ -177,20 +258,32 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_step_kernel(const __grid_c
   for (Walk w(a); w.tile < w.end; ++w.tile) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
-    const int64_t e = (w.tile - it.tile0) * kTile + 4 * threadIdx.x;
-    if (e >= it.n) continue;
-    float p[4], g[4], m[4], v[4], u;
-    load4(it.p, e, it.n, p);
-    load4(static_cast<const float*>(it.a), e, it.n, m);
-    load4(static_cast<const float*>(it.b), e, it.n, v);
-    load_grad(it, e, g);
+    const int64_t e = (w.tile - it.tile0) * (kThreads * kEach32) + kEach32 * threadIdx.x, left = it.n - e;
+    if (left <= 0) continue;
+    const bool sectors = it.sectors;
+    float p[kEach32], g[kEach32], m[kEach32], v[kEach32], u;
+    load_floats(it.p + e, left, sectors, p);
+    load_floats(static_cast<const float*>(it.a) + e, left, sectors, m);
+    load_floats(static_cast<const float*>(it.b) + e, left, sectors, v);
+    load_any(it.g, it.grad, e, left, sectors, g);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) step_elem(p[i], a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v[i], u, a.opt);
-    store4(it.p, e, it.n, p);
-    store4(static_cast<float*>(it.a), e, it.n, m);
-    store4(static_cast<float*>(it.b), e, it.n, v);
-    if (it.copy != nullptr) store_half4(it.copy, it.copied == uint8_t(Elem::kFp16), e, it.n, p);
+    for (int i = 0; i < kEach32; ++i) step_elem(p[i], a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v[i], u, a.opt);
+    store_floats(it.p + e, left, sectors, p);
+    store_floats(static_cast<float*>(it.a) + e, left, sectors, m);
+    store_floats(static_cast<float*>(it.b) + e, left, sectors, v);
+    if (it.copy != nullptr) store_any(it.copy, it.copied, e, left, sectors, p);
   }
+}
+
+// The words of elements 4 q on.
+__device__ __forceinline__ uint4 words_of(const Args& a, uint64_t q, uint32_t id) {
+  uint4 c = make_uint4(uint32_t(q), uint32_t(q >> 32), a.step, id);
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = uint64_t(kPhiloxM0) * c.x, p1 = uint64_t(kPhiloxM1) * c.z;
+    c = make_uint4(uint32_t(p1 >> 32) ^ c.y ^ a.keys[0][r], uint32_t(p1), uint32_t(p0 >> 32) ^ c.w ^ a.keys[1][r], uint32_t(p0));
+  }
+  return c;
 }
 
 __global__ void __launch_bounds__(kThreads) roi_adamw_step8_kernel(const __grid_constant__ Args a) {
@@ -200,46 +293,89 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_step8_kernel(const __grid_
   for (Walk w(a); w.tile < w.end; ++w.tile) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
-    const int64_t e = (w.tile - it.tile0) * kTile + 4 * threadIdx.x;
-    if (e - 4 * lane >= it.n) continue;  // (a warp has a block)
-    uint32_t* mc = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(it.a) + e);
-    uint32_t* uc = reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(it.b) + e);
+    const int64_t e = (w.tile - it.tile0) * (kThreads * kEach8) + kEach8 * threadIdx.x, left = it.n - e;
+    if (left + kEach8 * lane <= 0) continue;  // (a warp has four blocks)
+    const bool there = left + kEach8 * (lane & 7) > 0, sectors = it.sectors;
+    uint4* mc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.a) + e);
+    uint4* uc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.b) + e);
     uint16_t* sc = reinterpret_cast<uint16_t*>(it.scales) + (e >> 7);
-    float p[4], g[4], m[4], u[4];
-    load4(it.p, e, it.n, p);
-    load_grad(it, e, g);
-    const uint32_t mw = *mc, uw = *uc, sw = *sc;
-    const uint4 random = philox4x32_10(make_uint4(uint32_t(e >> 2), uint32_t(uint64_t(e) >> 34), a.step, it.id), a.k0, a.k1);
-    const float m_step = scale_step(sw & 0xffu), u_step = scale_step(sw >> 8);
-    uint32_t m_top = 0, u_top = 0;
+    float p[16], g[16], m[16], u[16];
+    uint4 mw = make_uint4(0u, 0u, 0u, 0u), uw = mw;
+    uint32_t sw = 0;
+    load_floats(it.p + e, left, sectors, p);
+    load_any(it.g, it.grad, e, left, sectors, g);
+    if (there) mw = *mc, uw = *uc, sw = *sc;
+    const float m_step = power(state_byte(sw & 0xffu));
+    const uint32_t u_byte = state_byte(sw >> 8);
+    decode_m4(mw.x, m_step, m), decode_m4(mw.y, m_step, m + 4), decode_m4(mw.z, m_step, m + 8), decode_m4(mw.w, m_step, m + 12);
+    decode_u4(uw.x, u_byte, u), decode_u4(uw.y, u_byte, u + 4), decode_u4(uw.z, u_byte, u + 8), decode_u4(uw.w, u_byte, u + 12);
+    float m_top = 0.0f, u_top = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      m[i] = decode<kMBits>((mw >> (8 * i)) & 0xffu, m_step);
-      u[i] = decode<kUBits>((uw >> (8 * i)) & 0xffu, u_step);
+    for (int i = 0; i < 16; ++i) {
       float v = __fmul_rn(u[i], u[i]);
       step_elem(p[i], a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v, u[i], a.opt);
-      if (e + i >= it.n) m[i] = 0.0f, u[i] = 0.0f;  // (padding's codes are 0)
-      m_top = max(m_top, finite_bits(m[i]));
-      u_top = max(u_top, finite_bits(u[i]));
     }
-    const uint32_t ms = state_scale<kMBits>(__reduce_max_sync(0xffffffffu, m_top)),
-                   us = state_scale<kUBits>(__reduce_max_sync(0xffffffffu, u_top));
-    const float m_inverse = scale_inverse(ms), u_inverse = scale_inverse(us);
-    const uint32_t r[4] = {random.x, random.y, random.z, random.w};
-    uint32_t mo = 0, uo = 0;
+    store_floats(it.p + e, left, sectors, p);
+    if (it.copy != nullptr) store_any(it.copy, it.copied, e, left, sectors, p);
+    if (left < 16) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t c = encode<kMBits>(m[i], m_inverse, r[i] & 0xffffu) | ((__float_as_uint(m[i]) >> 24) & 0x80u);
-      uint32_t d = encode<kUBits>(u[i], u_inverse, r[i] >> 16);
-      if (u[i] > 0.0f) d = max(d, 1u);  // what is not zero stays so: a step divides by it
-      mo |= c << (8 * i);
-      uo |= d << (8 * i);
+      for (int i = 0; i < 16; ++i)
+        if (i >= left) m[i] = 0.0f, u[i] = 0.0f;  // (padding's codes are 0)
     }
-    *mc = mo;
-    *uc = uo;
-    if (lane == 0) *sc = uint16_t(ms | us << 8);
-    store4(it.p, e, it.n, p);
-    if (it.copy != nullptr) store_half4(it.copy, it.copied == uint8_t(Elem::kFp16), e, it.n, p);
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      m_top = max3_nan(m_top, fabsf(m[i]), fabsf(m[i + 1]));
+      u_top = max3_nan(u_top, u[i], u[i + 1]);
+    }
+    // (a NaN's bits are above an infinity's)
+    uint32_t m_bits = block_max(abs_bits(m_top)), u_bits = block_max(abs_bits(u_top));
+    uint32_t ms = state_scale<kMBits>(m_bits), us = state_scale<kUBits>(u_bits);
+    const bool direct = max(m_bits, u_bits) < kInfBits && max(ms, us) <= kScaleDirect;
+    uint32_t mo[4], uo[4];
+    if (__all_sync(0xffffffffu, direct)) {
+      const float mk = power(134u - ms), uk = power(134u - us);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4 r = words_of(a, uint64_t(e >> 2) + q, it.id);
+        const float* x = m + 4 * q;
+        const float* y = u + 4 * q;
+        mo[q] = pack_byte<2>(encode<kMBits>(x[0], mk, r.x & 0xffffu), encode<kMBits>(x[1], mk, r.y & 0xffffu),
+                             encode<kMBits>(x[2], mk, r.z & 0xffffu), encode<kMBits>(x[3], mk, r.w & 0xffffu));
+        uo[q] = pack_byte<2>(encode<kUBits>(y[0], uk, r.x >> 16), encode<kUBits>(y[1], uk, r.y >> 16), encode<kUBits>(y[2], uk, r.z >> 16),
+                             encode<kUBits>(y[3], uk, r.w >> 16));
+      }
+    } else {
+      m_bits = u_bits = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m_bits = max(m_bits, finite_bits(m[i])), u_bits = max(u_bits, finite_bits(u[i]));
+      ms = state_scale<kMBits>(block_max(m_bits)), us = state_scale<kUBits>(block_max(u_bits));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4 r = words_of(a, uint64_t(e >> 2) + q, it.id);
+        const float* x = m + 4 * q;
+        const float* y = u + 4 * q;
+        mo[q] = pack_byte<2>(encode_any<kMBits>(x[0], ms, r.x & 0xffffu), encode_any<kMBits>(x[1], ms, r.y & 0xffffu),
+                             encode_any<kMBits>(x[2], ms, r.z & 0xffffu), encode_any<kMBits>(x[3], ms, r.w & 0xffffu));
+        uo[q] = pack_byte<2>(encode_any<kUBits>(y[0], us, r.x >> 16), encode_any<kUBits>(y[1], us, r.y >> 16),
+                             encode_any<kUBits>(y[2], us, r.z >> 16), encode_any<kUBits>(y[3], us, r.w >> 16));
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float* x = m + 4 * q;
+      mo[q] |= pack_byte<3>(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])) & 0x80808080u;
+      if (zero_byte(uo[q])) {
+        // what is not zero stays so: a step divides by it
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (((uo[q] >> (8 * i)) & 0xffu) == 0u && u[4 * q + i] > 0.0f) uo[q] |= 1u << (8 * i);
+      }
+    }
+    if (there) {
+      *mc = make_uint4(mo[0], mo[1], mo[2], mo[3]);
+      *uc = make_uint4(uo[0], uo[1], uo[2], uo[3]);
+      if ((lane & 7) == 0) *sc = uint16_t(ms | us << 8);
+    }
   }
 }
 
@@ -249,25 +385,21 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_state8_load_kernel(const _
   for (Walk w(a); w.tile < w.end; ++w.tile) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
-    const int64_t e = (w.tile - it.tile0) * kTile + 4 * threadIdx.x;
-    if (e >= it.n) continue;
-    const uint32_t mw = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(it.a) + e);
-    const uint32_t uw = *reinterpret_cast<const uint32_t*>(static_cast<const uint8_t*>(it.b) + e);
+    const int64_t e = (w.tile - it.tile0) * (kThreads * kEach8) + kEach8 * threadIdx.x, left = it.n - e;
+    if (left <= 0) continue;
+    const uint4 mw = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.a) + e);
+    const uint4 uw = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.b) + e);
     const uint32_t sw = reinterpret_cast<const uint16_t*>(it.scales)[e >> 7];
-    const float m_step = scale_step(sw & 0xffu), u_step = scale_step(sw >> 8);
-    float m[4], u[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      m[i] = decode<kMBits>((mw >> (8 * i)) & 0xffu, m_step);
-      u[i] = decode<kUBits>((uw >> (8 * i)) & 0xffu, u_step);
+    const float m_step = power(state_byte(sw & 0xffu));
+    const uint32_t u_byte = state_byte(sw >> 8);
+    float v[16];
+    if (it.p != nullptr) {
+      decode_m4(mw.x, m_step, v), decode_m4(mw.y, m_step, v + 4), decode_m4(mw.z, m_step, v + 8), decode_m4(mw.w, m_step, v + 12);
+      store_any(it.p, it.grad, e, left, it.sectors, v);
     }
-    if (it.grad == uint8_t(Elem::kFp32)) {
-      if (it.p != nullptr) store4(it.p, e, it.n, m);
-      if (it.copy != nullptr) store4(static_cast<float*>(it.copy), e, it.n, u);
-    } else {
-      const bool fp16 = it.grad == uint8_t(Elem::kFp16);
-      if (it.p != nullptr) store_half4(it.p, fp16, e, it.n, m);
-      if (it.copy != nullptr) store_half4(it.copy, fp16, e, it.n, u);
+    if (it.copy != nullptr) {
+      decode_u4(uw.x, u_byte, v), decode_u4(uw.y, u_byte, v + 4), decode_u4(uw.z, u_byte, v + 8), decode_u4(uw.w, u_byte, v + 12);
+      store_any(it.copy, it.grad, e, left, it.sectors, v);
     }
   }
 }
@@ -279,10 +411,13 @@ int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
   bool wait = lone_pdl(c.stream);
   Args a;
   a.opt = c.opt;
-  a.k0 = uint32_t(c.seed);
-  a.k1 = uint32_t(c.seed >> 32);
+  for (uint32_t r = 0; r < 10; ++r) {
+    a.keys[0][r] = uint32_t(c.seed) + r * kPhiloxW0;
+    a.keys[1][r] = uint32_t(c.seed >> 32) + r * kPhiloxW1;
+  }
   a.step = c.step;
   a.scale = c.scale;
+  const int tile = kThreads * (c.kind == OptimKind::kStep ? kEach32 : kEach8);
   auto kern = c.kind == OptimKind::kStep ? roi_adamw_step_kernel
               : c.kind == OptimKind::kStep8 ? roi_adamw_step8_kernel
                                             : roi_adamw_state8_load_kernel;
@@ -292,12 +427,16 @@ int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
     for (; i < count && a.count < kMost; ++i) {
       const OptimItem& x = items[i];
       if (x.n == 0) continue;
-      a.it[a.count++] = {x.p, x.g, x.a, x.b, x.scales, x.copy, x.n, a.tiles, x.id, uint8_t(x.grad), uint8_t(x.copied)};
-      a.tiles += (x.n + kTile - 1) / kTile;
+      // (codes are accessed by 16 bytes)
+      uintptr_t starts = reinterpret_cast<uintptr_t>(x.p) | reinterpret_cast<uintptr_t>(x.g) | reinterpret_cast<uintptr_t>(x.copy);
+      if (c.kind == OptimKind::kStep) starts |= reinterpret_cast<uintptr_t>(x.a) | reinterpret_cast<uintptr_t>(x.b);
+      a.it[a.count++] = {x.p,  x.g,     x.a,  x.b, x.scales,        x.copy,          x.n,
+                         a.tiles, x.id, uint8_t(x.grad), uint8_t(x.copied), (starts & 31u) == 0};
+      a.tiles += (x.n + tile - 1) / tile;
     }
     if (a.count == 0) break;
     a.wait = wait;
-    const int64_t cap = int64_t(sm_count()) * 5;
+    const int64_t cap = int64_t(sm_count()) * (c.kind == OptimKind::kStep ? 10 : c.kind == OptimKind::kStep8 ? 5 : 16);  // held at once
     if (launch_maybe_pdl(kern, int(a.tiles < cap ? a.tiles : cap), kThreads, 0, c.stream, wait, a) < 0) return -1;
     ++launched;
     wait = true;
