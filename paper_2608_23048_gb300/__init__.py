@@ -753,12 +753,21 @@ def new_fp8_weight(rows, cols, device="cuda"):
             torch.empty((rows + 127) // 128, roi_fp8_scale_pitch(cols), dtype=torch.uint8, device=device))
 
 
-def _fp8(pair, name, rows, cols, weight=False):
+_UINT8 = None  # torch.uint8, once torch is there
+
+
+def _fp8(pair, name, rows, cols, scale_rows):
     """Addresses of a copy's codes and scales (of a matrix [rows, cols])."""
-    import torch
+    global _UINT8
     codes, scales = pair
+    if (codes.dtype is _UINT8 and scales.dtype is _UINT8 and codes.is_cuda and scales.is_cuda and codes.is_contiguous()
+            and scales.is_contiguous() and codes.shape == (rows, (cols + 127) // 128 * 128)
+            and scales.shape == (scale_rows, (cols + 2047) // 2048 * 16)):
+        return codes.data_ptr(), scales.data_ptr()
+    import torch
+    _UINT8 = torch.uint8
     _check_tensor(codes, f"{name} codes", torch.uint8, (rows, (cols + 127) // 128 * 128))
-    _check_tensor(scales, f"{name} scales", torch.uint8, ((rows + 127) // 128 if weight else rows, (cols + 2047) // 2048 * 16))
+    _check_tensor(scales, f"{name} scales", torch.uint8, (scale_rows, (cols + 2047) // 2048 * 16))
     return codes.data_ptr(), scales.data_ptr()
 
 
@@ -767,7 +776,7 @@ def roi_fp8_save(x, format, out_codes, out_scales, stream=None):
     ("e4m3" or "e5m2") with a power of two for every 128 columns of a row."""
     ld = _stride(x, "x")
     rows, cols = x.shape
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, rows)
     s = lib().roi_fp8_save(x.data_ptr(), _type(x, "x"), rows, cols, ld, _format(format), codes, scales, _stream(stream))
     _raise(s, "roi_fp8_save")
 
@@ -777,31 +786,34 @@ def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
     import torch
     rows, cols = W.shape
     _check_tensor(W, "W", torch.bfloat16)
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, True)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, (rows + 127) // 128)
     s = lib().roi_fp8_save_weight(W.data_ptr(), rows, cols, codes, scales, _stream(stream))
     _raise(s, "roi_fp8_save_weight")
 
 
-def _fp8_linear(name, dgrad, x8, format, w8, out, stream):
-    ld = _stride(out, "out")
-    T, outs = out.shape
-    rows = w8[0].shape[0]
-    # the columns of the sum, or of the weight: padding is zeros, so a whole number of blocks stands for them
-    cols = outs if dgrad else w8[0].shape[1]
-    xq, xs = _fp8(x8, "x8", T, rows if dgrad else cols)
-    wq, ws = _fp8(w8, "w8", rows if dgrad else outs, cols, True)
-    s = getattr(lib(), name)(xq, xs, _format(format), wq, ws, T, rows, cols, out.data_ptr(), _type(out, "out"), ld, _stream(stream))
-    _raise(s, name)
-
-
 def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
     """out_y[T, rows] = x w^T from the (codes, scales) pairs of an activation (`format`) and of a weight."""
-    _fp8_linear("roi_fp8_linear_fwd", False, x8, format, w8, out_y, stream)
+    ld = _stride(out_y, "out_y")
+    T, rows = out_y.shape
+    # padding codes are zeros, so the whole blocks stand for the columns
+    cols = w8[0].shape[1]
+    xq, xs = _fp8(x8, "x8", T, cols, T)
+    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128)
+    s = lib().roi_fp8_linear_fwd(xq, xs, _format(format), wq, ws, T, rows, cols, out_y.data_ptr(), _type(out_y, "out_y"), ld,
+                                 _stream(stream))
+    _raise(s, "roi_fp8_linear_fwd")
 
 
 def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
     """out_dx[T, cols] = dy w, from the (codes, scales) pairs of dy [T, rows] (`format`) and of the weight [rows, cols]."""
-    _fp8_linear("roi_fp8_linear_dgrad", True, dy8, format, w8, out_dx, stream)
+    ld = _stride(out_dx, "out_dx")
+    T, cols = out_dx.shape
+    rows = w8[0].shape[0]
+    dq, ds = _fp8(dy8, "dy8", T, rows, T)
+    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128)
+    s = lib().roi_fp8_linear_dgrad(dq, ds, _format(format), wq, ws, T, rows, cols, out_dx.data_ptr(), _type(out_dx, "out_dx"), ld,
+                                   _stream(stream))
+    _raise(s, "roi_fp8_linear_dgrad")
 
 
 # ---------------------------------------------------------------------------
@@ -904,9 +916,9 @@ def make_adamw_state8_items(items):
 
 
 def _grad_scale(t):
-    import torch
     if t is None:
         return None
+    import torch
     _same_size(t, "grad_scale", torch.float32, 1)
     return t.data_ptr()
 

@@ -116,17 +116,21 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_weight_kernel(WeightArg
     const int64_t bm = b / a.blocks_n, bn = b - bm * a.blocks_n;
     const int64_t r0 = bm * 128 + (threadIdx.x >> 3), c = bn * 128 + 16 * (threadIdx.x & 7);
     RowWords<Elem::kBf16, 16> r[kPieces];
+    if constexpr (ANYWHERE) {
+      Window<Elem::kBf16, 16> w[kPieces];  // (all on their way before the first is used)
 #pragma unroll
-    for (int i = 0; i < kPieces; ++i) {
-      const int64_t row = r0 + 32 * i;
-      if constexpr (ANYWHERE) {
-        Window<Elem::kBf16, 16> w;
-        w.load(a.W + row * a.cols, c, row < a.rows ? a.cols : 0);
-        w.get(r[i]);
-      } else if (row < a.rows && c + 16 <= a.cols) {
-        load32(a.W + row * a.cols + c, r[i].u);
-      } else {
-        r[i].zero();  // (columns come in sixteens)
+      for (int i = 0; i < kPieces; ++i) {
+        const int64_t row = r0 + 32 * i;
+        w[i].load(a.W + row * a.cols, c, row < a.rows ? a.cols : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) w[i].get(r[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int64_t row = r0 + 32 * i;
+        if (row < a.rows && c + 16 <= a.cols) load32(a.W + row * a.cols + c, r[i].u);
+        else r[i].zero();  // (columns come in sixteens)
       }
     }
     uint32_t top = 0;

@@ -382,7 +382,7 @@ int64_t plan(int64_t T, int64_t tiles_o, int blocks, bool fp32, LinearArgs& a, i
       a.tmem_cols = 64;
       while (int(a.tmem_cols) < (int(n) * pieces + 31) / 32 * 32 + 32) a.tmem_cols *= 2;
     }
-    if (t >= T) break;
+    if (n == 16) break;
   }
   return least;
 }

@@ -21,7 +21,8 @@ namespace roi {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kEach32 = 8, kEach8 = 16;
+constexpr int kEach32 = 8, kEach8 = 16, kBlock = 128;
+constexpr int kCtas32 = 10, kCtas8 = 7, kCtasLoad = 12;  // of an SM
 
 struct Item {
   float* p;
@@ -36,18 +37,24 @@ struct Item {
   uint8_t grad, copied;  // roi_dtype
   bool sectors;          // every array starts on a sector
 };
-constexpr int kMost = 400;  // items a launch
-struct Args {
+// Items a launch: a launch copies its arguments whole, so few have a form of their own.
+constexpr int kMost = 400, kFew = 24;
+struct Settings {
   int count;
   bool wait;
   AdamW opt;
   uint32_t keys[2][10];  // of Philox's rounds
   uint32_t step;
   const float* scale;  // nullable: a factor of the gradients
+  bool plain;          // (8 bits) settings within quick_pair's range
+  float one;           // 1, as a number that the compiler does not know (add2)
   int64_t tiles;
-  Item it[kMost];
 };
-static_assert(sizeof(Args) <= 32764, "kernel parameter block");
+template <int N>
+struct ArgsOf : Settings {
+  Item it[N];
+};
+static_assert(sizeof(ArgsOf<kMost>) <= 32764, "kernel parameter block");
 
 // N elements from the `left` of a row that are left (zeros past them), and back.
 template <Elem E, int N>
@@ -157,32 +164,26 @@ __device__ __forceinline__ float power(uint32_t biased) { return __uint_as_float
 constexpr uint32_t kScaleDirect = 133;
 
 // Four codes of m: the instruction gives them in fp16, which holds them, and NaN with them.
-__device__ __forceinline__ void decode_m4(uint32_t w, float step, float* v) {
+__device__ __forceinline__ void decode_m4(uint32_t w, float step, F2* v) {
   uint32_t a, b;
   asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}"
       : "=r"(a), "=r"(b)
       : "r"(w));
   const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
-  v[0] = x.x * step, v[1] = x.y * step, v[2] = y.x * step, v[3] = y.y * step;
+  v[0] = f2(x.x, x.y) * f2(step), v[1] = f2(y.x, y.y) * f2(step);
 }
 // Whether a byte of w is zero.
 __device__ __forceinline__ bool zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
 // Four codes of u: a code's bits at the place of a float's are its value times 2^-120, subnormals among them.
-__device__ __forceinline__ void decode_u4(uint32_t w, uint32_t s, float* v) {
+__device__ __forceinline__ void decode_u4(uint32_t w, uint32_t s, F2* v) {
   constexpr uint32_t kMask = 0xffu << 19;
-  const float k = power(s <= kScaleDirect ? s + 120u : 247u);
-  v[0] = __uint_as_float((w << 19) & kMask) * k;
-  v[1] = __uint_as_float((w << 11) & kMask) * k;
-  v[2] = __uint_as_float((w << 3) & kMask) * k;
-  v[3] = __uint_as_float((w >> 5) & kMask) * k;
-  if (s > kScaleDirect) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= power(s);
-  }
+  const F2 k = f2(power(s <= kScaleDirect ? s + 120u : 247u));
+  v[0] = f2(__uint_as_float((w << 19) & kMask), __uint_as_float((w << 11) & kMask)) * k;
+  v[1] = f2(__uint_as_float((w << 3) & kMask), __uint_as_float((w >> 5) & kMask)) * k;
+  if (s > kScaleDirect) v[0] = v[0] * f2(power(s)), v[1] = v[1] * f2(power(s));
   if (zero_byte(~w)) {  // the last code, a NaN
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (((w >> (8 * i)) & 0xffu) == 0xffu) v[i] = __uint_as_float(0x7fc00000u);
+    auto nan = [&](int i, float x) { return ((w >> (8 * i)) & 0xffu) == 0xffu ? __uint_as_float(0x7fc00000u) : x; };
+    v[0] = f2(nan(0, lo(v[0])), nan(1, hi(v[0]))), v[1] = f2(nan(2, lo(v[1])), nan(3, hi(v[1])));
   }
 }
 // The scale byte from the bits of the largest finite magnitude (largest codes 1.75 2^8 and 1.875 2^8).
@@ -191,18 +192,25 @@ __device__ __forceinline__ uint32_t state_scale(uint32_t top_bits) {
   constexpr uint32_t kAbove = BITS == kMBits ? 0x1fffffu : 0x0fffffu;
   return uint32_t(max(int((top_bits + kAbove) >> 23) - 8, 1));
 }
-// The code of a magnitude, in bits 16 on: x 2^(127 - s) 2^-120 has the code at the head of a float's bits (products towards
-// zero: what is under 2^-149 is dropped), and the 16 bits behind it decide with 16 random ones whether it is rounded up.
+// The code of a magnitude, in bits 16 to 23: x 2^(127 - s) 2^-120 has the code at the head of a float's bits, behind the sign (products
+// towards zero: what is under 2^-149 is dropped), and the 16 bits behind it decide with 16 random ones whether it is rounded up.
 template <int BITS>
-__device__ __forceinline__ uint32_t encode(float x, float k, uint32_t random) {
-  return (__float_as_uint(__fmul_rz(fabsf(x), k)) >> (7 - BITS)) + random;
+__device__ __forceinline__ uint32_t encode_bits(float scaled, uint32_t random) {
+  return (__float_as_uint(scaled) >> (7 - BITS)) + random;
+}
+template <int BITS>
+__device__ __forceinline__ void encode_pair(F2 x, float k, uint32_t r0, uint32_t r1, uint32_t& c0, uint32_t& c1) {
+  F2 t;
+  asm("mul.rz.f32x2 %0, %1, %2;" : "=l"(t.v) : "l"(x.v), "l"(f2(k).v));
+  c0 = encode_bits<BITS>(lo(t), r0), c1 = encode_bits<BITS>(hi(t), r1);
 }
 // Any scale, and what is not finite.
 template <int BITS>
 __device__ __forceinline__ uint32_t encode_any(float x, uint32_t s, uint32_t random) {
   if (abs_bits(x) >= kInfBits) return (BITS == kMBits ? 0x7fu : 0xffu) << 16;
+  if (s <= kScaleDirect) return encode_bits<BITS>(__fmul_rz(x, power(134u - s)), random);
   // (2^-100 first: of what that rounds, nothing reaches a code of a block whose largest is over 2^14)
-  return s <= kScaleDirect ? encode<BITS>(x, power(134u - s), random) : encode<BITS>(x * power(27u), __uint_as_float(s <= 233u ? (234u - s) << 23 : 1u << (256u - s)), random);
+  return encode_bits<BITS>(__fmul_rz(x * power(27u), __uint_as_float(s <= 233u ? (234u - s) << 23 : 1u << (256u - s))), random);
 }
 __device__ __forceinline__ uint32_t finite_bits(float x) {
   const uint32_t b = abs_bits(x);
@@ -213,10 +221,10 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Of the eight lanes of a block.
+// Of the lanes of a block.
 __device__ __forceinline__ uint32_t block_max(uint32_t v) {
 #pragma unroll
-  for (int m = 1; m < 8; m *= 2) v = max(v, __shfl_xor_sync(0xffffffffu, v, m));
+  for (int m = 1; m < kBlock / kEach8; m *= 2) v = max(v, __shfl_xor_sync(0xffffffffu, v, m));
   return v;
 }
 // Byte k of each of four words.
@@ -226,22 +234,58 @@ __device__ __forceinline__ uint32_t pack_byte(uint32_t a, uint32_t b, uint32_t c
   return __byte_perm(__byte_perm(a, b, kPick), __byte_perm(c, d, kPick), 0x5410);
 }
 
-// One element's step; u is the root of the new v.  (adamw_elem, operation for operation.)
-__device__ __forceinline__ void step_elem(float& p, float g, float& m, float& v, float& u, const AdamW& o) {
-  p = __fmul_rn(p, o.decay);
+// One element's moments, then its parameter from them; u is the root of the new v.  (adamw_elem, operation for operation.)
+__device__ __forceinline__ void moments_elem(float g, float& m, float& v, const AdamW& o) {
   m = __fadd_rn(__fmul_rn(o.b1, m), __fmul_rn(o.omb1, g));
   v = __fadd_rn(__fmul_rn(o.b2, v), __fmul_rn(o.omb2, __fmul_rn(g, g)));
+}
+__device__ __forceinline__ float step_elem(float p, float m, float v, float& u, const AdamW& o) {
   u = __fsqrt_rn(v);
-  p = __fsub_rn(p, __fdiv_rn(__fmul_rn(o.step, m), __fadd_rn(__fmul_rn(u, o.r), o.eps)));
+  return __fsub_rn(__fmul_rn(p, o.decay), __fdiv_rn(__fmul_rn(o.step, m), __fadd_rn(__fmul_rn(u, o.r), o.eps)));
+}
+// The same for two elements side by side in packed instructions.  A packed product that a packed sum follows may be fused with
+// it; so the sums are multiplications by 1 and additions, fused by themselves, which round as the addition does.
+__device__ __forceinline__ F2 add2(F2 x, F2 y, const Settings& a) { return vfma(x, f2(a.one), y); }
+__device__ __forceinline__ void moments_pair(F2 g, F2& m, F2& v, const Settings& a) {
+  const AdamW& o = a.opt;
+  m = add2(f2(o.b1) * m, f2(o.omb1) * g, a);
+  v = add2(f2(o.b2) * v, f2(o.omb2) * (g * g), a);
+}
+// The parameters, without a branch for what is far out of range.  Root and quotient by Goldschmidt's and Newton's iterations from
+// the hardware's reciprocals, each with a last correction by its remainder, which a fused multiply-add gives exactly
+// (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  All roots to 2^31
+// round as the instruction does, and so did 2^34 quotients of random significands.  For v <= 2^62, |m| <= 2^62, eps >= 2^-40 and
+// steps of at most 2^20 (Args::plain); v comes from where it may be subnormal by 2^64; a quotient of a step m under 2^-102, whose
+// remainder may not be exact, may be a bit off.
+constexpr float kQuickMost = 4611686018427387904.0f;  // 2^62
+__device__ __forceinline__ F2 quick_pair(F2 p, F2 m, F2 v, F2& u, const Settings& a) {
+  const AdamW& o = a.opt;
+  const F2 w = v * f2(18446744073709551616.0f), minus = f2(-1.0f);
+  float y0, y1;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(lo(w)));
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(hi(w)));
+  F2 x = w * f2(y0, y1), h = f2(y0, y1) * f2(-0.5f);  // (the root, and minus half its reciprocal)
+  const F2 e = vfma(h, x, f2(0.5f));
+  x = vfma(x, e, x), h = vfma(h, e, h);
+  x = vfma(vfma(x, x, w * minus), h, x);
+  x = x * f2(2.3283064365386963e-10f);  // 2^-32
+  u = f2(lo(v) > 0.0f ? lo(x) : 0.0f, hi(v) > 0.0f ? hi(x) : 0.0f);
+  const F2 d = add2(u * f2(o.r), f2(o.eps), a), n = f2(o.step) * m, md = d * minus;
+  F2 r = f2(rcp_approx(lo(d)), rcp_approx(hi(d)));
+  r = vfma(r, vfma(md, r, f2(1.0f)), r);
+  F2 q = n * r;
+  q = vfma(vfma(md, q, n), r, q);
+  return vfma(q, f2(-a.one), p * f2(o.decay));
 }
 
-// The range of tiles of this CTA, and the item of its first.
+// The range of tiles of walker `i` of `n`, a CTA or a warp, and the item of its first.
 struct Walk {
   int64_t tile, end;
   int item;
-  __device__ __forceinline__ explicit Walk(const Args& a) {
-    tile = int64_t(blockIdx.x) * a.tiles / gridDim.x;
-    end = int64_t(blockIdx.x + 1) * a.tiles / gridDim.x;
+  template <class Args>
+  __device__ __forceinline__ explicit Walk(const Args& a, int64_t i = blockIdx.x, int64_t n = gridDim.x) {
+    tile = i * a.tiles / n;
+    end = (i + 1) * a.tiles / n;
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -252,7 +296,8 @@ struct Walk {
   }
 };
 
-__global__ void __launch_bounds__(kThreads) roi_adamw_step_kernel(const __grid_constant__ Args a) {
+template <class Args>
+__global__ void __launch_bounds__(kThreads, kCtas32) roi_adamw_step_kernel(const __grid_constant__ Args a) {
   pdl_begin(a.wait);
   const float scale = a.scale != nullptr ? __ldg(a.scale) : 1.0f;
   for (Walk w(a); w.tile < w.end; ++w.tile) {
@@ -267,7 +312,10 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_step_kernel(const __grid_c
     load_floats(static_cast<const float*>(it.b) + e, left, sectors, v);
     load_any(it.g, it.grad, e, left, sectors, g);
 #pragma unroll
-    for (int i = 0; i < kEach32; ++i) step_elem(p[i], a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v[i], u, a.opt);
+    for (int i = 0; i < kEach32; ++i) {
+      moments_elem(a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v[i], a.opt);
+      p[i] = step_elem(p[i], m[i], v[i], u, a.opt);
+    }
     store_floats(it.p + e, left, sectors, p);
     store_floats(static_cast<float*>(it.a) + e, left, sectors, m);
     store_floats(static_cast<float*>(it.b) + e, left, sectors, v);
@@ -276,7 +324,7 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_step_kernel(const __grid_c
 }
 
 // The words of elements 4 q on.
-__device__ __forceinline__ uint4 words_of(const Args& a, uint64_t q, uint32_t id) {
+__device__ __forceinline__ uint4 words_of(const Settings& a, uint64_t q, uint32_t id) {
   uint4 c = make_uint4(uint32_t(q), uint32_t(q >> 32), a.step, id);
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
@@ -286,7 +334,13 @@ __device__ __forceinline__ uint4 words_of(const Args& a, uint64_t q, uint32_t id
   return c;
 }
 
-__global__ void __launch_bounds__(kThreads) roi_adamw_step8_kernel(const __grid_constant__ Args a) {
+// The step with moments in 8 bits: 66 instructions an element (141 element by element, with branches around each root and quotient).
+// Seven CTAs an SM spill some words: a 7B-shaped block, fp32 gradients, states read back after it, with four to eight CTAs
+// 1031, 975, 1005, 961, 981 us.  As fast or slower: the next tile loaded into registers while one is encoded (950), by bulk copies into
+// shared memory (1054), prefetched into L2 (975), eight elements a thread (1073), pointers that move along a tensor (980).
+template <class Args>
+__global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const __grid_constant__ Args a) {
+  constexpr int kLanes = kBlock / kEach8, kPairs = kEach8 / 2, kWords = kEach8 / 4;  // lanes of a block; a lane's pairs, words of codes
   pdl_begin(a.wait);
   const float scale = a.scale != nullptr ? __ldg(a.scale) : 1.0f;
   const int lane = threadIdx.x & 31;
@@ -294,93 +348,122 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_step8_kernel(const __grid_
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
     const int64_t e = (w.tile - it.tile0) * (kThreads * kEach8) + kEach8 * threadIdx.x, left = it.n - e;
-    if (left + kEach8 * lane <= 0) continue;  // (a warp has four blocks)
-    const bool there = left + kEach8 * (lane & 7) > 0, sectors = it.sectors;
+    if (left + kEach8 * lane <= 0) continue;  // (a warp has whole blocks)
+    const bool there = left + kEach8 * (lane & (kLanes - 1)) > 0;  // whether its block has elements of the tensor
+    float p[kEach8], g[kEach8];
+    union {
+      uint4 c;
+      uint32_t w[kWords];
+    } mw, uw;
+    mw.c = uw.c = make_uint4(0u, 0u, 0u, 0u);
+    uint32_t sw = 0;
+    load_floats(it.p + e, left, it.sectors, p);
+    load_any(it.g, it.grad, e, left, it.sectors, g);
     uint4* mc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.a) + e);
     uint4* uc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.b) + e);
     uint16_t* sc = reinterpret_cast<uint16_t*>(it.scales) + (e >> 7);
-    float p[16], g[16], m[16], u[16];
-    uint4 mw = make_uint4(0u, 0u, 0u, 0u), uw = mw;
-    uint32_t sw = 0;
-    load_floats(it.p + e, left, sectors, p);
-    load_any(it.g, it.grad, e, left, sectors, g);
-    if (there) mw = *mc, uw = *uc, sw = *sc;
+    if (there) mw.c = *mc, uw.c = *uc, sw = *sc;
     const float m_step = power(state_byte(sw & 0xffu));
     const uint32_t u_byte = state_byte(sw >> 8);
-    decode_m4(mw.x, m_step, m), decode_m4(mw.y, m_step, m + 4), decode_m4(mw.z, m_step, m + 8), decode_m4(mw.w, m_step, m + 12);
-    decode_u4(uw.x, u_byte, u), decode_u4(uw.y, u_byte, u + 4), decode_u4(uw.z, u_byte, u + 8), decode_u4(uw.w, u_byte, u + 12);
-    float m_top = 0.0f, u_top = 0.0f;
+    F2 m[kPairs], u[kPairs];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float v = __fmul_rn(u[i], u[i]);
-      step_elem(p[i], a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v, u[i], a.opt);
-    }
-    store_floats(it.p + e, left, sectors, p);
-    if (it.copy != nullptr) store_any(it.copy, it.copied, e, left, sectors, p);
-    if (left < 16) {
+    for (int j = 0; j < kWords; ++j) decode_m4(mw.w[j], m_step, m + 2 * j), decode_u4(uw.w[j], u_byte, u + 2 * j);
+    // the moments, u for now v
 #pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (i >= left) m[i] = 0.0f, u[i] = 0.0f;  // (padding's codes are 0)
+    for (int i = 0; i < kPairs; ++i) {
+      u[i] = u[i] * u[i];
+      const F2 x = f2(g[2 * i], g[2 * i + 1]);
+      moments_pair(a.scale != nullptr ? x * f2(scale) : x, m[i], u[i], a);
     }
+    if (left < kEach8) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      m_top = max3_nan(m_top, fabsf(m[i]), fabsf(m[i + 1]));
-      u_top = max3_nan(u_top, u[i], u[i + 1]);
+      for (int i = 0; i < kPairs; ++i) {  // (padding's codes are 0)
+        m[i] = f2(2 * i < left ? lo(m[i]) : 0.0f, 2 * i + 1 < left ? hi(m[i]) : 0.0f);
+        u[i] = f2(2 * i < left ? lo(u[i]) : 0.0f, 2 * i + 1 < left ? hi(u[i]) : 0.0f);
+      }
     }
-    // (a NaN's bits are above an infinity's)
-    uint32_t m_bits = block_max(abs_bits(m_top)), u_bits = block_max(abs_bits(u_top));
+    float m_top = 0.0f, v_top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      m_top = max3_nan(m_top, fabsf(lo(m[i])), fabsf(hi(m[i])));
+      v_top = max3_nan(v_top, lo(u[i]), hi(u[i]));
+    }
+    const bool quick = a.plain && m_top <= kQuickMost && v_top <= kQuickMost;
+    if (__all_sync(0xffffffffu, quick)) {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const F2 x = quick_pair(f2(p[2 * i], p[2 * i + 1]), m[i], u[i], u[i], a);
+        p[2 * i] = lo(x), p[2 * i + 1] = hi(x);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        float u0, u1;
+        p[2 * i] = step_elem(p[2 * i], lo(m[i]), lo(u[i]), u0, a.opt);
+        p[2 * i + 1] = step_elem(p[2 * i + 1], hi(m[i]), hi(u[i]), u1, a.opt);
+        u[i] = f2(u0, u1);
+      }
+    }
+    store_floats(it.p + e, left, it.sectors, p);
+    if (it.copy != nullptr) store_any(it.copy, it.copied, e, left, it.sectors, p);
+    // (a NaN's bits are above an infinity's; the largest u is the root of the largest v)
+    uint32_t m_bits = block_max(abs_bits(m_top)), u_bits = block_max(abs_bits(__fsqrt_rn(v_top)));
     uint32_t ms = state_scale<kMBits>(m_bits), us = state_scale<kUBits>(u_bits);
     const bool direct = max(m_bits, u_bits) < kInfBits && max(ms, us) <= kScaleDirect;
-    uint32_t mo[4], uo[4];
     if (__all_sync(0xffffffffu, direct)) {
       const float mk = power(134u - ms), uk = power(134u - us);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint4 r = words_of(a, uint64_t(e >> 2) + q, it.id);
-        const float* x = m + 4 * q;
-        const float* y = u + 4 * q;
-        mo[q] = pack_byte<2>(encode<kMBits>(x[0], mk, r.x & 0xffffu), encode<kMBits>(x[1], mk, r.y & 0xffffu),
-                             encode<kMBits>(x[2], mk, r.z & 0xffffu), encode<kMBits>(x[3], mk, r.w & 0xffffu));
-        uo[q] = pack_byte<2>(encode<kUBits>(y[0], uk, r.x >> 16), encode<kUBits>(y[1], uk, r.y >> 16), encode<kUBits>(y[2], uk, r.z >> 16),
-                             encode<kUBits>(y[3], uk, r.w >> 16));
+      for (int q = 0; q < kWords; ++q) {
+        const uint4 r = words_of(a, (uint64_t(e) >> 2) + q, it.id);
+        uint32_t c[4], d[4];
+        encode_pair<kMBits>(m[2 * q], mk, r.x & 0xffffu, r.y & 0xffffu, c[0], c[1]);
+        encode_pair<kMBits>(m[2 * q + 1], mk, r.z & 0xffffu, r.w & 0xffffu, c[2], c[3]);
+        encode_pair<kUBits>(u[2 * q], uk, r.x >> 16, r.y >> 16, d[0], d[1]);
+        encode_pair<kUBits>(u[2 * q + 1], uk, r.z >> 16, r.w >> 16, d[2], d[3]);
+        mw.w[q] = pack_byte<2>(c[0], c[1], c[2], c[3]);
+        uw.w[q] = pack_byte<2>(d[0], d[1], d[2], d[3]);
       }
     } else {
       m_bits = u_bits = 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m_bits = max(m_bits, finite_bits(m[i])), u_bits = max(u_bits, finite_bits(u[i]));
+      for (int i = 0; i < kPairs; ++i) {
+        m_bits = max(m_bits, max(finite_bits(lo(m[i])), finite_bits(hi(m[i]))));
+        u_bits = max(u_bits, max(finite_bits(lo(u[i])), finite_bits(hi(u[i]))));
+      }
       ms = state_scale<kMBits>(block_max(m_bits)), us = state_scale<kUBits>(block_max(u_bits));
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint4 r = words_of(a, uint64_t(e >> 2) + q, it.id);
-        const float* x = m + 4 * q;
-        const float* y = u + 4 * q;
-        mo[q] = pack_byte<2>(encode_any<kMBits>(x[0], ms, r.x & 0xffffu), encode_any<kMBits>(x[1], ms, r.y & 0xffffu),
-                             encode_any<kMBits>(x[2], ms, r.z & 0xffffu), encode_any<kMBits>(x[3], ms, r.w & 0xffffu));
-        uo[q] = pack_byte<2>(encode_any<kUBits>(y[0], us, r.x >> 16), encode_any<kUBits>(y[1], us, r.y >> 16),
-                             encode_any<kUBits>(y[2], us, r.z >> 16), encode_any<kUBits>(y[3], us, r.w >> 16));
+      for (int q = 0; q < kWords; ++q) {
+        const uint4 r = words_of(a, (uint64_t(e) >> 2) + q, it.id);
+        const F2 *x = m + 2 * q, *y = u + 2 * q;
+        mw.w[q] = pack_byte<2>(encode_any<kMBits>(lo(x[0]), ms, r.x & 0xffffu), encode_any<kMBits>(hi(x[0]), ms, r.y & 0xffffu),
+                               encode_any<kMBits>(lo(x[1]), ms, r.z & 0xffffu), encode_any<kMBits>(hi(x[1]), ms, r.w & 0xffffu));
+        uw.w[q] = pack_byte<2>(encode_any<kUBits>(lo(y[0]), us, r.x >> 16), encode_any<kUBits>(hi(y[0]), us, r.y >> 16),
+                               encode_any<kUBits>(lo(y[1]), us, r.z >> 16), encode_any<kUBits>(hi(y[1]), us, r.w >> 16));
       }
     }
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const float* x = m + 4 * q;
-      mo[q] |= pack_byte<3>(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])) & 0x80808080u;
-      if (zero_byte(uo[q])) {
+    for (int q = 0; q < kWords; ++q) {
+      const F2 *x = m + 2 * q, *y = u + 2 * q;
+      mw.w[q] |= pack_byte<3>(__float_as_uint(lo(x[0])), __float_as_uint(hi(x[0])), __float_as_uint(lo(x[1])), __float_as_uint(hi(x[1]))) &
+                 0x80808080u;
+      const uint32_t codes = uw.w[q];
+      if (zero_byte(codes)) {
         // what is not zero stays so: a step divides by it
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (((uo[q] >> (8 * i)) & 0xffu) == 0u && u[4 * q + i] > 0.0f) uo[q] |= 1u << (8 * i);
+        auto least = [&](int i, float v) { return ((codes >> (8 * i)) & 0xffu) == 0u && v > 0.0f ? 1u << (8 * i) : 0u; };
+        uw.w[q] |= least(0, lo(y[0])) | least(1, hi(y[0])) | least(2, lo(y[1])) | least(3, hi(y[1]));
       }
     }
     if (there) {
-      *mc = make_uint4(mo[0], mo[1], mo[2], mo[3]);
-      *uc = make_uint4(uo[0], uo[1], uo[2], uo[3]);
-      if ((lane & 7) == 0) *sc = uint16_t(ms | us << 8);
+      *mc = mw.c;
+      *uc = uw.c;
+      if ((lane & (kLanes - 1)) == 0) *sc = uint16_t(ms | us << 8);
     }
   }
 }
 
 // What states in 8 bits stand for.  (Items: p and copy are where m and u go, `grad` their type.)
-__global__ void __launch_bounds__(kThreads) roi_adamw_state8_load_kernel(const __grid_constant__ Args a) {
+template <class Args>
+__global__ void __launch_bounds__(kThreads, kCtasLoad) roi_adamw_state8_load_kernel(const __grid_constant__ Args a) {
   pdl_begin(a.wait);
   for (Walk w(a); w.tile < w.end; ++w.tile) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
@@ -392,21 +475,27 @@ __global__ void __launch_bounds__(kThreads) roi_adamw_state8_load_kernel(const _
     const uint32_t sw = reinterpret_cast<const uint16_t*>(it.scales)[e >> 7];
     const float m_step = power(state_byte(sw & 0xffu));
     const uint32_t u_byte = state_byte(sw >> 8);
+    F2 x[8];
     float v[16];
+    auto store = [&](void* to) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[2 * i] = lo(x[i]), v[2 * i + 1] = hi(x[i]);
+      store_any(to, it.grad, e, left, it.sectors, v);
+    };
     if (it.p != nullptr) {
-      decode_m4(mw.x, m_step, v), decode_m4(mw.y, m_step, v + 4), decode_m4(mw.z, m_step, v + 8), decode_m4(mw.w, m_step, v + 12);
-      store_any(it.p, it.grad, e, left, it.sectors, v);
+      decode_m4(mw.x, m_step, x), decode_m4(mw.y, m_step, x + 2), decode_m4(mw.z, m_step, x + 4), decode_m4(mw.w, m_step, x + 6);
+      store(it.p);
     }
     if (it.copy != nullptr) {
-      decode_u4(uw.x, u_byte, v), decode_u4(uw.y, u_byte, v + 4), decode_u4(uw.z, u_byte, v + 8), decode_u4(uw.w, u_byte, v + 12);
-      store_any(it.copy, it.grad, e, left, it.sectors, v);
+      decode_u4(uw.x, u_byte, x), decode_u4(uw.y, u_byte, x + 2), decode_u4(uw.z, u_byte, x + 4), decode_u4(uw.w, u_byte, x + 6);
+      store(it.copy);
     }
   }
 }
 
-}  // namespace
-
-int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
+template <int N>
+int launch(const OptimCall& c, const OptimItem* items, int count) {
+  using Args = ArgsOf<N>;
   int launched = 0;
   bool wait = lone_pdl(c.stream);
   Args a;
@@ -417,14 +506,16 @@ int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
   }
   a.step = c.step;
   a.scale = c.scale;
-  const int tile = kThreads * (c.kind == OptimKind::kStep ? kEach32 : kEach8);
-  auto kern = c.kind == OptimKind::kStep ? roi_adamw_step_kernel
-              : c.kind == OptimKind::kStep8 ? roi_adamw_step8_kernel
-                                            : roi_adamw_state8_load_kernel;
+  a.one = 1.0f;
+  a.plain = c.opt.eps >= 9.094947017729282e-13f && c.opt.step <= 1048576.0f;  // 2^-40, 2^20
+  const int tile = c.kind == OptimKind::kStep ? kThreads * kEach32 : kThreads * kEach8;
+  auto kern = c.kind == OptimKind::kStep ? roi_adamw_step_kernel<Args>
+              : c.kind == OptimKind::kStep8 ? roi_adamw_step8_kernel<Args>
+                                            : roi_adamw_state8_load_kernel<Args>;
   for (int i = 0; i < count;) {
     a.count = 0;
     a.tiles = 0;
-    for (; i < count && a.count < kMost; ++i) {
+    for (; i < count && a.count < N; ++i) {
       const OptimItem& x = items[i];
       if (x.n == 0) continue;
       // (codes are accessed by 16 bytes)
@@ -436,12 +527,18 @@ int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
     }
     if (a.count == 0) break;
     a.wait = wait;
-    const int64_t cap = int64_t(sm_count()) * (c.kind == OptimKind::kStep ? 10 : c.kind == OptimKind::kStep8 ? 5 : 16);  // held at once
+    const int64_t cap = int64_t(sm_count()) * (c.kind == OptimKind::kStep ? kCtas32 : c.kind == OptimKind::kStep8 ? kCtas8 : kCtasLoad);
     if (launch_maybe_pdl(kern, int(a.tiles < cap ? a.tiles : cap), kThreads, 0, c.stream, wait, a) < 0) return -1;
     ++launched;
     wait = true;
   }
   return launched;
+}
+
+}  // namespace
+
+int launch_optim(const OptimCall& c, const OptimItem* items, int count) {
+  return count <= kFew ? launch<kFew>(c, items, count) : launch<kMost>(c, items, count);
 }
 
 }  // namespace roi
