@@ -8,7 +8,11 @@ goes), gate, up and their product.  The backward forms each layer's weight gradi
 checkpoint of its input, turns it into the logits' AdamW step, and closes with the norm's own
 backward.
 
-    python examples/masked_mlp_step.py [--shape qwen2.5-0.5b] [--tokens 2048] [--steps 20]
+With --fp8 the layers' products run in 8-bit floating point as well (the masked weight is copied once a
+step for both), and the logits' step is taken for all layers at once, from gradients that a data-parallel run
+would have reduced, with its moments in 8 bits.
+
+    python examples/masked_mlp_step.py [--shape qwen2.5-0.5b] [--tokens 2048] [--steps 20] [--fp8]
 """
 import argparse
 import os
@@ -45,11 +49,41 @@ class MaskedLinear:
         return dX
 
 
+class MaskedLinearFp8(MaskedLinear):
+    """The same with its products in 8-bit floating point; backward leaves the logits' gradient in dlogits."""
+
+    def __init__(self, rows, cols, tensor_id, seed, tokens):
+        super().__init__(rows, cols, tensor_id, seed)
+        self.m = self.v = None
+        self.moments = roi.new_adamw_state8(self.logits.numel())
+        self.dlogits = torch.empty_like(self.logits)
+        self.w8, self.in8, self.out8 = roi.new_fp8_weight(rows, cols), roi.new_fp8(tokens, cols), roi.new_fp8(tokens, rows)
+
+    def forward(self, X, step, tau):
+        self.state = roi.NoiseState(7, step, self.tensor_id, 1.0, 0)
+        roi.roi_mask_fwd_ex(self.logits, self.W, N, M, tau, self.state, self.Wm)
+        roi.roi_fp8_save_weight(self.Wm, *self.w8)
+        roi.roi_fp8_save(X, "e4m3", *self.in8)
+        Y = torch.empty(X.shape[0], self.W.shape[0], dtype=X.dtype, device="cuda")
+        roi.roi_fp8_linear_fwd(self.in8, "e4m3", self.w8, Y)
+        return Y
+
+    def backward(self, dY, x_checkpoint, tau, opt, workspace):
+        roi.roi_fp8_save(dY, "e5m2", *self.out8)
+        dX = torch.empty(dY.shape[0], self.W.shape[1], dtype=dY.dtype, device="cuda")
+        roi.roi_fp8_linear_dgrad(self.out8, "e5m2", self.w8, dX)
+        roi.roi_masked_linear_wgrad(dY, x_checkpoint, self.dWm, None, workspace)
+        roi.roi_mask_bwd(self.logits, self.W, self.state, N, M, self.dWm, tau, self.dlogits)
+        return dX
+
+
 class MaskedMLP:
-    def __init__(self, hidden, inter, tokens, seed=1000):
+    def __init__(self, hidden, inter, tokens, seed=1000, fp8=False):
         self.hidden, self.inter, self.tokens = hidden, inter, tokens
-        self.gate, self.up = MaskedLinear(inter, hidden, 4, seed + 4), MaskedLinear(inter, hidden, 5, seed + 5)
-        self.down = MaskedLinear(hidden, inter, 6, seed + 6)
+        make = (lambda *a: MaskedLinearFp8(*a, tokens)) if fp8 else MaskedLinear
+        self.gate, self.up = make(inter, hidden, 4, seed + 4), make(inter, hidden, 5, seed + 5)
+        self.down = make(hidden, inter, 6, seed + 6)
+        self.fp8 = fp8
         self.gamma = (1 + 0.1 * torch.randn(hidden, device="cuda")).to(torch.bfloat16)
         # what lives from the forward to the backward, and the steps' workspace
         self.x8, self.y8 = roi.new_checkpoint(tokens, hidden), roi.new_checkpoint(tokens, hidden)
@@ -85,6 +119,9 @@ class MaskedMLP:
         dy = self.gate.backward(dg, self.y8, tau, opt, self.workspace) + self.up.backward(du, self.y8, tau, opt, self.workspace)
         dx, dgamma = torch.empty_like(dy), torch.empty(self.hidden, device="cuda")
         roi.roi_norm_bwd(dy, self.x8, "rms", self.gamma, None, self.rstd, dx, dgamma, None, self.workspace)
+        if self.fp8:
+            # (a data-parallel run reduces the layers' dlogits here)
+            roi.roi_adamw_step8([(x.logits, x.dlogits, x.moments, None, x.tensor_id) for x in (self.gate, self.up, self.down)], opt, 7)
         return dx + d_out, dgamma
 
     def kept_bytes(self):
@@ -93,10 +130,10 @@ class MaskedMLP:
         return sum(t.numel() for q in pairs for t in q), 2 * self.tokens * (2 * self.hidden + 3 * self.inter)
 
 
-def train(hidden, inter, tokens, steps, lr=0.02, tau=0.5):
+def train(hidden, inter, tokens, steps, lr=0.02, tau=0.5, fp8=False):
     """The losses of `steps` steps on one batch."""
     torch.manual_seed(0)
-    block = MaskedMLP(hidden, inter, tokens)
+    block = MaskedMLP(hidden, inter, tokens, fp8=fp8)
     x = torch.randn(tokens, hidden, device="cuda").to(torch.bfloat16)
     target, losses = block.dense(x), []
     for step in range(steps):
@@ -114,9 +151,10 @@ def main():
     ap.add_argument("--shape", default="qwen2.5-0.5b", choices=sorted(WL.LAYER_SETS))
     ap.add_argument("--tokens", type=int, default=2048)
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--fp8", action="store_true", help="products in 8-bit floating point, AdamW's moments in 8 bits")
     a = ap.parse_args()
     s = WL.LAYER_SETS[a.shape]
-    block, losses = train(s.hidden, s.inter, a.tokens, a.steps)
+    block, losses = train(s.hidden, s.inter, a.tokens, a.steps, fp8=a.fp8)
     kept, plain = block.kept_bytes()
     print(f"{a.shape}-shaped MLP block, {a.tokens} tokens: activations kept {kept / 1e6:.1f} MB (bfloat16: {plain / 1e6:.1f} MB)")
     print("loss " + " ".join(f"{v:.4g}" for v in losses))

@@ -65,7 +65,8 @@ def decode(codes, scales, kind):
     v = np.where(field == 0, m, m + (1 << bits)) * np.exp2(np.maximum(field - 1, 0) - 6.0 - bits)
     v = v * np.exp2(np.clip(scales.astype(np.float64), 1, 247) - 127)[:, None]
     v = np.where(c == nan, np.nan, v)
-    return np.where(sign, -v, v).astype(F).reshape(-1)
+    with np.errstate(over="ignore"):
+        return np.where(sign, -v, v).astype(F).reshape(-1)
 
 
 def step8(p, g, state, k, seed, t, tensor_id, scale=None):

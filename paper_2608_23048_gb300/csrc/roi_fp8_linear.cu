@@ -29,7 +29,7 @@ constexpr int kScaleSlots = 4;                  // of four blocks' scales: 128 o
 constexpr uint32_t kScaleBytes = 512 + 1024;
 constexpr uint32_t kOffScales = kRingBytes, kOffBars = kOffScales + kScaleSlots * kScaleBytes;
 constexpr int kBars = 2 * kMaxStages + 2 * kScaleSlots + 2;
-constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 8;
+constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 40;
 static_assert(kSmem + 1024 <= 232448, "shared memory");
 
 struct LinearArgs {
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + kOffBars);
   uint64_t *full = bars, *empty = full + kMaxStages, *scale_full = empty + kMaxStages, *scale_empty = scale_full + kScaleSlots;
   uint64_t *done = scale_empty + kScaleSlots, *joined = done + 1;
-  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok
+  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok, [2 + r] whether CTA r of the cluster has sums
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int rank = a.splits > 1 ? int(cluster_rank()) : 0;
   const int tile = blockIdx.x / a.splits;
@@ -234,7 +234,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int each = (groups + a.splits - 1) / a.splits, mine = (groups - rank + a.splits - 1) / a.splits;
     float* own = reinterpret_cast<float*>(smem);
     const int place = 32 * warp + lane;
-    bool all = whole;
     for (int g = 0; whole && g < groups; ++g) {
       float v[16];
       read(g, v);
@@ -243,7 +242,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     fence_proxy_async_smem();
     if (tid == 0) mbar_arrive_expect_tx(joined, uint32_t((a.splits - 1) * mine) * kGroupBytes);
+    if (tid < a.splits) store_cluster(cluster_addr(misc + 2 + rank, uint32_t(tid)), whole ? 1u : 0u);
     cluster_sync();  // every CTA is done with its stages, and its sums lie there
+    int missing = 0;  // CTAs that gave up and send nothing
+    for (int r = 0; r < a.splits; ++r) missing += r != rank && misc[2 + r] == 0u ? 1 : 0;
+    if (tid == 0 && missing > 0 && mine > 0) mbar_complete_tx(joined, uint32_t(missing * mine) * kGroupBytes);
     if (warp == 0 && whole) {
       for (int g = lane; g < groups; g += 32) {
         const int to = g % a.splits;
@@ -252,8 +255,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         bulk_s2s(cluster_addr(smem + at, uint32_t(to)), smem + uint32_t(g) * kGroupBytes, kGroupBytes, cluster_addr(joined, uint32_t(to)));
       }
     }
-    if (all) all = agreed(mbar_wait_ring_cluster(joined, 0, lim));
-    if (!all && whole && lane == 0) atomicOr(a.status, kStatusTimeout);
+    const bool all = agreed(mbar_wait_ring_cluster(joined, 0, lim)) && whole && missing == 0;
+    if (!all) {
+      mbar_wait_bounded(joined, 0);  // what the others send has landed
+      if (lane == 0) atomicOr(a.status, kStatusTimeout);
+    }
     for (int g = rank; all && g < groups; g += a.splits) {
       float v[16];
 #pragma unroll

@@ -32,7 +32,7 @@ constexpr int kScaleSlots = 4;             // of four blocks' scales: 128 rows o
 constexpr uint32_t kScaleBytes = 512 + 1024;
 constexpr uint32_t kOffScales = kStages * kStageBytes, kOffBars = kOffScales + kScaleSlots * kScaleBytes;
 constexpr int kBars = 2 * kStages + 2 * kScaleSlots + 4;
-constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 8;
+constexpr uint32_t kOffMisc = kOffBars + kBars * 8, kSmem = kOffMisc + 24;
 static_assert(kSmem + 1024 <= 232448, "shared memory");
 constexpr uint32_t kTmemCols = 512, kTmemScales = 2 * kMaxN;
 
@@ -137,7 +137,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   // `full`, `scale_full` and `free` are the even CTA's, on which both arrive; the others each CTA's own
   uint64_t *full = bars, *empty = full + kStages, *scale_full = empty + kStages, *scale_empty = scale_full + kScaleSlots;
   uint64_t *sum = scale_empty + kScaleSlots, *free = sum + 2;
-  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);  // [0] TMEM base, [1] ok
+  // [0] TMEM base; [1] ok; blocks whose copies were sent off, and ok, of CTA 0 in [2] and [3], of CTA 1 in [4] and [5]
+  uint32_t* misc = reinterpret_cast<uint32_t*>(smem + kOffMisc);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank();
   const int g = blockIdx.x / 2;
@@ -320,19 +321,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   }
   if (!ok) misc[1] = 0u;
   __syncthreads();
-  if (misc[1] == 0u) {
-    // a wait gave up: MMAs end, and the copies that were sent off land, before it leaves (on the even CTA's barriers,
-    // where both CTAs' land; a stage that only one of them filled runs out of time)
-    if (warp == 0 && rank == 0)
-      for (int c = issued > kStages ? issued - kStages : 0; c < issued; ++c)
-        if (!mbar_wait_bounded(full + c % kStages, uint32_t(c / kStages) & 1u)) break;
+  tc_fence_after();
+  if (tid < 2) {  // (of warp 0, which sent the copies off)
+    const uint32_t at = cluster_addr(misc + 2 + 2 * rank, uint32_t(tid));
+    store_cluster(at, uint32_t(issued));
+    store_cluster(at + 4, misc[1]);
+  }
+  cluster_sync();
+  if ((misc[3] & misc[5]) == 0u) {
+    // a wait gave up: MMAs end, and the copies that were sent off land, before the pair leaves.  Both CTAs' land on
+    // the even CTA's barriers; a stage that only one of them filled is done without the other's bytes.
+    if (rank == 0 && tid == 0) {
+      const uint32_t bytes = kABytes + uint32_t(half) * kStep;
+      const int n0 = int(misc[2]), n1 = int(misc[4]), n = n0 > n1 ? n0 : n1;
+      for (int c = n > kStages ? n - kStages : 0; c < n; ++c) {
+        uint64_t* bar = full + c % kStages;
+        if (c >= n1) mbar_complete_tx(bar, bytes);
+        else if (c >= n0) mbar_arrive_expect_tx(bar, bytes);
+        mbar_wait_bounded(bar, uint32_t(c / kStages) & 1u);
+      }
+    }
     if (warp == 1 && committed > 0)
       mbar_wait_bounded(empty + (committed - 1) % kStages, uint32_t((committed - 1) / kStages) & 1u);
     if (tid == 0) atomicOr(a.status, kStatusTimeout);
     __syncthreads();
+    cluster_sync();
   }
-  tc_fence_after();
-  cluster_sync();
   if (warp == 0) tc_dealloc_pair(tmem, kTmemCols);
 }
 

@@ -300,6 +300,14 @@ __device__ __forceinline__ void bulk_s2s(uint32_t dst, const void* src_smem, uin
                "r"(smem_addr(src_smem)), "r"(bytes), "r"(bar)
                : "memory");
 }
+// A word into the shared memory of a CTA of the cluster (a cluster address).
+__device__ __forceinline__ void store_cluster(uint32_t at, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+}
+// Takes bytes that will not come off what a barrier of this CTA waits for.
+__device__ __forceinline__ void mbar_complete_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
 // A place in a ring of N, and the parity of the pass over it.
 template <int N>
 struct TcRing {
