@@ -22,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kEach32 = 8, kEach8 = 16, kBlock = 128;
-constexpr int kCtas32 = 10, kCtas8 = 7, kCtasLoad = 12;  // of an SM
+constexpr int kCtas32 = 10, kCtas8 = 5, kCtasLoad = 12;  // of an SM
 
 struct Item {
   float* p;
@@ -56,6 +56,13 @@ struct ArgsOf : Settings {
 };
 static_assert(sizeof(ArgsOf<kMost>) <= 32764, "kernel parameter block");
 
+// Whole sectors (memory that this kernel writes as well).
+__device__ __forceinline__ void load_sector(const void* p, uint32_t* w) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+               : "l"(p)
+               : "memory");
+}
 // N elements from the `left` of a row that are left (zeros past them), and back.
 template <Elem E, int N>
 __device__ __forceinline__ void load_words(const void* p, int64_t left, bool sectors, RowWords<E, N>& r) {
@@ -63,12 +70,7 @@ __device__ __forceinline__ void load_words(const void* p, int64_t left, bool sec
   constexpr int W = RowWords<E, N>::kWords;
   if (left >= N && W % 8 == 0 && sectors) {
 #pragma unroll
-    for (int i = 0; i < W / 8; ++i)
-      asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                   : "=r"(r.u[8 * i]), "=r"(r.u[8 * i + 1]), "=r"(r.u[8 * i + 2]), "=r"(r.u[8 * i + 3]), "=r"(r.u[8 * i + 4]),
-                     "=r"(r.u[8 * i + 5]), "=r"(r.u[8 * i + 6]), "=r"(r.u[8 * i + 7])
-                   : "l"(static_cast<const uint32_t*>(p) + 8 * i)
-                   : "memory");
+    for (int i = 0; i < W / 8; ++i) load_sector(static_cast<const uint32_t*>(p) + 8 * i, r.u + 8 * i);
   } else if (left >= N) {
 #pragma unroll
     for (int i = 0; i < W / 4; ++i) {
@@ -104,6 +106,13 @@ __device__ __forceinline__ void store_words(void* p, int64_t left, bool sectors,
     for (int i = 0; i < N; ++i)
       if (i < left) q[i] = r.at(i);
   }
+}
+template <Elem E, int N>
+__device__ __forceinline__ void load_sectors(const void* p, float (&v)[N]) {
+  RowWords<E, N> r;
+#pragma unroll
+  for (int i = 0; i < RowWords<E, N>::kWords / 8; ++i) load_sector(static_cast<const uint32_t*>(p) + 8 * i, r.u + 8 * i);
+  r.get(v);
 }
 template <int N>
 __device__ __forceinline__ void load_floats(const void* p, int64_t left, bool sectors, float (&v)[N]) {
@@ -172,8 +181,8 @@ __device__ __forceinline__ void decode_m4(uint32_t w, float step, F2* v) {
   const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&a)), y = __half22float2(*reinterpret_cast<const __half2*>(&b));
   v[0] = f2(x.x, x.y) * f2(step), v[1] = f2(y.x, y.y) * f2(step);
 }
-// Whether a byte of w is zero.
-__device__ __forceinline__ bool zero_byte(uint32_t w) { return ((w - 0x01010101u) & ~w & 0x80808080u) != 0u; }
+// Not zero where a byte of w is.
+__device__ __forceinline__ uint32_t zero_byte(uint32_t w) { return (w - 0x01010101u) & ~w & 0x80808080u; }
 // Four codes of u: a code's bits at the place of a float's are its value times 2^-120, subnormals among them.
 __device__ __forceinline__ void decode_u4(uint32_t w, uint32_t s, F2* v) {
   constexpr uint32_t kMask = 0xffu << 19;
@@ -181,9 +190,22 @@ __device__ __forceinline__ void decode_u4(uint32_t w, uint32_t s, F2* v) {
   v[0] = f2(__uint_as_float((w << 19) & kMask), __uint_as_float((w << 11) & kMask)) * k;
   v[1] = f2(__uint_as_float((w << 3) & kMask), __uint_as_float((w >> 5) & kMask)) * k;
   if (s > kScaleDirect) v[0] = v[0] * f2(power(s)), v[1] = v[1] * f2(power(s));
-  if (zero_byte(~w)) {  // the last code, a NaN
-    auto nan = [&](int i, float x) { return ((w >> (8 * i)) & 0xffu) == 0xffu ? __uint_as_float(0x7fc00000u) : x; };
-    v[0] = f2(nan(0, lo(v[0])), nan(1, hi(v[0]))), v[1] = f2(nan(2, lo(v[1])), nan(3, hi(v[1])));
+}
+// 16 codes of each: a lane's of a tile.
+__device__ __forceinline__ void decode_m(const uint32_t (&w)[4], float step, F2 (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) decode_m4(w[j], step, v + 2 * j);
+}
+__device__ __forceinline__ void decode_u(const uint32_t (&w)[4], uint32_t s, F2 (&v)[8]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) decode_u4(w[j], s, v + 2 * j);
+  if ((zero_byte(~w[0]) | zero_byte(~w[1]) | zero_byte(~w[2]) | zero_byte(~w[3])) != 0u) {
+    // the last code, a NaN
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      auto nan = [&](int k, float x) { return ((w[i / 2] >> (8 * k)) & 0xffu) == 0xffu ? __uint_as_float(0x7fc00000u) : x; };
+      v[i] = f2(nan(2 * (i & 1), lo(v[i])), nan(2 * (i & 1) + 1, hi(v[i])));
+    }
   }
 }
 // The scale byte from the bits of the largest finite magnitude (largest codes 1.75 2^8 and 1.875 2^8).
@@ -278,14 +300,13 @@ __device__ __forceinline__ F2 quick_pair(F2 p, F2 m, F2 v, F2& u, const Settings
   return vfma(q, f2(-a.one), p * f2(o.decay));
 }
 
-// The range of tiles of walker `i` of `n`, a CTA or a warp, and the item of its first.
+// The tiles of this CTA, every gridDim.x-th, and the item of its first.
 struct Walk {
-  int64_t tile, end;
+  int64_t tile;
   int item;
   template <class Args>
-  __device__ __forceinline__ explicit Walk(const Args& a, int64_t i = blockIdx.x, int64_t n = gridDim.x) {
-    tile = i * a.tiles / n;
-    end = (i + 1) * a.tiles / n;
+  __device__ __forceinline__ explicit Walk(const Args& a) {
+    tile = blockIdx.x;
     int lo = 0, hi = a.count - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
@@ -300,17 +321,25 @@ template <class Args>
 __global__ void __launch_bounds__(kThreads, kCtas32) roi_adamw_step_kernel(const __grid_constant__ Args a) {
   pdl_begin(a.wait);
   const float scale = a.scale != nullptr ? __ldg(a.scale) : 1.0f;
-  for (Walk w(a); w.tile < w.end; ++w.tile) {
+  for (Walk w(a); w.tile < a.tiles; w.tile += gridDim.x) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
     const int64_t e = (w.tile - it.tile0) * (kThreads * kEach32) + kEach32 * threadIdx.x, left = it.n - e;
     if (left <= 0) continue;
     const bool sectors = it.sectors;
     float p[kEach32], g[kEach32], m[kEach32], v[kEach32], u;
-    load_floats(it.p + e, left, sectors, p);
-    load_floats(static_cast<const float*>(it.a) + e, left, sectors, m);
-    load_floats(static_cast<const float*>(it.b) + e, left, sectors, v);
-    load_any(it.g, it.grad, e, left, sectors, g);
+    // (without a branch between the loads: where ways meet, the compiler waits for what is on its way)
+    if (sectors && left >= kEach32 && it.grad == uint8_t(Elem::kFp32)) {
+      load_sectors<Elem::kFp32>(it.p + e, p);
+      load_sectors<Elem::kFp32>(static_cast<const float*>(it.a) + e, m);
+      load_sectors<Elem::kFp32>(static_cast<const float*>(it.b) + e, v);
+      load_sectors<Elem::kFp32>(static_cast<const float*>(it.g) + e, g);
+    } else {
+      load_floats(it.p + e, left, sectors, p);
+      load_floats(static_cast<const float*>(it.a) + e, left, sectors, m);
+      load_floats(static_cast<const float*>(it.b) + e, left, sectors, v);
+      load_any(it.g, it.grad, e, left, sectors, g);
+    }
 #pragma unroll
     for (int i = 0; i < kEach32; ++i) {
       moments_elem(a.scale != nullptr ? __fmul_rn(g[i], scale) : g[i], m[i], v[i], a.opt);
@@ -344,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const
   pdl_begin(a.wait);
   const float scale = a.scale != nullptr ? __ldg(a.scale) : 1.0f;
   const int lane = threadIdx.x & 31;
-  for (Walk w(a); w.tile < w.end; ++w.tile) {
+  for (Walk w(a); w.tile < a.tiles; w.tile += gridDim.x) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
     const int64_t e = (w.tile - it.tile0) * (kThreads * kEach8) + kEach8 * threadIdx.x, left = it.n - e;
@@ -357,23 +386,34 @@ __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const
     } mw, uw;
     mw.c = uw.c = make_uint4(0u, 0u, 0u, 0u);
     uint32_t sw = 0;
-    load_floats(it.p + e, left, it.sectors, p);
-    load_any(it.g, it.grad, e, left, it.sectors, g);
     uint4* mc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.a) + e);
     uint4* uc = reinterpret_cast<uint4*>(static_cast<uint8_t*>(it.b) + e);
     uint16_t* sc = reinterpret_cast<uint16_t*>(it.scales) + (e >> 7);
-    if (there) mw.c = *mc, uw.c = *uc, sw = *sc;
+    // All loads of a way follow one another without a branch: where ways meet, the compiler waits for what is on its way.
+    const bool whole = it.sectors && left + kEach8 * lane >= kEach8 * 32;  // (of the warp)
+    if (whole && it.grad == uint8_t(Elem::kFp32)) {
+      mw.c = *mc, uw.c = *uc, sw = *sc;
+      load_sectors<Elem::kFp32>(it.p + e, p);
+      load_sectors<Elem::kFp32>(static_cast<const float*>(it.g) + e, g);
+    } else if (whole && it.grad == uint8_t(Elem::kBf16)) {
+      mw.c = *mc, uw.c = *uc, sw = *sc;
+      load_sectors<Elem::kFp32>(it.p + e, p);
+      load_sectors<Elem::kBf16>(static_cast<const uint16_t*>(it.g) + e, g);
+    } else {
+      if (there) mw.c = *mc, uw.c = *uc, sw = *sc;
+      load_floats(it.p + e, left, it.sectors, p);
+      load_any(it.g, it.grad, e, left, it.sectors, g);
+    }
     const float m_step = power(state_byte(sw & 0xffu));
     const uint32_t u_byte = state_byte(sw >> 8);
     F2 m[kPairs], u[kPairs];
-#pragma unroll
-    for (int j = 0; j < kWords; ++j) decode_m4(mw.w[j], m_step, m + 2 * j), decode_u4(uw.w[j], u_byte, u + 2 * j);
+    decode_m(mw.w, m_step, m);
+    decode_u(uw.w, u_byte, u);
     // the moments, u for now v
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
       u[i] = u[i] * u[i];
-      const F2 x = f2(g[2 * i], g[2 * i + 1]);
-      moments_pair(a.scale != nullptr ? x * f2(scale) : x, m[i], u[i], a);
+      moments_pair(f2(g[2 * i], g[2 * i + 1]) * f2(scale), m[i], u[i], a);  // (1 without a factor: the product is exact)
     }
     if (left < kEach8) {
 #pragma unroll
@@ -443,14 +483,17 @@ __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const
     }
 #pragma unroll
     for (int q = 0; q < kWords; ++q) {
-      const F2 *x = m + 2 * q, *y = u + 2 * q;
+      const F2* x = m + 2 * q;
       mw.w[q] |= pack_byte<3>(__float_as_uint(lo(x[0])), __float_as_uint(hi(x[0])), __float_as_uint(lo(x[1])), __float_as_uint(hi(x[1]))) &
                  0x80808080u;
-      const uint32_t codes = uw.w[q];
-      if (zero_byte(codes)) {
-        // what is not zero stays so: a step divides by it
-        auto least = [&](int i, float v) { return ((codes >> (8 * i)) & 0xffu) == 0u && v > 0.0f ? 1u << (8 * i) : 0u; };
-        uw.w[q] |= least(0, lo(y[0])) | least(1, hi(y[0])) | least(2, lo(y[1])) | least(3, hi(y[1]));
+    }
+    if ((zero_byte(uw.w[0]) | zero_byte(uw.w[1]) | zero_byte(uw.w[2]) | zero_byte(uw.w[3])) != 0u) {
+      // what is not zero stays so: a step divides by it
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const uint32_t codes = uw.w[i / 2];
+        auto least = [&](int k, float v) { return ((codes >> (8 * k)) & 0xffu) == 0u && v > 0.0f ? 1u << (8 * k) : 0u; };
+        uw.w[i / 2] |= least(2 * (i & 1), lo(u[i])) | least(2 * (i & 1) + 1, hi(u[i]));
       }
     }
     if (there) {
@@ -465,13 +508,14 @@ __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const
 template <class Args>
 __global__ void __launch_bounds__(kThreads, kCtasLoad) roi_adamw_state8_load_kernel(const __grid_constant__ Args a) {
   pdl_begin(a.wait);
-  for (Walk w(a); w.tile < w.end; ++w.tile) {
+  for (Walk w(a); w.tile < a.tiles; w.tile += gridDim.x) {
     while (w.item + 1 < a.count && a.it[w.item + 1].tile0 <= w.tile) ++w.item;
     const Item& it = a.it[w.item];
     const int64_t e = (w.tile - it.tile0) * (kThreads * kEach8) + kEach8 * threadIdx.x, left = it.n - e;
     if (left <= 0) continue;
-    const uint4 mw = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.a) + e);
-    const uint4 uw = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.b) + e);
+    const uint4 mq = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.a) + e);
+    const uint4 uq = *reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(it.b) + e);
+    const uint32_t mw[4] = {mq.x, mq.y, mq.z, mq.w}, uw[4] = {uq.x, uq.y, uq.z, uq.w};
     const uint32_t sw = reinterpret_cast<const uint16_t*>(it.scales)[e >> 7];
     const float m_step = power(state_byte(sw & 0xffu));
     const uint32_t u_byte = state_byte(sw >> 8);
@@ -483,11 +527,11 @@ __global__ void __launch_bounds__(kThreads, kCtasLoad) roi_adamw_state8_load_ker
       store_any(to, it.grad, e, left, it.sectors, v);
     };
     if (it.p != nullptr) {
-      decode_m4(mw.x, m_step, x), decode_m4(mw.y, m_step, x + 2), decode_m4(mw.z, m_step, x + 4), decode_m4(mw.w, m_step, x + 6);
+      decode_m(mw, m_step, x);
       store(it.p);
     }
     if (it.copy != nullptr) {
-      decode_u4(uw.x, u_byte, x), decode_u4(uw.y, u_byte, x + 2), decode_u4(uw.z, u_byte, x + 4), decode_u4(uw.w, u_byte, x + 6);
+      decode_u(uw, u_byte, x);
       store(it.copy);
     }
   }
