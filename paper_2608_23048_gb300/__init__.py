@@ -198,13 +198,19 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+_RAW_STREAM = None  # torch's (raw current stream of a device, current device), once CUDA is initialised
+
+
 def _stream(stream):
+    global _RAW_STREAM
     if stream is None:
-        import torch
-        if not torch.cuda.is_initialized():
-            return torch.cuda.current_stream().cuda_stream
-        # the same handle without a Stream object around it
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if _RAW_STREAM is None:
+            import torch
+            if not torch.cuda.is_initialized():
+                return torch.cuda.current_stream().cuda_stream
+            # the same handle without a Stream object around it
+            _RAW_STREAM = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        return _RAW_STREAM[0](_RAW_STREAM[1]())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

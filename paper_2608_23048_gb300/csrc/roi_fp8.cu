@@ -3,6 +3,9 @@
 // Bound by memory: b bytes an element are read and 129/128 written.  A thread takes 16 consecutive columns (one 16-byte
 // store of codes), so eight neighbouring lanes hold a block of a row and its largest magnitude takes three shuffles.  A
 // weight's block of 128 x 128 is a CTA's, four such pieces a thread, and its largest magnitude goes through shared memory.
+//
+// Measured (of 6.79 TB/s copied): 8192 x 18944 bf16 73 us (6.39 TB/s; 77 with two pieces a thread in flight), fp32 2048 x 18944 32 us
+// (6.15), 37 x 896 2.2 us; rows that start anywhere, 8192 x 18943 bf16, 97 us.  Weights: 18944 x 3584 32 us (6.46), 18944 x 3583 43 us.
 #include "roi_fp8.cuh"
 #include "roi_launch.h"
 
@@ -10,7 +13,6 @@ namespace roi {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnits = 2;  // pieces of 16 columns a thread has in flight
 
 struct SaveArgs {
   const void* x;
@@ -49,26 +51,21 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_kernel(SaveArgs a) {
   pdl_begin(a.wait);
   const T* x = static_cast<const T*>(a.x);
   const int64_t total = a.rows * a.pieces;
-  constexpr int kTile = kThreads * kUnits;
-  for (int64_t base = int64_t(blockIdx.x) * kTile; base < total; base += int64_t(gridDim.x) * kTile) {
+  for (int64_t base = int64_t(blockIdx.x) * kThreads; base < total; base += int64_t(gridDim.x) * kThreads) {
     const int64_t row0 = base / a.pieces, rem0 = base - row0 * a.pieces;
-    RowWords<E, 16> r[kUnits];
-    int64_t row[kUnits], j[kUnits];
+    RowWords<E, 16> r;
+    int64_t row, j;
+    walk(row0, rem0, threadIdx.x, a.pieces, row, j);
+    const T* p = x + row * a.ld + 16 * j;
+    if (row < a.rows && a.cols - 16 * j >= 16) {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      walk(row0, rem0, uint32_t(u * kThreads) + threadIdx.x, a.pieces, row[u], j[u]);
-      const T* p = x + row[u] * a.ld + 16 * j[u];
-      if (row[u] < a.rows && a.cols - 16 * j[u] >= 16) {
-#pragma unroll
-        for (int i = 0; i < kWords / 8; ++i) load32(reinterpret_cast<const uint4*>(p) + 2 * i, r[u].u + 8 * i);
-      } else if (row[u] < a.rows) {
-        r[u].load_elements(x + row[u] * a.ld, 16 * j[u], a.cols);
-      } else {
-        r[u].zero();
-      }
+      for (int i = 0; i < kWords / 8; ++i) load32(reinterpret_cast<const uint4*>(p) + 2 * i, r.u + 8 * i);
+    } else if (row < a.rows) {
+      r.load_elements(x + row * a.ld, 16 * j, a.cols);
+    } else {
+      r.zero();
     }
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) save_piece<F, E>(a, r[u], row[u], j[u]);
+    save_piece<F, E>(a, r, row, j);
   }
 }
 
@@ -77,21 +74,15 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_rows_kernel(SaveArgs a)
   using T = typename ElemType<E>::T;
   pdl_begin(a.wait);
   const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
-  const int64_t stride = int64_t(gridDim.x) * (kThreads / 32) * kUnits;
-  for (int64_t t = (int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5)) * kUnits; t < tasks; t += stride) {
-    Window<E, 16> x[kUnits];
-    int64_t row[kUnits], j[kUnits];
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      row_task(t + u, a.width, a.segments, row[u], j[u]);
-      x[u].load(static_cast<const T*>(a.x) + row[u] * a.ld, 16 * j[u], row[u] < a.rows ? a.cols : 0);
-    }
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      RowWords<E, 16> r;
-      x[u].get(r);
-      save_piece<F, E>(a, r, row[u], j[u]);
-    }
+  const int64_t stride = int64_t(gridDim.x) * (kThreads / 32);
+  for (int64_t t = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); t < tasks; t += stride) {
+    Window<E, 16> x;
+    int64_t row, j;
+    row_task(t, a.width, a.segments, row, j);
+    x.load(static_cast<const T*>(a.x) + row * a.ld, 16 * j, row < a.rows ? a.cols : 0);
+    RowWords<E, 16> r;
+    x.get(r);
+    save_piece<F, E>(a, r, row, j);
   }
 }
 
@@ -117,19 +108,19 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_weight_kernel(WeightArg
     const int64_t r0 = bm * 128 + (threadIdx.x >> 3), c = bn * 128 + 16 * (threadIdx.x & 7);
     RowWords<Elem::kBf16, 16> r[kPieces];
     if constexpr (ANYWHERE) {
-      Window<Elem::kBf16, 16> w[kPieces];  // (all on their way before the first is used)
+      Window<Elem::kBf16, 16> w[kPieces];
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) {
-        const int64_t row = r0 + 32 * i;
-        w[i].load(a.W + row * a.cols, c, row < a.rows ? a.cols : 0);
-      }
+      for (int i = 0; i < kPieces; ++i) w[i].load(a.W + (r0 + 32 * i) * a.cols, c, r0 + 32 * i < a.rows ? a.cols : 0);
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) w[i].get(r[i]);
+    } else if (r0 + 32 * (kPieces - 1) < a.rows && c + 16 <= a.cols) {
+      // (no branch between the loads: where ways meet, the compiler waits for what is on its way)
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) load32(a.W + (r0 + 32 * i) * a.cols + c, r[i].u);
     } else {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i) {
-        const int64_t row = r0 + 32 * i;
-        if (row < a.rows && c + 16 <= a.cols) load32(a.W + row * a.cols + c, r[i].u);
+        if (r0 + 32 * i < a.rows && c + 16 <= a.cols) load32(a.W + (r0 + 32 * i) * a.cols + c, r[i].u);
         else r[i].zero();  // (columns come in sixteens)
       }
     }
@@ -167,10 +158,10 @@ int save(const Fp8SaveCall& c) {
              lone_pdl(c.stream)};
   if (!in_sectors(c.x, c.ld, c.rows, elem_bytes<E>())) {
     const int64_t tasks = by_rows(a);
-    return launch(roi_fp8_save_rows_kernel<F, E>, a, (tasks + kThreads / 32 * kUnits - 1) / (kThreads / 32 * kUnits), c.stream);
+    return launch(roi_fp8_save_rows_kernel<F, E>, a, (tasks + kThreads / 32 - 1) / (kThreads / 32), c.stream);
   }
   const int64_t total = a.rows * a.pieces;
-  return launch(roi_fp8_save_kernel<F, E>, a, (total + kThreads * kUnits - 1) / (kThreads * kUnits), c.stream);
+  return launch(roi_fp8_save_kernel<F, E>, a, (total + kThreads - 1) / kThreads, c.stream);
 }
 
 template <Fp8 F>
