@@ -255,9 +255,9 @@ roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi
  * as roi_adamw_step does, from the unrounded moments, and rounds m and sqrt(v) up with the probability of what their
  * codes would drop (to the nearest, u could not follow a beta2 of 0.95 down): code = floor(|x| / step + r / 65536), r the low
  * (m) or high (u) half of the element's Philox word for (seed, opt->t, tensor_id), counters as for the mask's noise.
- * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.
- * Results are a pure function of the arguments: they do not depend on how elements are divided among calls' items,
- * except that blocks start with each item. */
+ * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.  The step's quotient
+ * may be a bit off roi_adamw_step's in its last place (none of 2^34 was).  Items that share (seed, t) need a
+ * tensor_id of their own each, as layers of the mask do. */
 typedef struct {
     float* param;
     const void* grad;
@@ -527,7 +527,9 @@ roi_status roi_fp8_save_weight(const roi_bf16* W, int64_t rows, int64_t cols, ui
 
 /* The layer's forward, Y[t, r] = sum_c x^[t, c] w^[r, c], and the gradient of its input,
  * dX[t, c] = sum_r dy^[t, r] w^[r, c], x^, w^, dy^ the values that the copies stand for.  Products are exact,
- * sums in fp32 on the tensor cores' block-scaled instructions, rounded once to dtype.
+ * sums in fp32 on the tensor cores' block-scaled instructions, rounded once to dtype.  Those drop the bits below a sum's
+ * last instead of rounding, 1.4e-6 of the result's norm over a width of 18944; for float32 results sums are made of pieces of
+ * at most 2048 columns, added with rounding (1.2e-7, where a float32 product has 2.1e-7).
  *  x_codes, x_scales, format    the copy of x [T, cols]
  *  dy_codes, dy_scales, format  the copy of dy [T, rows]
  *  w_codes, w_scales            the copy of the weight [rows, cols]

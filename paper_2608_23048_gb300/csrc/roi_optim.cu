@@ -9,9 +9,9 @@
 // The probability is compared in 16 bits, m's in the low and u's in the high half of the element's Philox word (counter
 // as the mask's noise: element / 4, step, tensor).  The parameters take the step from the moments before they are rounded.
 //
-// Bound by memory in 32 bits (28 bytes an element, fp32 gradients); in 8 (16 bytes) near the rate of its instructions too.
+// Bound by memory: 28 bytes an element in 32 bits (fp32 gradients; 6.5 TB/s of the 6.79 copied), 16 in 8.
 //
-// Tensors are cut into tiles that follow one another over all tensors; a CTA has a range of them.  A thread has 8
+// Tensors are cut into tiles that follow one another over all tensors; a CTA has every gridDim.x-th.  A thread has 8
 // consecutive elements of a tile, or 16 where the moments are in 8 bits: whole sectors of each array, and a block in eight
 // neighbouring lanes.
 #include "roi_launch.h"
@@ -37,7 +37,8 @@ struct Item {
   uint8_t grad, copied;  // roi_dtype
   bool sectors;          // every array starts on a sector
 };
-// Items a launch: a launch copies its arguments whole, so few have a form of their own.
+// Items a launch: a launch copies its arguments whole, so few have a form of their own (nine tensors, one call on the host:
+// 5.2 us with the arguments of 400, 4.3 with those of 24).
 constexpr int kMost = 400, kFew = 24;
 struct Settings {
   int count;
@@ -363,10 +364,12 @@ __device__ __forceinline__ uint4 words_of(const Settings& a, uint64_t q, uint32_
   return c;
 }
 
-// The step with moments in 8 bits: 66 instructions an element (141 element by element, with branches around each root and quotient).
-// Seven CTAs an SM spill some words: a 7B-shaped block, fp32 gradients, states read back after it, with four to eight CTAs
-// 1031, 975, 1005, 961, 981 us.  As fast or slower: the next tile loaded into registers while one is encoded (950), by bulk copies into
-// shared memory (1054), prefetched into L2 (975), eight elements a thread (1073), pointers that move along a tensor (980).
+// The step with moments in 8 bits.  64 instructions an element issue in 60 % of the cycles, at 5.4 TB/s; on the way (a 7B-shaped
+// block of 233 million elements, fp32 gradients, the states read back after it, us): element by element, four a thread 1884;
+// whole sectors, decoding and encoding by words 1067; roots and quotients without a branch 1001; packed arithmetic 975; a CTA's tiles
+// gridDim apart, and loads without a branch between them 896.  With four to seven CTAs an SM 923, 896, 902 (spills 80 bytes), 936
+// (320).  As fast or slower: the next tile by bulk copies into shared memory, prefetched into L2, or loaded into registers
+// while one is encoded; eight elements a thread; pointers that move along a tensor.
 template <class Args>
 __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const __grid_constant__ Args a) {
   constexpr int kLanes = kBlock / kEach8, kPairs = kEach8 / 2, kWords = kEach8 / 4;  // lanes of a block; a lane's pairs, words of codes
