@@ -149,6 +149,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   const uint32_t rank = cluster_rank();
   const int g = blockIdx.x / 2;
 
+  if (tid == 32) prefetch_tensor_map(&tm_a), prefetch_tensor_map(&tm_b);
   if (tid == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(full + s, 1);

@@ -300,6 +300,15 @@ __device__ __forceinline__ void bulk_s2s(uint32_t dst, const void* src_smem, uin
                "r"(smem_addr(src_smem)), "r"(bytes), "r"(bar)
                : "memory");
 }
+// The first copy by a tensor map need not wait for the map itself.
+__device__ __forceinline__ void prefetch_tensor_map(const void* tmap) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(tmap)) : "memory");
+}
+// A box of a tensor map on its way into L2.
+__device__ __forceinline__ void tma_prefetch_2d(const void* tmap, int x, int y) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y)
+               : "memory");
+}
 // A word into the shared memory of a CTA of the cluster (a cluster address).
 __device__ __forceinline__ void store_cluster(uint32_t at, uint32_t v) {
   asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
