@@ -4,8 +4,8 @@
 // store of codes), so eight neighbouring lanes hold a block of a row and its largest magnitude takes three shuffles.  A
 // weight's block of 128 x 128 is a CTA's, four such pieces a thread, and its largest magnitude goes through shared memory.
 //
-// Measured (of 6.79 TB/s copied): 8192 x 18944 bf16 73 us (6.39 TB/s; 77 with two pieces a thread in flight), fp32 2048 x 18944 32 us
-// (6.15), 37 x 896 2.2 us; rows that start anywhere, 8192 x 18943 bf16, 97 us.  Weights: 18944 x 3584 32 us (6.46), 18944 x 3583 43 us.
+// Measured (of 6.79 TB/s copied): 8192 x 18944 bf16 71 us (6.6 TB/s), fp32 2048 x 18944 30 us (6.6), 37 x 896 2.2 us; rows that
+// start anywhere, 8192 x 18943 bf16, 91 us.  Weights: 18944 x 3584 31 us (6.6), 18944 x 3583 43 us.
 #include "roi_fp8.cuh"
 #include "roi_launch.h"
 
@@ -148,7 +148,9 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_weight_kernel(WeightArg
 
 template <class Args>
 int launch(void (*kern)(Args), const Args& a, int64_t grid, cudaStream_t stream) {
-  const int64_t cap = int64_t(sm_count()) * 8;  // what an SM holds at once
+  // four times what an SM holds at once: tiles are taken nearly in their order (8192 x 18944 bf16: once 74 us, twice 72, four times 71,
+  // eight times 69, all 74; 8192 x 3584 15.6, 14.9, 14.9, 15.5, 15.5)
+  const int64_t cap = int64_t(sm_count()) * 32;
   return launch_maybe_pdl(kern, int(grid < cap ? grid : cap), kThreads, 0, stream, a.wait, a);
 }
 

@@ -9,7 +9,7 @@
 // The probability is compared in 16 bits, m's in the low and u's in the high half of the element's Philox word (counter
 // as the mask's noise: element / 4, step, tensor).  The parameters take the step from the moments before they are rounded.
 //
-// Bound by memory: 28 bytes an element in 32 bits (fp32 gradients; 6.5 TB/s of the 6.79 copied), 16 in 8.
+// Bound by memory: 28 bytes an element in 32 bits (fp32 gradients; 7.15 TB/s, where a copy has 6.79), 16 in 8 (6.0).
 //
 // Tensors are cut into tiles that follow one another over all tensors; a CTA has every gridDim.x-th.  A thread has 8
 // consecutive elements of a tile, or 16 where the moments are in 8 bits: whole sectors of each array, and a block in eight
@@ -23,6 +23,11 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kEach32 = 8, kEach8 = 16, kBlock = 128;
 constexpr int kCtas32 = 10, kCtas8 = 5, kCtasLoad = 12;  // of an SM
+// A launch has a CTA a tile, so that tiles are taken in their order: 912 us for a 7B-shaped block's step in 32 bits, 1019 where the CTAs
+// that an SM holds went over them, 992 and 959 with two and four times as many.  In 8 bits, where a CTA's start counts, four
+// times what is held (the block with the states read back: one, two, four, eight times and a CTA a tile 893, 864, 852, 844, 885 us;
+// eight 0.5B-shaped blocks 468, 457, 454, 467, 467).
+constexpr int kWaves8 = 4;
 
 struct Item {
   float* p;
@@ -364,12 +369,13 @@ __device__ __forceinline__ uint4 words_of(const Settings& a, uint64_t q, uint32_
   return c;
 }
 
-// The step with moments in 8 bits.  64 instructions an element issue in 60 % of the cycles, at 5.4 TB/s; on the way (a 7B-shaped
+// The step with moments in 8 bits.  64 instructions an element; on the way (a 7B-shaped
 // block of 233 million elements, fp32 gradients, the states read back after it, us): element by element, four a thread 1884;
 // whole sectors, decoding and encoding by words 1067; roots and quotients without a branch 1001; packed arithmetic 975; a CTA's tiles
-// gridDim apart, and loads without a branch between them 896.  With four to seven CTAs an SM 923, 896, 902 (spills 80 bytes), 936
-// (320).  As fast or slower: the next tile by bulk copies into shared memory, prefetched into L2, or loaded into registers
-// while one is encoded; eight elements a thread; pointers that move along a tensor.
+// gridDim apart, and loads without a branch between them 896; more CTAs than an SM holds 839.  Registers for four to seven CTAs an
+// SM: 878, 839, 846 (spills 80 bytes), 866 (320).  As fast or slower, before the last two: the next tile by bulk copies into shared
+// memory, prefetched into L2, or loaded into registers while one is encoded; eight elements a thread; pointers that move
+// along a tensor.
 template <class Args>
 __global__ void __launch_bounds__(kThreads, kCtas8) roi_adamw_step8_kernel(const __grid_constant__ Args a) {
   constexpr int kLanes = kBlock / kEach8, kPairs = kEach8 / 2, kWords = kEach8 / 4;  // lanes of a block; a lane's pairs, words of codes
@@ -574,8 +580,8 @@ int launch(const OptimCall& c, const OptimItem* items, int count) {
     }
     if (a.count == 0) break;
     a.wait = wait;
-    const int64_t cap = int64_t(sm_count()) * (c.kind == OptimKind::kStep ? kCtas32 : c.kind == OptimKind::kStep8 ? kCtas8 : kCtasLoad);
-    if (launch_maybe_pdl(kern, int(a.tiles < cap ? a.tiles : cap), kThreads, 0, c.stream, wait, a) < 0) return -1;
+    const int64_t most = c.kind == OptimKind::kStep8 ? int64_t(sm_count()) * kWaves8 * kCtas8 : int64_t(1) << 30;
+    if (launch_maybe_pdl(kern, int(a.tiles < most ? a.tiles : most), kThreads, 0, c.stream, wait, a) < 0) return -1;
     ++launched;
     wait = true;
   }
