@@ -11,8 +11,9 @@
 // fewer than the SMs, a range of its sum: the CTAs of a tile are a cluster, copy their sums into one another's shared memory and
 // add them in the order of the ranges, each for some of the tokens.  Many tokens go to roi_fp8_pair.cu.
 //
-// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 13.8 from memory; the rest is a call's start and end.  Ranges joined by bulk copies: 777 tokens of 1531 x 1001
-// 5.9 us, 7.1 in one range a tile, 46 where each sum was stored into the other CTAs' memory by itself; 37 of 128 x 896 4.3, 9.7.
+// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 13.7 from memory; the rest is a call's start and end.
+// Ranges joined by bulk copies: 777 tokens of 1531 x 1001 5.9 us, 7.1 in one range a tile, 46 where each sum was stored into the
+// other CTAs' memory by itself; 37 tokens of 128 x 896 4.3, 9.7 by stores.
 #include <atomic>
 
 #include "roi_fp8.cuh"
@@ -98,6 +99,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 0) tc_alloc(misc, a.tmem_cols);
   tc_fence_before();
   __syncthreads();
+  if (a.splits > 1) cluster_arrive();  // this CTA has started: the others may write into its memory
   tc_fence_after();
   const uint32_t tmem = misc[0], scales_at = tmem + a.tmem_cols - 32;
   pdl_begin(a.wait);
@@ -254,7 +256,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     fence_proxy_async_smem();
     if (tid == 0) mbar_arrive_expect_tx(joined, uint32_t((a.splits - 1) * mine) * kGroupBytes);
+    __syncwarp();
+    cluster_wait();  // (they have long started)
     if (tid < a.splits) store_cluster(cluster_addr(misc + 2 + rank, uint32_t(tid)), whole ? 1u : 0u);
+    __syncwarp();
     cluster_sync();  // every CTA is done with its stages, and its sums lie there
     int missing = 0;  // CTAs that gave up and send nothing
     for (int r = 0; r < a.splits; ++r) missing += r != rank && misc[2 + r] == 0u ? 1 : 0;

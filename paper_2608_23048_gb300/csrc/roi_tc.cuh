@@ -191,6 +191,9 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
 }
+// The two halves of cluster_sync, with other work between them.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 // One arrival on the mbarrier at `bar`'s place in the shared memory of CTA `rank` of the cluster.
 // Release at CTA scope, as an arrival without qualifiers has: what is handed over lies in this
 // CTA's own shared memory or TMEM and is read there by the tensor cores, behind the writers' proxy
