@@ -15,8 +15,8 @@
 // Bound by what an SM takes in (64 bytes a cycle) and by the clock under load.  8192 tokens, us (at twice the measured cuBLAS
 // bf16 rate, 3764 TFLOP/s, 296): 18944 x 3584 forward 305 (3645 TFLOP/s), 3584 x 18944 330, its input gradient 315, 331 to 344
 // for the gradient of 18944 inputs.  On the way: one CTA a tile 480; pairs 320; the weight as A in the gradient 395 -> 331
-// (as B, its tiles of 112 columns began between sectors); two warps for the scales 319 -> 305.  Five or six stages are alike,
-// four take 2 to 12 % more.
+// (as B, its tiles of 112 columns began between sectors); two warps for the scales 319 -> 305.  Six stages are as good but for
+// 2048 tokens of 3584 x 18944 in fp32 (100, 94 with seven); five take 1 to 2 % more, four 3 to 12 %.
 #include <atomic>
 #include <type_traits>
 
@@ -32,8 +32,8 @@ constexpr int kThreads = 384;
 constexpr int kSide = 256;                 // rows of A of a tile
 constexpr int kStep = 128;                 // of the sum a stage holds: a block
 constexpr int kMaxN = 224;
-constexpr int kStages = 6;
-constexpr uint32_t kABytes = 128 * kStep, kStageBytes = 2 * kABytes;
+constexpr int kStages = 7;
+constexpr uint32_t kABytes = 128 * kStep, kStageBytes = kABytes + kMaxN / 2 * kStep;
 constexpr int kScaleSlots = 4;             // of four blocks' scales: 128 rows of A, up to 256 of B
 constexpr uint32_t kScaleBytes = 512 + 1024;
 constexpr uint32_t kOffScales = kStages * kStageBytes, kOffBars = kOffScales + kScaleSlots * kScaleBytes;
@@ -381,7 +381,7 @@ int launch_of(Elem e, const CUtensorMap& tm_a, const CUtensorMap& tm_b, const Pa
 }
 
 // A block's stage brings an SM 128 rows of A and n / 2 of B, 64 bytes a cycle: 256 + n cycles, where its MMAs take 2 n.  Measured
-// a round of tiles (8192 tokens, 3584 x 18944), n = 128, 160, 192, 224: 40.1, 42.2, 46.1, 48.9 us, 0.10 us per 256 + n.
+// a round of tiles (8192 tokens, 3584 x 18944), n = 128, 160, 192, 224: 39.1, 42.0, 46.1, 48.9 us, 0.10 us per 256 + n.
 // What a tile, and the launch, cost besides is from a sweep over 1 to 4096 tokens of seven layers.
 constexpr int kTileCycles = 2000, kLaunchCycles = 4000;
 // Finds the n of the least time for tiles of `m` by n outputs; returns that time in cycles.
