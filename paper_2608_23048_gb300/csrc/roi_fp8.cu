@@ -5,7 +5,7 @@
 // weight's block of 128 x 128 is a CTA's, four such pieces a thread, and its largest magnitude goes through shared memory.
 //
 // Measured (of 6.79 TB/s copied): 8192 x 18944 bf16 71 us (6.6 TB/s), fp32 2048 x 18944 30 us (6.6), 37 x 896 2.2 us; rows that
-// start anywhere, 8192 x 18943 bf16, 91 us.  Weights: 18944 x 3584 31 us (6.6), 18944 x 3583 43 us.
+// start anywhere, 8192 x 18943 bf16, 90 us.  Weights: 18944 x 3584 31 us (6.6), 18944 x 3583 38 us (43 by rows of their own).
 #include "roi_fp8.cuh"
 #include "roi_launch.h"
 
@@ -75,13 +75,17 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_rows_kernel(SaveArgs a)
   pdl_begin(a.wait);
   const int64_t per = 32 / a.width, tasks = (a.rows + per - 1) / per * a.segments;
   const int64_t stride = int64_t(gridDim.x) * (kThreads / 32);
+  const T* end = static_cast<const T*>(a.x) + (a.rows - 1) * a.ld + a.cols;
   for (int64_t t = int64_t(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5); t < tasks; t += stride) {
     Window<E, 16> x;
     int64_t row, j;
     row_task(t, a.width, a.segments, row, j);
-    x.load(static_cast<const T*>(a.x) + row * a.ld, 16 * j, row < a.rows ? a.cols : 0);
+    const T* p = static_cast<const T*>(a.x) + row * a.ld + 16 * j;
+    const int64_t left = row < a.rows ? a.cols - 16 * j : 0;
+    if (left > 0 && x.in_matrix(p, a.x, end)) x.load_granules(p);
+    else x.load(static_cast<const T*>(a.x) + row * a.ld, 16 * j, row < a.rows ? a.cols : 0);
     RowWords<E, 16> r;
-    x.get(r);
+    x.get_masked(r, left);
     save_piece<F, E>(a, r, row, j);
   }
 }
@@ -108,11 +112,19 @@ __global__ void __launch_bounds__(kThreads) roi_fp8_save_weight_kernel(WeightArg
     const int64_t r0 = bm * 128 + (threadIdx.x >> 3), c = bn * 128 + 16 * (threadIdx.x & 7);
     RowWords<Elem::kBf16, 16> r[kPieces];
     if constexpr (ANYWHERE) {
-      Window<Elem::kBf16, 16> w[kPieces];
+      using Piece = Window<Elem::kBf16, 16>;
+      Piece w[kPieces];
+      const uint16_t *p = a.W + r0 * a.cols + c, *end = a.W + a.rows * a.cols;
+      const int64_t left = a.cols - c;
+      if (left > 0 && Piece::in_matrix(p, a.W, end) && Piece::in_matrix(p + 32 * (kPieces - 1) * a.cols, a.W, end)) {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) w[i].load(a.W + (r0 + 32 * i) * a.cols, c, r0 + 32 * i < a.rows ? a.cols : 0);
+        for (int i = 0; i < kPieces; ++i) w[i].load_granules(p + 32 * i * a.cols);
+      } else {
 #pragma unroll
-      for (int i = 0; i < kPieces; ++i) w[i].get(r[i]);
+        for (int i = 0; i < kPieces; ++i) w[i].load(a.W + (r0 + 32 * i) * a.cols, c, r0 + 32 * i < a.rows ? a.cols : 0);
+      }
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) w[i].get_masked(r[i], r0 + 32 * i < a.rows ? left : 0);
     } else if (r0 + 32 * (kPieces - 1) < a.rows && c + 16 <= a.cols) {
       // (no branch between the loads: where ways meet, the compiler waits for what is on its way)
 #pragma unroll

@@ -23,8 +23,8 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kEach32 = 8, kEach8 = 16, kBlock = 128;
 constexpr int kCtas32 = 10, kCtas8 = 5, kCtasLoad = 12;  // of an SM
-// A launch has a CTA a tile, so that tiles are taken in their order: 912 us for a 7B-shaped block's step in 32 bits, 1019 where the CTAs
-// that an SM holds went over them, 992 and 959 with two and four times as many.  In 8 bits, where a CTA's start counts, four
+// In 32 bits a launch has a CTA a tile, so that tiles are taken in their order: 912 us for a 7B-shaped block's step, 1019 where the CTAs
+// that the SMs hold went over them, 992 and 959 with two and four times as many.  In 8 bits, where a CTA's start counts, four
 // times what is held (the block with the states read back: one, two, four, eight times and a CTA a tile 893, 864, 852, 844, 885 us;
 // eight 0.5B-shaped blocks 468, 457, 454, 467, 467).
 constexpr int kWaves8 = 4;
@@ -283,7 +283,7 @@ __device__ __forceinline__ void moments_pair(F2 g, F2& m, F2& v, const Settings&
 // the hardware's reciprocals, each with a last correction by its remainder, which a fused multiply-add gives exactly
 // (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  All roots to 2^31
 // round as the instruction does, and so did 2^34 quotients of random significands.  For v <= 2^62, |m| <= 2^62, eps >= 2^-40 and
-// steps of at most 2^20 (Args::plain); v comes from where it may be subnormal by 2^64; a quotient of a step m under 2^-102, whose
+// steps of at most 2^20 (Settings::plain); v comes from where it may be subnormal by 2^64; a quotient of a step m under 2^-102, whose
 // remainder may not be exact, may be a bit off.
 constexpr float kQuickMost = 4611686018427387904.0f;  // 2^62
 __device__ __forceinline__ F2 quick_pair(F2 p, F2 m, F2 v, F2& u, const Settings& a) {

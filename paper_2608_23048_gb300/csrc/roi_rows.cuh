@@ -152,7 +152,33 @@ struct Window {
       for (int i = 0; i < kWords; ++i) w[i] = r.u[i];
     }
   }
+  // Where the granules around them lie in the matrix, whose first byte and end are given (what is between rows, or the next
+  // rows', is read and dropped by get_masked): all lanes but those at the matrix's ends go this way, without a branch at each row's.
+  static __device__ __forceinline__ bool in_matrix(const typename ElemType<E>::T* p, const void* begin, const void* end) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p) & ~uintptr_t(15);
+    return from >= reinterpret_cast<uintptr_t>(begin) && from + kWords * 4 + 16 <= reinterpret_cast<uintptr_t>(end);
+  }
+  __device__ __forceinline__ void load_granules(const typename ElemType<E>::T* p) {
+    m = uint32_t(reinterpret_cast<uintptr_t>(p) & 15u);
+    const uint4* q = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(p) - m);
+#pragma unroll
+    for (int i = 0; i < kWords / 4 + 1; ++i) {
+      const uint4 v = __ldg(q + i);
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
+  }
   __device__ __forceinline__ void get(R& r) const { shift_words<kWords>(w, m, r.u); }
+  // ... those from `left` on as zeros.
+  __device__ __forceinline__ void get_masked(R& r, int64_t left) const {
+    get(r);
+    if (left < N) {
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) {
+        if constexpr (E == Elem::kFp32) r.u[i] = i < left ? r.u[i] : 0u;
+        else r.u[i] &= (2 * i < left ? 0xffffu : 0u) | (2 * i + 1 < left ? 0xffff0000u : 0u);
+      }
+    }
+  }
 };
 
 // All lanes of a warp, in groups of `width` (a power of two) with a row each: lane l of a group
