@@ -762,19 +762,23 @@ def new_fp8_weight(rows, cols, device="cuda"):
 _UINT8 = None  # torch.uint8, once torch is there
 
 
-def _fp8(pair, name, rows, cols, scale_rows):
-    """Addresses of a copy's codes and scales (of a matrix [rows, cols])."""
+def _fp8(pair, name, rows, pitch, scale_rows, scale_pitch):
+    """Addresses of a copy's codes [rows, pitch] and scales."""
     global _UINT8
     codes, scales = pair
-    if (codes.dtype is _UINT8 and scales.dtype is _UINT8 and codes.is_cuda and scales.is_cuda and codes.is_contiguous()
-            and scales.is_contiguous() and codes.shape == (rows, (cols + 127) // 128 * 128)
-            and scales.shape == (scale_rows, (cols + 2047) // 2048 * 16)):
+    if (codes.dtype is scales.dtype is _UINT8 and codes.is_cuda and scales.is_cuda and codes.is_contiguous()
+            and scales.is_contiguous() and codes.shape == (rows, pitch) and scales.shape == (scale_rows, scale_pitch)):
         return codes.data_ptr(), scales.data_ptr()
     import torch
     _UINT8 = torch.uint8
-    _check_tensor(codes, f"{name} codes", torch.uint8, (rows, (cols + 127) // 128 * 128))
-    _check_tensor(scales, f"{name} scales", torch.uint8, (scale_rows, (cols + 2047) // 2048 * 16))
+    _check_tensor(codes, f"{name} codes", torch.uint8, (rows, pitch))
+    _check_tensor(scales, f"{name} scales", torch.uint8, (scale_rows, scale_pitch))
     return codes.data_ptr(), scales.data_ptr()
+
+
+def _pitches(cols):
+    """Codes and scale bytes in a row of a copy of `cols` columns."""
+    return (cols + 127) // 128 * 128, (cols + 2047) // 2048 * 16
 
 
 def roi_fp8_save(x, format, out_codes, out_scales, stream=None):
@@ -782,9 +786,11 @@ def roi_fp8_save(x, format, out_codes, out_scales, stream=None):
     ("e4m3" or "e5m2") with a power of two for every 128 columns of a row."""
     ld = _stride(x, "x")
     rows, cols = x.shape
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, rows)
+    pitch, scale_pitch = _pitches(cols)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, rows, scale_pitch)
     s = lib().roi_fp8_save(x.data_ptr(), _type(x, "x"), rows, cols, ld, _format(format), codes, scales, _stream(stream))
-    _raise(s, "roi_fp8_save")
+    if s != ROI_OK:
+        _raise(s, "roi_fp8_save")
 
 
 def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
@@ -792,9 +798,11 @@ def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
     import torch
     rows, cols = W.shape
     _check_tensor(W, "W", torch.bfloat16)
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, cols, (rows + 127) // 128)
+    pitch, scale_pitch = _pitches(cols)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, (rows + 127) // 128, scale_pitch)
     s = lib().roi_fp8_save_weight(W.data_ptr(), rows, cols, codes, scales, _stream(stream))
-    _raise(s, "roi_fp8_save_weight")
+    if s != ROI_OK:
+        _raise(s, "roi_fp8_save_weight")
 
 
 def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
@@ -802,12 +810,13 @@ def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
     ld = _stride(out_y, "out_y")
     T, rows = out_y.shape
     # padding codes are zeros, so the whole blocks stand for the columns
-    cols = w8[0].shape[1]
-    xq, xs = _fp8(x8, "x8", T, cols, T)
-    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128)
+    cols, scale_pitch = _pitches(w8[0].shape[1])
+    xq, xs = _fp8(x8, "x8", T, cols, T, scale_pitch)
+    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128, scale_pitch)
     s = lib().roi_fp8_linear_fwd(xq, xs, _format(format), wq, ws, T, rows, cols, out_y.data_ptr(), _type(out_y, "out_y"), ld,
                                  _stream(stream))
-    _raise(s, "roi_fp8_linear_fwd")
+    if s != ROI_OK:
+        _raise(s, "roi_fp8_linear_fwd")
 
 
 def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
@@ -815,11 +824,14 @@ def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
     ld = _stride(out_dx, "out_dx")
     T, cols = out_dx.shape
     rows = w8[0].shape[0]
-    dq, ds = _fp8(dy8, "dy8", T, rows, T)
-    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128)
+    pitch, scale_pitch = _pitches(rows)
+    dq, ds = _fp8(dy8, "dy8", T, pitch, T, scale_pitch)
+    pitch, scale_pitch = _pitches(cols)
+    wq, ws = _fp8(w8, "w8", rows, pitch, (rows + 127) // 128, scale_pitch)
     s = lib().roi_fp8_linear_dgrad(dq, ds, _format(format), wq, ws, T, rows, cols, out_dx.data_ptr(), _type(out_dx, "out_dx"), ld,
                                    _stream(stream))
-    _raise(s, "roi_fp8_linear_dgrad")
+    if s != ROI_OK:
+        _raise(s, "roi_fp8_linear_dgrad")
 
 
 # ---------------------------------------------------------------------------

@@ -353,11 +353,11 @@ constexpr int kMostBlocks = 16;
 
 // Clusters of `size` CTAs of this kernel that the device holds at once: a cluster lies within one of its GPCs, so that
 // they do not use every SM (7 CTAs to a cluster, 21 clusters, 147 CTAs on 152 SMs: two waves).
-int clusters_at_once(int size) {
+// (`dev` the current device.)
+int clusters_at_once(int dev, int size) {
   if (size == 1) return sm_count();
   static std::atomic<int> known[64][9];
-  int dev = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
+  if (dev < 0 || dev >= 64) return 1;
   int n = known[dev][size].load(std::memory_order_acquire);
   if (n == 0) {
     auto kern = roi_fp8_linear_kernel<false, Elem::kBf16>;
@@ -385,6 +385,8 @@ int clusters_at_once(int size) {
 // a cycle: 2 (128 + n) cycles a block.  Filling the ring and writing the tile come once a tile, joining ranges once a range.
 constexpr int kTileCycles = 2000, kTokenCycles = 12, kJoinCycles = 2000;
 int64_t plan(int64_t T, int64_t tiles_o, int blocks, bool fp32, LinearArgs& a, int64_t& tiles_t) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
   int64_t least = INT64_MAX;
   int64_t last = 0;
   for (int64_t t = (T + 255) / 256, tries = 0; tries < 16; ++t, ++tries) {
@@ -392,7 +394,7 @@ int64_t plan(int64_t T, int64_t tiles_o, int blocks, bool fp32, LinearArgs& a, i
     if (n == last) continue;
     last = n;
     for (int s = 1; s <= 8 && s <= blocks; ++s) {
-      const int64_t once = clusters_at_once(s);
+      const int64_t once = clusters_at_once(dev, s);
       if (s > 1 && (tiles_o * t > once || join_bytes(int(n), s) > kRingBytes)) break;
       const int range = (blocks + s - 1) / s;
       const int pieces = fp32 ? (range + kMostBlocks - 1) / kMostBlocks : 1;
