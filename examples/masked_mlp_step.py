@@ -25,6 +25,9 @@ import paper_2608_23048_gb300 as roi  # noqa: E402
 import workloads as WL  # noqa: E402
 
 N, M, EPS = 2, 4, 1e-6
+# of the masks' noise, and of what rounds the moments: with one seed for both, the words that round a logit's moments would be
+# those of its noise in a mask
+NOISE_SEED, ROUNDING_SEED = 7, 8
 
 
 class MaskedLinear:
@@ -37,7 +40,7 @@ class MaskedLinear:
         self.tensor_id = tensor_id
 
     def forward(self, X, step, tau):
-        self.state = roi.NoiseState(7, step, self.tensor_id, 1.0, 0)
+        self.state = roi.NoiseState(NOISE_SEED, step, self.tensor_id, 1.0, 0)
         roi.roi_mask_fwd_ex(self.logits, self.W, N, M, tau, self.state, self.Wm)
         return X @ self.Wm.T
 
@@ -60,7 +63,7 @@ class MaskedLinearFp8(MaskedLinear):
         self.w8, self.in8, self.out8 = roi.new_fp8_weight(rows, cols), roi.new_fp8(tokens, cols), roi.new_fp8(tokens, rows)
 
     def forward(self, X, step, tau):
-        self.state = roi.NoiseState(7, step, self.tensor_id, 1.0, 0)
+        self.state = roi.NoiseState(NOISE_SEED, step, self.tensor_id, 1.0, 0)
         roi.roi_mask_fwd_ex(self.logits, self.W, N, M, tau, self.state, self.Wm)
         roi.roi_fp8_save_weight(self.Wm, *self.w8)
         roi.roi_fp8_save(X, "e4m3", *self.in8)
@@ -121,7 +124,8 @@ class MaskedMLP:
         roi.roi_norm_bwd(dy, self.x8, "rms", self.gamma, None, self.rstd, dx, dgamma, None, self.workspace)
         if self.fp8:
             # (a data-parallel run reduces the layers' dlogits here)
-            roi.roi_adamw_step8([(x.logits, x.dlogits, x.moments, None, x.tensor_id) for x in (self.gate, self.up, self.down)], opt, 7)
+            items = [(x.logits, x.dlogits, x.moments, None, x.tensor_id) for x in (self.gate, self.up, self.down)]
+            roi.roi_adamw_step8(items, opt, ROUNDING_SEED)
         return dx + d_out, dgamma
 
     def kept_bytes(self):

@@ -257,7 +257,9 @@ roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi
  * (m) or high (u) half of the element's Philox word for (seed, opt->t, tensor_id), counters as for the mask's noise.
  * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.  The step's quotient
  * may be a bit off roi_adamw_step's in its last place (none of 2^34 was).  Items that share (seed, t) need a
- * tensor_id of their own each, as layers of the mask do. */
+ * tensor_id of their own each, as layers of the mask do.  Nor may (seed, t, tensor_id) be the (seed, step, tensor_id) of a
+ * mask's noise: the words would be the same, and a logit's moments rounded up where its noise in that mask is large.  A
+ * seed that no mask uses keeps the two apart. */
 typedef struct {
     float* param;
     const void* grad;

@@ -951,7 +951,8 @@ def roi_adamw_step(items, opt: AdamW, grad_scale=None, stream=None):
 
 def roi_adamw_step8(items, opt: AdamW, seed, grad_scale=None, stream=None):
     """roi_adamw_step with states in 8 bits, rounded by the noise of (seed, opt.t, tensor_id) (an AdamWStep8Item array
-    from make_adamw_step8_items, or a list of (param, grad, state, copy, tensor_id) tuples)."""
+    from make_adamw_step8_items, or a list of (param, grad, state, copy, tensor_id) tuples).  The seed is not one of the
+    masks' NoiseState: the same words would round the moments and draw a mask."""
     arr = items if isinstance(items, ctypes.Array) else make_adamw_step8_items(items)
     s = lib().roi_adamw_step8(arr, len(arr), ctypes.byref(opt), int(seed), _grad_scale(grad_scale), _stream(stream))
     _raise(s, "roi_adamw_step8")
