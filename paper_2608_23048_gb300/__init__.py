@@ -762,17 +762,19 @@ def new_fp8_weight(rows, cols, device="cuda"):
 _UINT8 = None  # torch.uint8, once torch is there
 
 
-def _fp8(pair, name, rows, pitch, scale_rows, scale_pitch):
-    """Addresses of a copy's codes [rows, pitch] and scales."""
+def _fp8(pair, name, rows, pitch, scale_rows, scale_pitch, like):
+    """Addresses of a copy's codes [rows, pitch] and scales, on the device of `like` (a CUDA tensor)."""
     global _UINT8
     codes, scales = pair
-    if (codes.dtype is scales.dtype is _UINT8 and codes.is_cuda and scales.is_cuda and codes.is_contiguous()
-            and scales.is_contiguous() and codes.shape == (rows, pitch) and scales.shape == (scale_rows, scale_pitch)):
+    if (codes.dtype is scales.dtype is _UINT8 and codes.get_device() == scales.get_device() == like.get_device()
+            and codes.is_contiguous() and scales.is_contiguous() and codes.shape == (rows, pitch)
+            and scales.shape == (scale_rows, scale_pitch)):
         return codes.data_ptr(), scales.data_ptr()
     import torch
     _UINT8 = torch.uint8
     _check_tensor(codes, f"{name} codes", torch.uint8, (rows, pitch))
     _check_tensor(scales, f"{name} scales", torch.uint8, (scale_rows, scale_pitch))
+    _device((like, codes, scales), name)
     return codes.data_ptr(), scales.data_ptr()
 
 
@@ -787,7 +789,7 @@ def roi_fp8_save(x, format, out_codes, out_scales, stream=None):
     ld = _stride(x, "x")
     rows, cols = x.shape
     pitch, scale_pitch = _pitches(cols)
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, rows, scale_pitch)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, rows, scale_pitch, x)
     s = lib().roi_fp8_save(x.data_ptr(), _type(x, "x"), rows, cols, ld, _format(format), codes, scales, _stream(stream))
     if s != ROI_OK:
         _raise(s, "roi_fp8_save")
@@ -799,7 +801,7 @@ def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
     rows, cols = W.shape
     _check_tensor(W, "W", torch.bfloat16)
     pitch, scale_pitch = _pitches(cols)
-    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, (rows + 127) // 128, scale_pitch)
+    codes, scales = _fp8((out_codes, out_scales), "out", rows, pitch, (rows + 127) // 128, scale_pitch, W)
     s = lib().roi_fp8_save_weight(W.data_ptr(), rows, cols, codes, scales, _stream(stream))
     if s != ROI_OK:
         _raise(s, "roi_fp8_save_weight")
@@ -811,8 +813,8 @@ def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
     T, rows = out_y.shape
     # padding codes are zeros, so the whole blocks stand for the columns
     cols, scale_pitch = _pitches(w8[0].shape[1])
-    xq, xs = _fp8(x8, "x8", T, cols, T, scale_pitch)
-    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128, scale_pitch)
+    xq, xs = _fp8(x8, "x8", T, cols, T, scale_pitch, out_y)
+    wq, ws = _fp8(w8, "w8", rows, cols, (rows + 127) // 128, scale_pitch, out_y)
     s = lib().roi_fp8_linear_fwd(xq, xs, _format(format), wq, ws, T, rows, cols, out_y.data_ptr(), _type(out_y, "out_y"), ld,
                                  _stream(stream))
     if s != ROI_OK:
@@ -825,9 +827,9 @@ def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
     T, cols = out_dx.shape
     rows = w8[0].shape[0]
     pitch, scale_pitch = _pitches(rows)
-    dq, ds = _fp8(dy8, "dy8", T, pitch, T, scale_pitch)
+    dq, ds = _fp8(dy8, "dy8", T, pitch, T, scale_pitch, out_dx)
     pitch, scale_pitch = _pitches(cols)
-    wq, ws = _fp8(w8, "w8", rows, pitch, (rows + 127) // 128, scale_pitch)
+    wq, ws = _fp8(w8, "w8", rows, pitch, (rows + 127) // 128, scale_pitch, out_dx)
     s = lib().roi_fp8_linear_dgrad(dq, ds, _format(format), wq, ws, T, rows, cols, out_dx.data_ptr(), _type(out_dx, "out_dx"), ld,
                                    _stream(stream))
     if s != ROI_OK:
@@ -854,21 +856,21 @@ def _same_size(t, name, dtype, n):
         raise ValueError(f"{name}: expected {n} elements, got {t.numel()}")
 
 
-def _device(tensors, name):
-    """One device for all of an item's tensors."""
-    first = None
+def _device(tensors, name, first=None):
+    """The one device of a call's tensors, of which those before lie on `first`."""
     for t in tensors:
         if t is not None:
             first = t.device if first is None else first
             if t.device != first:
                 raise ValueError(f"{name}: tensors on {first} and on {t.device}")
+    return first
 
 
 def make_adamw_step_items(items):
     """ctypes array of AdamWStepItem from (param, grad, m, v, copy) tuples: tensors of any shape, copy (bfloat16 or
     float16) or None."""
     import torch
-    arr = (AdamWStepItem * len(items))()
+    arr, device = (AdamWStepItem * len(items))(), None
     for k, (param, grad, m, v, copy) in enumerate(items):
         shape = param.shape
         _check_tensor(param, "param", torch.float32)
@@ -877,8 +879,9 @@ def make_adamw_step_items(items):
         _check_tensor(m, "m", torch.float32, shape)
         _check_tensor(v, "v", torch.float32, shape)
         half = _half(copy, "copy", shape)
-        _device((param, grad, m, v, copy), f"item {k}")
+        device = _device((param, grad, m, v, copy), f"item {k}", device)
         arr[k] = AdamWStepItem(_addr(param), _addr(grad), _addr(m), _addr(v), _addr(copy), param.numel(), code, half)
+    arr.device = device
     return arr
 
 
@@ -902,7 +905,7 @@ def _state8(state, n):
 def make_adamw_step8_items(items):
     """ctypes array of AdamWStep8Item from (param, grad, state, copy, tensor_id) tuples, state as from new_adamw_state8."""
     import torch
-    arr = (AdamWStep8Item * len(items))()
+    arr, device = (AdamWStep8Item * len(items))(), None
     for k, (param, grad, state, copy, tensor_id) in enumerate(items):
         shape = param.shape
         _check_tensor(param, "param", torch.float32)
@@ -911,14 +914,15 @@ def make_adamw_step8_items(items):
         half = _half(copy, "copy", shape)
         n = param.numel()
         at = _state8(state, n)
-        _device((param, grad, *state, copy), f"item {k}")
+        device = _device((param, grad, *state, copy), f"item {k}", device)
         arr[k] = AdamWStep8Item(_addr(param), _addr(grad), *at, _addr(copy), n, code, half, int(tensor_id))
+    arr.device = device
     return arr
 
 
 def make_adamw_state8_items(items):
     """ctypes array of AdamWState8Item from (state, out_m, out_u) tuples: tensors of one type, one of them or None."""
-    arr = (AdamWState8Item * len(items))()
+    arr, device = (AdamWState8Item * len(items))(), None
     for k, (state, out_m, out_u) in enumerate(items):
         like = out_m if out_m is not None else out_u
         if like is None:
@@ -928,16 +932,17 @@ def make_adamw_state8_items(items):
             if t is not None:
                 _same_size(t, name, like.dtype, n)
         at = _state8(state, n)
-        _device((*state, out_m, out_u), f"item {k}")
+        device = _device((*state, out_m, out_u), f"item {k}", device)
         arr[k] = AdamWState8Item(*at, _addr(out_m), _addr(out_u), n, code)
     return arr
 
 
-def _grad_scale(t):
+def _grad_scale(t, items):
     if t is None:
         return None
     import torch
     _same_size(t, "grad_scale", torch.float32, 1)
+    _device((t,), "grad_scale", getattr(items, "device", None))
     return t.data_ptr()
 
 
@@ -945,7 +950,7 @@ def roi_adamw_step(items, opt: AdamW, grad_scale=None, stream=None):
     """One AdamW step of many tensors in place (an AdamWStepItem array from make_adamw_step_items, reusable while its
     tensors live, or a list of (param, grad, m, v, copy) tuples).  grad_scale: float32 [1] on the device, or None."""
     arr = items if isinstance(items, ctypes.Array) else make_adamw_step_items(items)
-    s = lib().roi_adamw_step(arr, len(arr), ctypes.byref(opt), _grad_scale(grad_scale), _stream(stream))
+    s = lib().roi_adamw_step(arr, len(arr), ctypes.byref(opt), _grad_scale(grad_scale, arr), _stream(stream))
     _raise(s, "roi_adamw_step")
 
 
@@ -954,7 +959,7 @@ def roi_adamw_step8(items, opt: AdamW, seed, grad_scale=None, stream=None):
     from make_adamw_step8_items, or a list of (param, grad, state, copy, tensor_id) tuples).  The seed is not one of the
     masks' NoiseState: the same words would round the moments and draw a mask."""
     arr = items if isinstance(items, ctypes.Array) else make_adamw_step8_items(items)
-    s = lib().roi_adamw_step8(arr, len(arr), ctypes.byref(opt), int(seed), _grad_scale(grad_scale), _stream(stream))
+    s = lib().roi_adamw_step8(arr, len(arr), ctypes.byref(opt), int(seed), _grad_scale(grad_scale, arr), _stream(stream))
     _raise(s, "roi_adamw_step8")
 
 
