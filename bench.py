@@ -20,6 +20,7 @@ import hashlib
 import json
 import math
 import os
+import re
 import statistics
 import subprocess
 import sys
@@ -195,29 +196,40 @@ def hbm_peak():
         return FALLBACK_HBM_GBS, "fallback"
 
 
-def kernel_source_hash():
-    d = os.path.join(ROOT, "paper_2608_23048_gb300", "csrc")
+CSRC = os.path.join(ROOT, "paper_2608_23048_gb300", "csrc")
+
+
+def kernel_source_hash(source: str, csrc: str = CSRC):
+    """Hash of a .cu file and of the library's headers that it includes, directly or not; None without the file."""
+    texts, todo = {}, [source]
+    while todo:
+        name = todo.pop()
+        try:
+            with open(os.path.join(csrc, name), "rb") as f:
+                texts[name] = f.read()
+        except OSError:
+            if name == source:
+                return None
+            continue  # (include/roi.h, which holds no device code)
+        todo += [n for n in re.findall(r'^#include "([^"]+)"', texts[name].decode(), re.M) if n not in texts]
     h = hashlib.sha256()
-    for name in sorted(os.listdir(d)):
-        with open(os.path.join(d, name), "rb") as f:
-            h.update(name.encode() + f.read())
+    for name in sorted(texts):
+        h.update(name.encode() + texts[name])
     return h.hexdigest()[:16]
 
 
-def recorded_traffic(kernel_tag: str):
-    """DRAM bytes per element of `kernel_tag` from profiles/dram_traffic.txt, if the
-    kernel sources are unchanged since that capture; else None."""
-    path = os.path.join(ROOT, "profiles", "dram_traffic.txt")
+def recorded_traffic(kernel_tag: str, path: str = os.path.join(ROOT, "profiles", "dram_traffic.txt"), csrc: str = CSRC):
+    """DRAM bytes per element of `kernel_tag` from profiles/dram_traffic.txt, if the files that
+    the kernel is compiled from are unchanged since that capture; else None."""
     try:
         lines = open(path).read().splitlines()
     except OSError:
         return None
-    want = kernel_source_hash()
     for ln in lines:
         if ln.startswith("#") or not ln.strip():
             continue
         kv = dict(x.split("=", 1) for x in ln.split() if "=" in x)
-        if kv.get("kernel") == kernel_tag and kv.get("sources") == want:
+        if kv.get("kernel") == kernel_tag and "file" in kv and kv.get("sources") == kernel_source_hash(kv["file"], csrc):
             return float(kv["dram_bytes_per_element"])
     return None
 

@@ -7,6 +7,7 @@
 #include <cstring>
 
 #include "roi.h"
+#include "roi_fp8.cuh"
 #include "roi_launch.h"
 
 namespace roi {

@@ -7,7 +7,6 @@
 
 #include "roi_block8.cuh"
 #include "roi_common.cuh"
-#include "roi_fp8.cuh"
 
 namespace roi {
 
@@ -186,6 +185,9 @@ struct WgradCall {
   unsigned int* status;
   cudaStream_t stream;
 };
+
+// (roi_fp8.cuh)
+enum class Fp8 : int;
 
 // A copy in 8-bit floating point: of an activation (x of type dtype, rows ld apart) or of a weight (bf16, rows whole).
 struct Fp8SaveCall {
