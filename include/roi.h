@@ -253,7 +253,7 @@ roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi
  *  scales            [blocks][2] uint8, m's and u's; 2-byte aligned
  * All of them zero before the first step.  A step forms m and v = u * u in float32, updates them and the parameters
  * as roi_adamw_step does, from the unrounded moments, and rounds m and sqrt(v) up with the probability of what their
- * codes would drop (to the nearest, u could not follow a beta2 of 0.95 down): code = floor(|x| / step + r / 65536), r the low
+ * codes would drop (to the nearest, a u that a beta2 of 0.95 takes down would stay at 1.1875 times a power of two for good): code = floor(|x| / step + r / 65536), r the low
  * (m) or high (u) half of the element's Philox word for (seed, opt->t, tensor_id), counters as for the mask's noise.
  * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.  The step's quotient
  * may be a bit off roi_adamw_step's in its last place (none of 2^34 was).  Items that share (seed, t) need a

@@ -4,8 +4,9 @@
 // Moments in 8 bits: m in e4m3 and u = sqrt(v) without a sign, four bits of exponent and four of mantissa with the same
 // bias, in blocks of 128 consecutive elements with a power of two each (2^(s - 127), s - 127 the least exponent that keeps
 // the block's largest under the largest code, 448 and 480).  The root halves v's range in octaves, so that 19 octaves under a
-// block's largest stay.  Codes are rounded up with the probability of what they would drop: u moves by at most
-// 1 - sqrt(b2) a step, 2.5 % at b2 = 0.95, less than half of a code's step, so that to the nearest it would never move down.
+// block's largest stay.  Codes are rounded up with the probability of what they would drop.  To the nearest, u would not follow
+// a vanishing gradient down: it falls by 1 - sqrt(b2) a step, 2.5 % at b2 = 0.95, and half a code's step is 3.1 % of u at the start of an
+// octave and 1.6 % at its end, so that it would fall too fast there and stay for good at 1.1875 times a power of two, or 1.125, or 1.0625.
 // The probability is compared in 16 bits, m's in the low and u's in the high half of the element's Philox word (counter
 // as the mask's noise: element / 4, step, tensor).  The parameters take the step from the moments before they are rounded.
 //
