@@ -253,8 +253,9 @@ roi_status roi_adamw_step(const roi_adamw_step_item* items, int count, const roi
  *  scales            [blocks][2] uint8, m's and u's; 2-byte aligned
  * All of them zero before the first step.  A step forms m and v = u * u in float32, updates them and the parameters
  * as roi_adamw_step does, from the unrounded moments, and rounds m and sqrt(v) up with the probability of what their
- * codes would drop (to the nearest, a u that a beta2 of 0.95 takes down would stay at 1.1875 times a power of two for good): code = floor(|x| / step + r / 65536), r the low
- * (m) or high (u) half of the element's Philox word for (seed, opt->t, tensor_id), counters as for the mask's noise.
+ * codes would drop (to the nearest, a u that a beta2 of 0.95 takes down would stay at 1.1875 times a power of two for
+ * good): code = floor(|x| / step + r / 65536), r the low (m) or high (u) half of the element's Philox word for
+ * (seed, opt->t, tensor_id), counters as for the mask's noise.
  * A u that is not zero keeps a code that is not zero.  What is not finite becomes a NaN and stays one.  The step's quotient
  * may be a bit off roi_adamw_step's in its last place (none of 2^34 was).  Items that share (seed, t) need a
  * tensor_id of their own each, as layers of the mask do.  Nor may (seed, t, tensor_id) be the (seed, step, tensor_id) of a
@@ -509,7 +510,8 @@ roi_status roi_masked_linear_wgrad(const roi_bf16* dY, int64_t lddy, const int8_
  * x * 2^(127 - s) rounded to the format, ties to even.  A block with an infinity or a NaN has s = 255 and codes 0
  * and makes every sum NaN that it is part of.  Padding codes are 0, padding scales 1.  Both arrays are
  * contiguous and 16-byte aligned, as every row of theirs is: an activation's copy may be saved and used in slices of rows,
- * a weight's in slices of 128.
+ * a weight's in slices of 128.  A copy does not hold its number of columns, and padding adds nothing to a sum: a product of
+ * copies of different widths that are padded alike (200 and 250 columns) is that of the narrower with the wider's first columns.
  */
 typedef enum {
     ROI_E4M3 = 0,
@@ -519,6 +521,7 @@ int64_t roi_fp8_pitch(int64_t cols);
 int64_t roi_fp8_scale_pitch(int64_t cols);
 
 /* Copies x [rows, cols] of type dtype (roi_dtype), row stride ldx, aligned to its elements; rows and cols at most 2^30.
+ * What lies between its rows may be read, and has no effect.
  *  format: roi_fp8_format (e4m3 for activations; e5m2, a longer range and one bit less, for gradients)          */
 roi_status roi_fp8_save(const void* x, int dtype, int64_t rows, int64_t cols, int64_t ldx, int format,
                         uint8_t* out_codes, uint8_t* out_scales, void* stream);
@@ -530,8 +533,9 @@ roi_status roi_fp8_save_weight(const roi_bf16* W, int64_t rows, int64_t cols, ui
 /* The layer's forward, Y[t, r] = sum_c x^[t, c] w^[r, c], and the gradient of its input,
  * dX[t, c] = sum_r dy^[t, r] w^[r, c], x^, w^, dy^ the values that the copies stand for.  Products are exact,
  * sums in fp32 on the tensor cores' block-scaled instructions, rounded once to dtype.  Those drop the bits below a sum's
- * last instead of rounding, 1.4e-6 of the result's norm over a width of 18944; for float32 results sums are made of pieces of
- * at most 2048 columns, added with rounding (1.2e-7, where a float32 product has 2.1e-7).
+ * last instead of rounding, 1.4e-6 of the result's norm over a width of 18944.  16-bit results are such sums.  For float32
+ * results sums are made of pieces of at most 2048 columns, added with rounding: 1.2e-7 over 18944, where a float32 product
+ * has 2.1e-7; up to 2048 columns it is one piece, 2.5e-8 over 1001.
  *  x_codes, x_scales, format    the copy of x [T, cols]
  *  dy_codes, dy_scales, format  the copy of dy [T, rows]
  *  w_codes, w_scales            the copy of the weight [rows, cols]

@@ -808,7 +808,8 @@ def roi_fp8_save_weight(W, out_codes, out_scales, stream=None):
 
 
 def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
-    """out_y[T, rows] = x w^T from the (codes, scales) pairs of an activation (`format`) and of a weight."""
+    """out_y[T, rows] = x w^T from the (codes, scales) pairs of an activation (`format`) and of a weight, of the same number of
+    columns (which a copy holds to the next 128 only)."""
     ld = _stride(out_y, "out_y")
     T, rows = out_y.shape
     # padding codes are zeros, so the whole blocks stand for the columns
@@ -822,7 +823,8 @@ def roi_fp8_linear_fwd(x8, format, w8, out_y, stream=None):
 
 
 def roi_fp8_linear_dgrad(dy8, format, w8, out_dx, stream=None):
-    """out_dx[T, cols] = dy w, from the (codes, scales) pairs of dy [T, rows] (`format`) and of the weight [rows, cols]."""
+    """out_dx[T, cols] = dy w, from the (codes, scales) pairs of dy [T, rows] (`format`; it holds its columns to the next 128
+    only) and of the weight [rows, cols]."""
     ld = _stride(out_dx, "out_dx")
     T, cols = out_dx.shape
     rows = w8[0].shape[0]

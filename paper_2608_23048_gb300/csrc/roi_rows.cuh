@@ -7,8 +7,10 @@
 //  - a store puts together aligned granules from the end of the lane before and its own words
 //    (store_words, by the whole warp; the first and last lane write what has no neighbour
 //    element by element).
-// Nothing outside [row, row + cols) is read or written: what lies at the ends of a row goes
-// element by element.
+// Nothing outside a row, [row, row + cols), is written, and load and store_words read nothing outside it either: what lies at
+// its ends goes element by element.  load_granules reads whole granules, up to 15 bytes before its words and what follows
+// them to the granule's end, and with a row's last words whatever of the next rows or of the gap between they cover;
+// get_masked drops it.  in_matrix keeps these reads between the matrix's first byte and its last.
 #pragma once
 
 #include "roi_block8.cuh"

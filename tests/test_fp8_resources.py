@@ -37,3 +37,10 @@ def test_adamw():
     for name, ctas in (("roi_adamw_step_kernel", 10), ("roi_adamw_step8_kernel", 5), ("roi_adamw_state8_load_kernel", 12)):
         found = kernels("roi_optim.cu", name)
         assert len(found) == 2 and all(spill == 0 and -(-regs // 8) * 8 * 128 * ctas <= 65536 for regs, spill in found), (name, found)
+
+
+def test_copies_are_found():
+    """Rows whole sectors apart and anywhere, two formats and three types each, and weights of either kind."""
+    found = kernels("roi_fp8.cu", "roi_fp8_save")
+    assert len(found) == 14 and all(spill == 0 for _, spill in found)
+    assert len(kernels("roi_fp8.cu", "roi_fp8_save_weight_kernel")) == 2
