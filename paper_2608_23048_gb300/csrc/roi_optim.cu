@@ -283,8 +283,8 @@ __device__ __forceinline__ void moments_pair(F2 g, F2& m, F2& v, const Settings&
 // The parameters, without a branch for what is far out of range.  Root and quotient by Goldschmidt's and Newton's iterations from
 // the hardware's reciprocals, each with a last correction by its remainder, which a fused multiply-add gives exactly
 // (Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990).  All roots to 2^31
-// round as the instruction does, and so did 2^34 quotients of random significands.  For v <= 2^62, |m| <= 2^62, eps >= 2^-40 and
-// steps of at most 2^20 (Settings::plain); v comes from where it may be subnormal by 2^64; a quotient of a step m under 2^-102, whose
+// round as the instruction does, and so did 2^34 quotients of random significands.  For v <= 2^62, |m| <= 2^62, eps from 2^-40 to
+// 2^40 (the reciprocal of a divisor over 2^126 would be 0) and steps of at most 2^20 (Settings::plain); v comes from where it may be subnormal by 2^64; a quotient of a step m under 2^-102, whose
 // remainder may not be exact, may be a bit off.
 constexpr float kQuickMost = 4611686018427387904.0f;  // 2^62
 __device__ __forceinline__ F2 quick_pair(F2 p, F2 m, F2 v, F2& u, const Settings& a) {
@@ -561,7 +561,7 @@ int launch(const OptimCall& c, const OptimItem* items, int count) {
   a.step = c.step;
   a.scale = c.scale;
   a.one = 1.0f;
-  a.plain = c.opt.eps >= 9.094947017729282e-13f && c.opt.step <= 1048576.0f;  // 2^-40, 2^20
+  a.plain = c.opt.eps >= 9.094947017729282e-13f && c.opt.eps <= 1099511627776.0f && c.opt.step <= 1048576.0f;  // 2^-40, 2^40, 2^20
   const int tile = c.kind == OptimKind::kStep ? kThreads * kEach32 : kThreads * kEach8;
   auto kern = c.kind == OptimKind::kStep ? roi_adamw_step_kernel<Args>
               : c.kind == OptimKind::kStep8 ? roi_adamw_step8_kernel<Args>
