@@ -317,7 +317,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(free + b, 0);
+      if (lane == 0) mbar_arrive_cluster_tmem(free + b, 0);
       if (!w.last) continue;
 #pragma unroll
       for (int q = 0; q < kChunks; ++q) {

@@ -195,13 +195,23 @@ __device__ __forceinline__ void cluster_sync() {
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.aligned;" ::: "memory"); }
 // One arrival on the mbarrier at `bar`'s place in the shared memory of CTA `rank` of the cluster.
-// Release at CTA scope, as an arrival without qualifiers has: what is handed over lies in this
-// CTA's own shared memory or TMEM and is read there by the tensor cores, behind the writers' proxy
-// fences; nothing is read across.  (.release.cluster took 1000 cycles an arrival.)
+// What is handed over lies in this CTA's own shared memory, and the other CTA's thread has the tensor
+// cores read it there: a release to the cluster of shared memory alone, which pairs with
+// mbar_wait_ring_cluster's acquire.  (.release.cluster, of all memory, took 1000 cycles an arrival.)
 __device__ __forceinline__ void mbar_arrive_cluster(uint64_t* bar, uint32_t rank) {
   asm volatile(
       "{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\t"
-      "mbarrier.arrive.shared::cluster.b64 _, [ra];\n\t}" ::"r"(smem_addr(bar)),
+      "fence.release.sync_restrict::shared::cta.cluster;\n\t"
+      "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [ra];\n\t}" ::"r"(smem_addr(bar)),
+      "r"(rank)
+      : "memory");
+}
+// The same where columns of TMEM are given back, behind tc_fence_before: that orders the reads of them, and shared memory
+// has no part in it.
+__device__ __forceinline__ void mbar_arrive_cluster_tmem(uint64_t* bar, uint32_t rank) {
+  asm volatile(
+      "{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %0, %1;\n\t"
+      "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [ra];\n\t}" ::"r"(smem_addr(bar)),
       "r"(rank)
       : "memory");
 }

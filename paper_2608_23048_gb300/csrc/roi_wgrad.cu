@@ -23,8 +23,9 @@
 // chunk 1888 us; without that release 982; two sets of converting warps and the scales staged apart
 // 867; even bytes converted where they are 727; rings of their own and loops of whole warps
 // around the MMAs, so that descriptors stay in uniform registers, 631; whole sectors out 583 to 600,
-// which is 1860 to 1910 TFLOP/s; waits that a whole warp answers as one 605.  Under a long load the clock falls with the
-// power (697 us).
+// which is 1860 to 1910 TFLOP/s; waits that a whole warp answers as one 605; arrivals on the pair's barriers that release
+// shared memory to the cluster 608 (with acc 785 -> 817; handed on by the warp that tells of dY alone, 622 and 816).  Under a
+// long load the clock falls with the power (697 us).
 // Every wait is bounded; a CTA that gives up lets its copies and MMAs end before it leaves.
 //
 // Tiles go to the pairs in rounds.  In the last, partial round the tokens of
@@ -569,7 +570,7 @@ __device__ __forceinline__ void wgrad(const CUtensorMap& tm_dy, const CUtensorMa
       }
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(free + b, 0);
+      if (lane == 0) mbar_arrive_cluster_tmem(free + b, 0);
     }
   }
   if (!ok) misc[1] = 0u;
