@@ -402,14 +402,25 @@ constexpr int kMostBlocks = 16;
 
 }  // namespace
 
-int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width) {
-  const int groups = sm_count() / 2, blocks = int((width + kStep - 1) / kStep);
-  int n;
-  const int64_t a = rows_of_b(T, outs, blocks, groups, n), b = rows_of_b(outs, T, blocks, groups, n);
-  return a < b ? a : b;
+// Tokens in the lanes need whole sectors of out and K-major weights.
+bool fp8_pair_tokens(const Fp8LinearCall& c) {
+  const int b = c.dtype == Elem::kFp32 ? 4 : 2;
+  return !c.dgrad && (reinterpret_cast<uintptr_t>(c.out) & 31u) == 0 && c.ldo * b % 32 == 0;
 }
 
-int launch_fp8_pair(const Fp8LinearCall& c) {
+int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width, bool tokens, int groups, Fp8PairPlan& plan) {
+  const int blocks = int((width + kStep - 1) / kStep);
+  const int64_t by_outputs = rows_of_b(outs, T, blocks, groups, plan.n);
+  plan.outputs = true;
+  if (!tokens) return by_outputs;
+  int n;
+  const int64_t by_tokens = rows_of_b(T, outs, blocks, groups, n);
+  if (by_tokens > by_outputs) return by_outputs;
+  plan = {n, false};
+  return by_tokens;
+}
+
+int launch_fp8_pair(const Fp8LinearCall& c, const Fp8PairPlan& plan) {
   PairArgs a;
   const int64_t outs = c.dgrad ? c.cols : c.rows, width = c.dgrad ? c.rows : c.cols;
   a.w_scales = c.w_scales;
@@ -425,15 +436,8 @@ int launch_fp8_pair(const Fp8LinearCall& c) {
   a.unbroken = c.dtype == Elem::kFp32 ? kMostBlocks : (a.blocks + 3) / 4 * 4;
   a.pieces = (a.blocks + a.unbroken - 1) / a.unbroken;
   a.groups = sm_count() / 2;
-  // Tokens in the lanes need whole sectors of out and K-major weights; with both ways open, the one of fewer rounds.
-  const int b = c.dtype == Elem::kFp32 ? 4 : 2;
-  bool outputs = c.dgrad || (reinterpret_cast<uintptr_t>(c.out) & 31u) != 0 || c.ldo * b % 32 != 0;
-  const int64_t by_outputs = rows_of_b(outs, c.T, a.blocks, a.groups, a.n);
-  if (!outputs) {
-    int n;
-    if (rows_of_b(c.T, outs, a.blocks, a.groups, n) <= by_outputs) a.n = n;
-    else outputs = true;
-  }
+  a.n = plan.n;
+  const bool outputs = plan.outputs;
   const int64_t m = outputs ? outs : c.T, n = outputs ? c.T : outs;
   a.tiles_m = int((m + kSide - 1) / kSide);
   a.tiles = int(a.tiles_m * ((n + a.n - 1) / a.n));

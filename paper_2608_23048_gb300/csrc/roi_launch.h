@@ -251,9 +251,15 @@ int launch_wgrad(const WgradCall& c);
 int launch_fp8_save(const Fp8SaveCall& c);
 int launch_fp8_save_weight(const Fp8SaveCall& c);
 int launch_fp8_linear(const Fp8LinearCall& c);
-// (many tokens; and the time it would take, in cycles)
-int launch_fp8_pair(const Fp8LinearCall& c);
-int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width);
+// Many tokens, by pairs of CTAs: with outputs or tokens as the 256 rows of a tile, and n of the others.
+struct Fp8PairPlan {
+  int n;
+  bool outputs;
+};
+// The plan of the least time with `groups` pairs, and that time in cycles; `tokens`: whether tokens may be the rows.
+int64_t fp8_pair_cycles(int64_t T, int64_t outs, int64_t width, bool tokens, int groups, Fp8PairPlan& plan);
+bool fp8_pair_tokens(const Fp8LinearCall& c);
+int launch_fp8_pair(const Fp8LinearCall& c, const Fp8PairPlan& plan);
 int launch_optim(const OptimCall& c, const OptimItem* items, int count);
 int launch_fwd(const FwdCall& c);
 int launch_bwd(const BwdCall& c);
