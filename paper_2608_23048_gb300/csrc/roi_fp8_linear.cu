@@ -11,9 +11,12 @@
 // fewer than the SMs, a range of its sum: the CTAs of a tile are a cluster, copy their sums into one another's shared memory and
 // add them in the order of the ranges, each for some of the tokens.  Many tokens go to roi_fp8_pair.cu.
 //
-// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 13.7 from memory; the rest is a call's start and end.
-// Ranges joined by bulk copies: 777 tokens of 1531 x 1001 5.9 us, 7.1 in one range a tile, 46 where each sum was stored into the
-// other CTAs' memory by itself; 37 tokens of 128 x 896 4.3, 9.7 by stores.
+// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 12.7 from memory, call after call; the rest is a call's start
+// and end.  What ranges of a sum give, call after call in a graph, weights in L2, by the ranges that plan() takes: one token of
+// 3584 x 18944 in five 16.0 us, in one 46.3; 200 tokens of 640 x 6000 (fp32) in eight 10.8, in one 16.9, in five 9.7; 37 tokens of
+// 896 x 4864 in eight 9.0, in one 14.2, in five 8.6; 37 of 1565 x 1941 in eight 8.5, in one 7.8, in four 7.2: what a range costs is
+// more for many of them than plan() counts.  One range, as taken: the gradient of 777 tokens, 1001 x 1531, 6.5 (in two 10.0), 37
+// tokens of 128 x 896 5.0 (6.3 to 6.9 in two to seven).
 #include <atomic>
 
 #include "roi_fp8.cuh"
@@ -301,9 +304,11 @@ uint32_t join_bytes(int n, int splits) {
   return uint32_t(groups + (splits - 1) * each) * kGroupBytes;
 }
 
-// Blocks of the weight sent for ahead, where it is read once and a CTA's share is more than the ring holds.  One token of
-// 18944 x 3584, weights from memory, call after call: none, 8, 16, 24, 64 blocks 15.3, 14.6, 13.8, 14.8, 15.1 us.
-constexpr int kAhead = 16;
+// Blocks of the weight sent for ahead, where it is read once and a CTA's share is more than the ring holds.  Weights from memory,
+// us with 8, 12, 16 blocks: call after call, 1 token of 18944 x 3584 13.0, 12.7, 12.8 and behind the token's copy 14.9, 14.6, 15.1, 16 tokens
+// 12.9, 12.6, 12.9, 64 tokens 13.0, 13.3, 13.7, 1 token of 3584 x 18944 17.6, 17.3, 17.9, the gradient of 16 tokens 13.0, 13.4, 13.6; in a
+// graph, 1 token of 18944 x 3584 14.0, 14.0, 14.9 (with none 15.0, 4 14.3, 24 16.3), of 3584 x 18944 18.2, 17.5, 17.7 (none 18.6).
+constexpr int kAhead = 12;
 
 template <bool DGRAD, Elem E>
 int launch(const CUtensorMap& tm_w, const CUtensorMap& tm_x, const LinearArgs& a, int64_t grid, cudaStream_t stream) {
