@@ -11,7 +11,7 @@
 // fewer than the SMs, a range of its sum: the CTAs of a tile are a cluster, copy their sums into one another's shared memory and
 // add them in the order of the ranges, each for some of the tokens.  Many tokens go to roi_fp8_pair.cu.
 //
-// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 12.7 from memory, call after call; the rest is a call's start
+// One token of 18944 x 3584 is bound by the weight's bytes, 10 us of 12.8 from memory, call after call; the rest is a call's start
 // and end.  What ranges of a sum give, call after call in a graph, weights in L2, by the ranges that plan() takes: one token of
 // 3584 x 18944 in five 16.0 us, in one 46.3; 200 tokens of 640 x 6000 (fp32) in eight 10.8, in one 16.9, in five 9.7; 37 tokens of
 // 896 x 4864 in eight 9.0, in one 14.2, in five 8.6; 37 of 1565 x 1941 in eight 8.5, in one 7.8, in four 7.2: what a range costs is
@@ -304,11 +304,15 @@ uint32_t join_bytes(int n, int splits) {
   return uint32_t(groups + (splits - 1) * each) * kGroupBytes;
 }
 
-// Blocks of the weight sent for ahead, where it is read once and a CTA's share is more than the ring holds.  Weights from memory,
-// us with 8, 12, 16 blocks: call after call, 1 token of 18944 x 3584 13.0, 12.7, 12.8 and behind the token's copy 14.9, 14.6, 15.1, 16 tokens
-// 12.9, 12.6, 12.9, 64 tokens 13.0, 13.3, 13.7, 1 token of 3584 x 18944 17.6, 17.3, 17.9, the gradient of 16 tokens 13.0, 13.4, 13.6; in a
-// graph, 1 token of 18944 x 3584 14.0, 14.0, 14.9 (with none 15.0, 4 14.3, 24 16.3), of 3584 x 18944 18.2, 17.5, 17.7 (none 18.6).
-constexpr int kAhead = 12;
+// Blocks of the weight sent for ahead, where it is read once and a CTA's share is more than the ring holds.  Twelve to sixteen are
+// best, by what stands before the call.  Weights from memory, us with 8, 12, 16 blocks:
+//   1 token of 18944 x 3584, copied before it, other inputs each time   15.6, 15.3, 15.1 (4: 15.9)
+//     the same input, 4 weights in turn                                 14.9, 14.6, 15.1; the product alone 13.0, 12.7, 12.8
+//     in a graph, the product alone                                     14.0, 14.0, 14.9 (none 15.0, 4: 14.3, 24: 16.3)
+//   16 and 64 tokens of it, alone                                       12.9, 12.6, 12.9 and 13.0, 13.3, 13.7
+//   1 token of 3584 x 18944, alone                                      17.6, 17.3, 17.9; in a graph 18.2, 17.5, 17.7 (none 18.6)
+//   input gradient of 16 tokens, 18944 x 3584, alone                    13.0, 13.4, 13.6
+constexpr int kAhead = 16;
 
 template <bool DGRAD, Elem E>
 int launch(const CUtensorMap& tm_w, const CUtensorMap& tm_x, const LinearArgs& a, int64_t grid, cudaStream_t stream) {
